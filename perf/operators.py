@@ -241,7 +241,7 @@ def _recurrence_own(s):
     binding.bagel_recurrence(s["value"], s["forget"], r["hidden"], s["offsets"], bias=s["bias"], initial=s["initial"], final=r["final"],
                              carry=carry)
     binding.bagel_recurrence_grad(s["value"], s["forget"], s["d_hidden"], r["d_value"], r["d_forget"], s["offsets"], carry, bias=s["bias"],
-                                  d_final=s["d_final"], d_initial=r["d_initial"], d_bias=r["d_bias"])
+                                  initial=s["initial"], d_final=s["d_final"], d_initial=r["d_initial"], d_bias=r["d_bias"])
     return r
 
 
