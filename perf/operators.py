@@ -330,7 +330,7 @@ def _recurrence_plain(s):
     before = torch.cat([h0[:1], h[:-1]])
     before[first] = h0[full]
     # the same recurrence backwards: the gradient of h_t takes that of h_{t+1} times 1 - q_{t+1}
-    d = s["d_hidden"].float()
+    d = s["d_hidden"].to(torch.float32, copy=True)
     d[last] += s["d_final"][full]
     back = torch.cat([a[1:], a[:1]])
     back[last] = 0
