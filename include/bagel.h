@@ -308,8 +308,159 @@ int bagel_profile_enable(bagel_ctx *ctx, int every);
 int bagel_profile_read(bagel_ctx *ctx, double *kernel_ms, int *launches);
 
 /* Message of the last error on this context ("" if none); valid until the next call on it.
- * With ctx == NULL: message of the last failed bagel_create on this thread. */
+ * With ctx == NULL: message of the last failed call without a context on this thread (bagel_create among them). */
 const char *bagel_last_error(const bagel_ctx *ctx);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * Operators of a policy with memory.
+ *
+ * Where not every state of a machine is measured, a policy has to remember: it is a stack of recurrent blocks that read recorded
+ * trajectories whole in training and one control period at a time in use.  The calls below are what such a stack needs beside its
+ * matrix products: the join of two blocks, the recurrence, and an optimiser over many tensors.  They need no context: they enqueue
+ * kernels on `hip_stream` (NULL: the default stream) of the current device and return, allocate nothing and do not synchronise, so
+ * they may be captured into a HIP graph.  Work space, where a call needs any, is the caller's: as many bytes as the *_workspace call says, at
+ * a multiple of 16 bytes, holding anything before and nothing of use after the call.
+ * The message of a failed call is bagel_last_error(NULL).
+ *
+ * Activations are matrices of `rows` x `width` in one of three types, with rows a `stride` apart (in elements, at least the width
+ * where there are several rows) and the entries of a row next to each other; any start and any stride is allowed, those that are multiples
+ * of 16 bytes are faster.  Parameters, states that pass from step to step and their gradients are contiguous float32.  All
+ * arithmetic is in float32; a result in 16 bits is rounded once, to nearest.  Matrices of one call may not overlap where one of them is
+ * written, but for the pairs that are named.  NaN and infinities are not screened; they stay within the row (join) or the sequence (recurrence)
+ * that they come in, except in the gradients of the parameters, which are sums over all.
+ */
+#define BAGEL_FLOAT32 0
+#define BAGEL_BFLOAT16 1
+#define BAGEL_FLOAT16 2
+
+typedef struct {
+    void *data;              /* device pointer, or NULL for a matrix that is left out */
+    int64_t stride;          /* elements from one row to the next */
+} bagel_matrix;
+
+/*
+ * The end of one block and the start of the next: the norm after the block, its gate, the residual sum and the norm before
+ * the next block.  With R(z) = z / sqrt(mean(z^2) + eps) over a row,
+ *   out    = resid + scale * act(gate) * (R(branch) * post_weight)
+ *   normed = R(out) * pre_weight
+ * gate: BAGEL_ACT_NONE (no gate is read, act = 1), or act(g) = g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  Vectors of `width`
+ * that are NULL stand for ones.  `branch` may be left out (out = resid: the first block's norm), and so may `out` or `normed`.
+ * `normed` is the norm of `out` before it is rounded.  `out` may be `resid` itself.
+ *
+ * bagel_block_join_grad: the gradient for given d_out and d_normed (either may be left out: zero), at the stored `out`
+ * (`resid` is not read).  Any of d_branch, d_gate, d_resid, d_post_weight, d_scale and d_pre_weight may be left out.  d_resid may be d_out
+ * itself.  The gradients of the vectors are sums over all rows in an order that depends on the sizes alone: two calls on
+ * the same inputs give the same bits.
+ * rows >= 0, 1 <= width <= BAGEL_JOIN_MAX_WIDTH, eps > 0.  Errors: EINVAL, EHIP.
+ */
+#define BAGEL_JOIN_MAX_WIDTH 16384
+#define BAGEL_ACT_NONE 0
+#define BAGEL_ACT_IDENTITY 1
+#define BAGEL_ACT_LOGISTIC 2
+#define BAGEL_ACT_SILU 3
+
+typedef struct {
+    int64_t rows;
+    int32_t width, dtype, act;
+    float eps;
+    bagel_matrix branch, gate, resid, out, normed;
+    const float *post_weight, *scale, *pre_weight;
+    /* gradients (not looked at by bagel_block_join) */
+    bagel_matrix d_out, d_normed, d_branch, d_gate, d_resid;
+    float *d_post_weight, *d_scale, *d_pre_weight;
+    void *workspace;         /* needed for the gradients of the vectors */
+    int64_t workspace_bytes;
+} bagel_join;
+
+int64_t bagel_block_join_workspace(int64_t rows, int32_t width);
+int bagel_block_join(const bagel_join *args, void *hip_stream);
+int bagel_block_join_grad(const bagel_join *args, void *hip_stream);
+
+/*
+ * Gated linear recurrence of every channel along the steps of a sequence:
+ *   q_t = 1 / (1 + exp(forget_t + bias)),   h_t = h_{t-1} + q_t (value_t - h_{t-1}),
+ * over `sequences` sequences packed one after the other in the rows of value, forget and hidden: sequence i has the rows offsets[i] to
+ * offsets[i+1] - 1 (offsets[sequences+1], int32 on the device, not decreasing, offsets[0] = 0) and may be empty.  Rows from
+ * offsets[sequences] on belong to no sequence: what they hold is not used, and their results are zero.  offsets NULL:
+ * sequences of equal length, `sequences` divides `rows`.  (Offsets that break these rules give wrong numbers, but no access
+ * outside of the arrays.)
+ *   initial[sequences][width]  h before the first step, NULL: zero
+ *   final_state[sequences][width] or NULL: h after the last step; of an empty sequence, its initial state
+ *   carry[bagel_recurrence_carry_rows(rows)][width] or NULL: what bagel_recurrence_grad needs of the forward pass, h before the
+ *   rows 0, BAGEL_RECURRENCE_SPAN, 2 BAGEL_RECURRENCE_SPAN, ... (where a sequence begins there, anything finite)
+ *
+ * bagel_recurrence_grad: from the same value, forget, bias, initial and offsets, that carry, d_hidden (the gradient for
+ * hidden) and d_final[sequences][width] (for final_state, NULL: zero): d_value, d_forget, d_initial[sequences][width] and d_bias[width],
+ * any of which may be left out.  h itself is computed again in float32 and not read.  d_bias is a sum over all rows in an order
+ * that depends on the sizes alone.
+ *
+ * bagel_recurrence_step: one step of `sequences` sequences, whose rows are value, forget and hidden; state[sequences][width] is
+ * updated in place, hidden is the new state in the type of the activations (it may be left out).
+ * rows >= 0, below 2^31 - BAGEL_RECURRENCE_SPAN; sequences >= 0 (>= 1 where there are rows); width >= 1, below 2^20.  Errors: EINVAL, EHIP.
+ */
+#define BAGEL_RECURRENCE_SPAN 128
+
+typedef struct {
+    int64_t rows;
+    int32_t width, dtype, sequences;
+    const int32_t *offsets;
+    bagel_matrix value, forget, hidden;
+    const float *bias, *initial;             /* NULL: zeros */
+    float *final_state, *carry;
+    float *state;                            /* bagel_recurrence_step only */
+    /* gradients (looked at by bagel_recurrence_grad only) */
+    bagel_matrix d_hidden, d_value, d_forget;
+    const float *d_final;
+    float *d_initial, *d_bias;
+    void *workspace;                         /* bagel_recurrence and bagel_recurrence_grad */
+    int64_t workspace_bytes;
+} bagel_gated_recurrence;
+
+int64_t bagel_recurrence_carry_rows(int64_t rows);
+int64_t bagel_recurrence_workspace(int64_t rows, int32_t width);
+int bagel_recurrence(const bagel_gated_recurrence *args, void *hip_stream);
+int bagel_recurrence_grad(const bagel_gated_recurrence *args, void *hip_stream);
+int bagel_recurrence_step(const bagel_gated_recurrence *args, void *hip_stream);
+
+/*
+ * One update of many tensors by Adam with decoupled weight decay.  Update number step >= 1, with g = grad * grad_scale[0]:
+ *   m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   param <- (1 - lr weight_decay) param - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps);  copy <- param.
+ * param is float32, grad and copy (a working copy of the parameters, NULL: none) in the types given.  grad_scale is a device scalar, NULL:
+ * one; where it holds an infinity or NaN (a loss scale that overflowed), the call changes nothing.
+ * The tensors are an array on the host, read before the call returns; any number, of any count >= 0, at any alignment of their type
+ * (multiples of 16 bytes are faster).
+ * state_bits 32: m and v are float32[count].
+ * state_bits 8: m and v are float8 e4m3 codes[count] in blocks of BAGEL_ADAMW_BLOCK, with a float32 scale for each, m_scale and
+ *   v_scale[ceil(count / BAGEL_ADAMW_BLOCK)], both zero at the start.  m = code * scale and sqrt(v) = code * scale, where scale = (largest magnitude
+ *   of the block) / 448.  A value between two codes becomes one or the other by chance, so that its mean is kept: with beta2 = 0.999 a step
+ *   moves v by far less than codes are apart, and rounding to nearest would lose every move.  The chance is 16 bits of a hash of
+ *   the place in the tensor, `step` and `seed`: the library draws no random numbers, and equal calls give equal results.  A root
+ *   above zero never becomes code zero, which would make its next update unbounded.  Blocks whose largest magnitude is below 1e-30 are held as zero.
+ * lr >= 0, 0 <= beta < 1, eps > 0 (also as a float), lr weight_decay < 1.  Errors: EINVAL, EHIP.
+ */
+#define BAGEL_ADAMW_BLOCK 256
+
+typedef struct {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;                /* state_bits 8 only */
+    void *copy;
+    int64_t count;
+    double weight_decay;
+} bagel_adamw_tensor;
+
+typedef struct {
+    int64_t step;
+    double lr, beta1, beta2, eps;
+    const float *grad_scale;
+    int32_t grad_dtype, copy_dtype, state_bits;
+    uint32_t seed;
+} bagel_adamw;
+
+int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_tensors, const bagel_adamw *options, void *hip_stream);
 
 #ifdef __cplusplus
 }

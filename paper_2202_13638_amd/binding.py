@@ -22,7 +22,10 @@ EXPORTS = ["bagel_num_params", "bagel_create", "bagel_destroy", "bagel_workspace
            "bagel_prepare_samples", "bagel_set_samples", "bagel_rollout_loss",
            "bagel_rollout_loss_grad", "bagel_sample_eval", "bagel_last_error", "bagel_adam_step", "bagel_optimize",
            "bagel_hyper_lml_grad", "bagel_hyper_fit", "bagel_prepare_posterior", "bagel_posterior_rollout_loss", "bagel_posterior_rollout_loss_grad",
-           "bagel_profile_enable", "bagel_profile_read", "bagel_sample_eval_static"]
+           "bagel_profile_enable", "bagel_profile_read", "bagel_sample_eval_static",
+           "bagel_block_join", "bagel_block_join_grad", "bagel_block_join_workspace",
+           "bagel_recurrence", "bagel_recurrence_grad", "bagel_recurrence_step", "bagel_recurrence_workspace",
+           "bagel_recurrence_carry_rows", "bagel_adamw_step"]
 
 
 class BagelError(RuntimeError):
@@ -65,6 +68,39 @@ def dims_from_config(cfg, S: Optional[int] = None, **kw) -> Dims:
     return make_dims(d_s=cfg.d_s, d_a=cfg.d_a, d_g=cfg.d_g, N=cfg.N, L=cfg.L,
                      S=cfg.B if S is None else S, B=cfg.B, H=cfg.H, hidden=cfg.hidden,
                      act_bound=cfg.act_bound, tracked=cfg.tracked, q=cfg.q, **kw)
+
+
+def _matrices(*names):
+    return [f for n in names for f in ((n, C.c_void_p), (n + "_stride", C.c_int64))]
+
+
+class _Join(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float),
+                *_matrices("branch", "gate", "resid", "out", "normed"),
+                ("post_weight", C.c_void_p), ("scale", C.c_void_p), ("pre_weight", C.c_void_p),
+                *_matrices("d_out", "d_normed", "d_branch", "d_gate", "d_resid"),
+                ("d_post_weight", C.c_void_p), ("d_scale", C.c_void_p), ("d_pre_weight", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class _Recurrence(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("sequences", C.c_int32), ("offsets", C.c_void_p),
+                *_matrices("value", "forget", "hidden"),
+                ("bias", C.c_void_p), ("initial", C.c_void_p), ("final", C.c_void_p), ("carry", C.c_void_p), ("state", C.c_void_p),
+                *_matrices("d_hidden", "d_value", "d_forget"),
+                ("d_final", C.c_void_p), ("d_initial", C.c_void_p), ("d_bias", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class _AdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64), ("weight_decay", C.c_double)]
+
+
+class _AdamW(C.Structure):
+    _fields_ = [("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("grad_scale", C.c_void_p), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
+                ("seed", C.c_uint32)]
 
 
 _lib = None
@@ -119,6 +155,15 @@ def load():
         L.bagel_optimize.argtypes = [vp] + [fp] * 5 + [C.c_int] * 3 + [C.c_float] * 4 + [fp]
         L.bagel_sample_eval_static.restype = C.c_int
         L.bagel_sample_eval_static.argtypes = [C.POINTER(Dims), vp] + [fp] * 10
+        L.bagel_block_join_workspace.restype = L.bagel_recurrence_workspace.restype = L.bagel_recurrence_carry_rows.restype = C.c_int64
+        L.bagel_block_join_workspace.argtypes = L.bagel_recurrence_workspace.argtypes = [C.c_int64, C.c_int32]
+        L.bagel_recurrence_carry_rows.argtypes = [C.c_int64]
+        for name in ("bagel_block_join", "bagel_block_join_grad"):
+            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [C.POINTER(_Join), vp]
+        for name in ("bagel_recurrence", "bagel_recurrence_grad", "bagel_recurrence_step"):
+            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [C.POINTER(_Recurrence), vp]
+        L.bagel_adamw_step.restype = C.c_int
+        L.bagel_adamw_step.argtypes = [vp, C.c_int32, C.POINTER(_AdamW), vp]
         L.bagel_last_error.restype = C.c_char_p
         L.bagel_last_error.argtypes = [vp]
         _lib = L
@@ -162,6 +207,257 @@ def bagel_sample_eval_static(dims: Dims, X, lengthscale, signal_var, omega, phas
         _ptr(jac, (dims.B, M, D), "jac", optional=True))
     if rc != OK:
         raise BagelError(rc, lib.bagel_last_error(None).decode())
+
+
+# ---------------------------------------------------------------------------- operators of a policy with memory
+# Outputs are tensors of the caller; what is None is left out.  `stream` None: torch's current one.  All tensors are on the current device.
+JOIN_MAX_WIDTH, RECURRENCE_SPAN, ADAMW_BLOCK = 16384, 128, 256
+_ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
+_DTYPES = None
+
+
+def _dtype_code(t, name):
+    global _DTYPES
+    import torch
+    if _DTYPES is None:
+        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None:
+        raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor")
+    return code
+
+
+def _matrix(args, name, t, like):
+    """A matrix argument: shape, type and device of `like`, the entries of a row next to each other, any row stride."""
+    if t is None:
+        return
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape != like.shape:
+        raise ValueError(f"{name} must be a {like.dtype} tensor of shape {tuple(like.shape)} on {like.device}, "
+                         f"not {t.dtype} of {tuple(t.shape)} on {t.device}")
+    rows, width = like.shape
+    stride, step = t.stride()
+    if step != 1 and width > 1 and rows > 0:
+        raise ValueError(f"{name}: the entries of a row must be next to each other")
+    setattr(args, name, t.data_ptr())
+    setattr(args, name + "_stride", stride if rows > 1 else width)
+
+
+def _vector(args, name, t, shape, device):
+    if t is not None:
+        setattr(args, name, _ptr(t, shape, name))
+        if t.get_device() != device:
+            raise ValueError(f"{name} must be on cuda:{device}")
+
+
+def _first_matrix(t, name):
+    """(rows, width, type, device) of the matrix that the others of a call are held to."""
+    import torch
+    code = _dtype_code(t, name)
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current GPU")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, rows and width, not {t.dim()}")
+    return t.shape[0], t.shape[1], code, t.get_device()
+
+
+def _workspace(args, workspace, need, device, stream):
+    """The caller's work space, or one from torch's allocator on the call's stream."""
+    import torch
+    if workspace is None:
+        with torch.cuda.stream(stream):
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{device}")
+    args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    return workspace
+
+
+def _run(lib, call, args, stream):
+    if stream is None:
+        import torch
+        stream = torch.cuda.current_stream()
+    rc = call(args, stream.cuda_stream)
+    if rc != OK:
+        raise BagelError(rc, lib.bagel_last_error(None).decode())
+
+
+def bagel_block_join_workspace(rows: int, width: int) -> int:
+    """Bytes of work space of bagel_block_join_grad."""
+    return int(load().bagel_block_join_workspace(rows, width))
+
+
+def _join_args(first, name, gate, act, eps, post_weight, scale, pre_weight):
+    if act not in _ACTS:
+        raise ValueError(f"act must be one of {sorted(_ACTS)}")
+    args = _Join()
+    args.rows, args.width, args.dtype, device = _first_matrix(first, name)
+    args.act, args.eps = _ACTS[act], eps
+    _matrix(args, "gate", gate, first)
+    shape = (args.width,)
+    _vector(args, "post_weight", post_weight, shape, device)
+    _vector(args, "scale", scale, shape, device)
+    _vector(args, "pre_weight", pre_weight, shape, device)
+    return args, device
+
+
+def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None, eps=1e-6,
+                     stream=None):
+    """out = resid + scale * act(gate) * (R(branch) * post_weight), normed = R(out) * pre_weight (see include/bagel.h)."""
+    lib = load()
+    first, name = (resid, "resid") if resid is not None else (branch, "branch")
+    args, _ = _join_args(first, name, gate, act, eps, post_weight, scale, pre_weight)
+    for key, t in (("branch", branch), ("resid", resid), ("out", out), ("normed", normed)):
+        _matrix(args, key, t, first)
+    _run(lib, lib.bagel_block_join, args, stream)
+
+
+def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None,
+                          eps=1e-6, d_branch=None, d_gate=None, d_resid=None, d_post_weight=None, d_scale=None, d_pre_weight=None,
+                          workspace=None, stream=None):
+    """The gradient of bagel_block_join at the `out` it stored (see include/bagel.h)."""
+    lib = load()
+    args, device = _join_args(out, "out", gate, act, eps, post_weight, scale, pre_weight)
+    for key, t in (("branch", branch), ("out", out), ("d_out", d_out), ("d_normed", d_normed), ("d_branch", d_branch), ("d_gate", d_gate),
+                   ("d_resid", d_resid)):
+        _matrix(args, key, t, out)
+    shape = (args.width,)
+    _vector(args, "d_post_weight", d_post_weight, shape, device)
+    _vector(args, "d_scale", d_scale, shape, device)
+    _vector(args, "d_pre_weight", d_pre_weight, shape, device)
+    keep = None
+    if d_post_weight is not None or d_scale is not None or d_pre_weight is not None:
+        keep = _workspace(args, workspace, lib.bagel_block_join_workspace(args.rows, args.width), device, stream)
+    _run(lib, lib.bagel_block_join_grad, args, stream)
+    del keep
+
+
+def bagel_recurrence_carry_rows(rows: int) -> int:
+    """Rows of `carry`, the part of the forward pass that bagel_recurrence_grad needs, for so many rows of activations."""
+    return int(load().bagel_recurrence_carry_rows(rows))
+
+
+def bagel_recurrence_workspace(rows: int, width: int) -> int:
+    """Bytes of work space of bagel_recurrence and bagel_recurrence_grad."""
+    return int(load().bagel_recurrence_workspace(rows, width))
+
+
+def _recurrence_args(value, forget, offsets, bias):
+    """`offsets`: an int32 tensor on the GPU, or the number of sequences of equal length."""
+    import torch
+    args = _Recurrence()
+    args.rows, args.width, args.dtype, device = _first_matrix(value, "value")
+    if isinstance(offsets, torch.Tensor):
+        if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
+            raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
+        args.sequences, args.offsets = offsets.numel() - 1, offsets.data_ptr()
+    else:
+        args.sequences = int(offsets)
+    _matrix(args, "value", value, value)
+    if forget is None:
+        raise ValueError("forget is required")
+    _matrix(args, "forget", forget, value)
+    _vector(args, "bias", bias, (args.width,), device)
+    return args, device
+
+
+def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None, final=None, carry=None, workspace=None, stream=None):
+    """h_t = h_{t-1} + q_t (value_t - h_{t-1}), q_t = 1 / (1 + exp(forget_t + bias)), along packed sequences (see include/bagel.h)."""
+    lib = load()
+    args, device = _recurrence_args(value, forget, offsets, bias)
+    _matrix(args, "hidden", hidden, value)
+    shape = (args.sequences, args.width)
+    _vector(args, "initial", initial, shape, device)
+    _vector(args, "final", final, shape, device)
+    _vector(args, "carry", carry, (lib.bagel_recurrence_carry_rows(args.rows), args.width), device)
+    keep = _workspace(args, workspace, lib.bagel_recurrence_workspace(args.rows, args.width), device, stream)
+    _run(lib, lib.bagel_recurrence, args, stream)
+    del keep
+
+
+def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, carry, *, bias=None, initial=None, d_final=None, d_initial=None,
+                          d_bias=None, workspace=None, stream=None):
+    """The gradient of bagel_recurrence, with the `carry` it wrote (see include/bagel.h)."""
+    lib = load()
+    args, device = _recurrence_args(value, forget, offsets, bias)
+    for key, t in (("d_hidden", d_hidden), ("d_value", d_value), ("d_forget", d_forget)):
+        _matrix(args, key, t, value)
+    shape = (args.sequences, args.width)
+    _vector(args, "initial", initial, shape, device)
+    _vector(args, "d_final", d_final, shape, device)
+    _vector(args, "d_initial", d_initial, shape, device)
+    _vector(args, "d_bias", d_bias, (args.width,), device)
+    _vector(args, "carry", carry, (lib.bagel_recurrence_carry_rows(args.rows), args.width), device)
+    keep = _workspace(args, workspace, lib.bagel_recurrence_workspace(args.rows, args.width), device, stream)
+    _run(lib, lib.bagel_recurrence_grad, args, stream)
+    del keep
+
+
+def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, stream=None):
+    """One step of as many sequences as there are rows, the float32 state updated in place (see include/bagel.h)."""
+    lib = load()
+    if forget is None or state is None:
+        raise ValueError("forget and state are required")
+    args = _Recurrence()
+    rows, args.width, args.dtype, device = _first_matrix(value, "value")
+    args.sequences = rows
+    for key, t in (("value", value), ("forget", forget), ("hidden", hidden)):
+        _matrix(args, key, t, value)
+    _vector(args, "bias", bias, (args.width,), device)
+    _vector(args, "state", state, (rows, args.width), device)
+    _run(lib, lib.bagel_recurrence_step, args, stream)
+
+
+def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, copy=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
+                     weight_decay=0.01, grad_scale=None, seed=0, stream=None):
+    """One update of a list of tensors (see include/bagel.h).
+
+    params: contiguous float32 tensors; grads, m, v, copy (None: none): lists of tensors of the same shapes.  grads are all of one
+    type, and so are the entries of copy.  m and v are float32, or float8_e4m3fn with m_scale and v_scale, lists of float32 tensors
+    with an entry for every ADAMW_BLOCK values.  weight_decay: a number, or one for every tensor."""
+    import torch
+    lib = load()
+    n = len(params)
+    eight = n > 0 and m[0].dtype == torch.float8_e4m3fn
+    state = torch.float8_e4m3fn if eight else torch.float32
+    decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+    lists = [params, grads, m, v, decay] + ([copy] if copy is not None else []) + ([m_scale, v_scale] if eight else [])
+    if any(x is None or len(x) != n for x in lists):
+        raise ValueError("the lists of one update must have an entry for every tensor (moments in 8 bits need m_scale and v_scale)")
+    options = _AdamW()
+    options.step, options.lr, options.beta1, options.beta2, options.eps, options.seed = int(step), lr, beta1, beta2, eps, int(seed) & 0xFFFFFFFF
+    options.state_bits = 8 if eight else 32
+    if n:
+        device = torch.cuda.current_device()
+        options.grad_dtype = _dtype_code(grads[0], "grads")
+        types = [torch.float32, grads[0].dtype, state, state]
+        columns = [params, grads, m, v]
+        if copy is not None:
+            options.copy_dtype = _dtype_code(copy[0], "copy")
+            types.append(copy[0].dtype)
+            columns.append(copy)
+        if grad_scale is not None:
+            options.grad_scale = _ptr(grad_scale, tuple(grad_scale.shape), "grad_scale")
+            if grad_scale.numel() != 1 or grad_scale.get_device() != device:
+                raise ValueError("grad_scale must hold one value and be on the current GPU")
+        table = (_AdamWTensor * n)()
+        for i in range(n):
+            shape = params[i].shape
+            for x, t in zip(columns, types):
+                x = x[i]
+                if x.dtype != t or x.shape != shape or not x.is_contiguous() or x.get_device() != device:
+                    raise ValueError(f"tensor {i} of an update: a contiguous {t} tensor of shape {tuple(shape)} on cuda:{device} is needed, "
+                                     f"not {x.dtype} of {tuple(x.shape)} on {x.device}")
+            count = params[i].numel()
+            scales = (None, None)
+            if eight:
+                blocks = (-(-count // ADAMW_BLOCK),)
+                scales = (_ptr(m_scale[i], blocks, "m_scale"), _ptr(v_scale[i], blocks, "v_scale"))
+            table[i] = (params[i].data_ptr(), grads[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr(), *scales,
+                        copy[i].data_ptr() if copy is not None else None, count, decay[i])
+        _run(lib, lambda o, s: lib.bagel_adamw_step(table, n, o, s), options, stream)
 
 
 class Bagel:

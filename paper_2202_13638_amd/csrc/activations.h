@@ -1,0 +1,52 @@
+// What the operators of a policy with memory share: activations in three types, their checks on the host, and small device functions.
+// Nothing here is part of the public ABI (see include/bagel.h).
+#pragma once
+
+#include <math.h>
+
+#include "bagel_internal.h"
+
+// Sets the message of bagel_last_error(NULL) on this thread and returns `code` (bagel_api.hip).
+int bagel_refuse(int code, const char *format, ...) __attribute__((format(printf, 2, 3)));
+void bagel_no_error();
+
+inline int bagel_type_bytes(int dtype) { return dtype == BAGEL_FLOAT32 ? 4 : 2; }
+inline bool bagel_type_ok(int dtype) { return dtype == BAGEL_FLOAT32 || dtype == BAGEL_BFLOAT16 || dtype == BAGEL_FLOAT16; }
+
+// Whether a matrix that is there can be addressed: its start at a multiple of its type, and rows that do not overlap.
+inline bool bagel_matrix_ok(const bagel_matrix &m, int64_t rows, int64_t width, int dtype)
+{
+    return !m.data || (((uintptr_t)m.data & (bagel_type_bytes(dtype) - 1)) == 0 && (rows <= 1 || (m.stride >= width && m.stride < (1ll << 40))));
+}
+
+// The largest power of two up to `most` such that packs of so many entries are aligned in every row of m.
+inline int bagel_matrix_pack(const bagel_matrix &m, int64_t rows, int dtype, int most)
+{
+    if (!m.data) return most;
+    const uint64_t places = (uint64_t)(uintptr_t)m.data / bagel_type_bytes(dtype) | (rows > 1 ? (uint64_t)m.stride : 0);
+    while (most > 1 && (places & (most - 1))) most /= 2;
+    return most;
+}
+
+// Launches f<type>() for the type that `dtype` says.
+template <typename T> struct bagel_type { using type = T; };
+template <typename F> hipError_t bagel_by_type(int dtype, F &&f)
+{
+    if (dtype == BAGEL_FLOAT32) return f(bagel_type<float>());
+    if (dtype == BAGEL_BFLOAT16) return f(bagel_type<__bf16>());
+    return f(bagel_type<_Float16>());
+}
+
+template <typename T> struct bagel_rows {
+    T *data;
+    int64_t stride;
+    __device__ __forceinline__ T *row(int64_t r) const { return data + r * stride; }
+};
+template <typename T> inline bagel_rows<T> bagel_rows_of(const bagel_matrix &m) { return {(T *)m.data, m.stride}; }
+
+__device__ __forceinline__ float bagel_wave_sum(float v)
+{
+#pragma unroll
+    for (int i = 32; i > 0; i >>= 1) v += __shfl_xor(v, i);
+    return v;
+}

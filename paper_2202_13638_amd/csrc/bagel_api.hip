@@ -7,12 +7,14 @@
 // bagel_optimize wraps that in the inner loop of Algorithm 1 with an Adam update per iteration.
 #include <math.h>
 #include <stdio.h>
+#include <stdarg.h>
 #include <stdlib.h>
 #include <string.h>
 
 #include <mutex>
 #include <new>
 
+#include "activations.h"
 #include "bagel_internal.h"
 
 static thread_local char g_create_err[512] = "";
@@ -22,6 +24,17 @@ static thread_local char g_create_err[512] = "";
         snprintf(g_create_err, sizeof(g_create_err), __VA_ARGS__); \
         return (code);                                            \
     } while (0)
+
+int bagel_refuse(int code, const char *format, ...)
+{
+    va_list args;
+    va_start(args, format);
+    vsnprintf(g_create_err, sizeof(g_create_err), format, args);
+    va_end(args);
+    return code;
+}
+
+void bagel_no_error() { g_create_err[0] = 0; }
 
 static const char *check_dims(const bagel_dims *d)
 {
