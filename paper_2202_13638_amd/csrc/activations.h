@@ -44,9 +44,46 @@ template <typename T> struct bagel_rows {
 };
 template <typename T> inline bagel_rows<T> bagel_rows_of(const bagel_matrix &m) { return {(T *)m.data, m.stride}; }
 
+// V entries of a row, one load or store of up to 16 bytes.
+template <typename T, int V> using bagel_pack = T __attribute__((ext_vector_type(V)));
+
+template <typename T, int V> __device__ __forceinline__ void bagel_load(const T *p, float (&v)[V])
+{
+    if constexpr (V == 1) {
+        v[0] = (float)*p;
+    } else {
+        const bagel_pack<T, V> x = *reinterpret_cast<const bagel_pack<T, V> *>(p);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)x[i];
+    }
+}
+
+template <typename T, int V> __device__ __forceinline__ void bagel_store(T *p, const float (&v)[V])
+{
+    if constexpr (V == 1) {
+        *p = (T)v[0];
+    } else {
+        bagel_pack<T, V> x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+        *reinterpret_cast<bagel_pack<T, V> *>(p) = x;
+    }
+}
+
+// Data-parallel moves within 16 lanes: 0xB1 swaps neighbours, 0x4E pairs, 0x141 mirrors 8 lanes, 0x140 all 16.
+template <int MOVE> __device__ __forceinline__ float bagel_moved(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), MOVE, 0xF, 0xF, false));
+}
+
+// The sum over the 64 lanes of a wave, the same in all of them.
 __device__ __forceinline__ float bagel_wave_sum(float v)
 {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) v += __shfl_xor(v, i);
-    return v;
+    v += bagel_moved<0xB1>(v);
+    v += bagel_moved<0x4E>(v);
+    v += bagel_moved<0x141>(v);
+    v += bagel_moved<0x140>(v);
+    const int i = __float_as_int(v);
+    return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));
 }

@@ -1,13 +1,15 @@
 // Adam with decoupled weight decay over many tensors at once (include/bagel.h), the moments in 32 bits or in 8 with a scale for
 // every 256 values.
 //
-// A launch takes up to TENSORS tensors by value, with the number of the first block of each: the table of a thousand tensors needs no
+// A launch takes up to TENSORS tensors by value, with the number of the first piece of each: the table of a thousand tensors needs no
 // memory on the device that would have to be filled, kept and waited for.
+#include <type_traits>
+
 #include "activations.h"
 
 namespace {
 
-constexpr int TENSORS = 48;                  // 72 bytes each, within the 4 KB of a kernel's arguments
+constexpr int TENSORS = 48;                  // 76 bytes each, within the 4 KB of a kernel's arguments
 constexpr int BLOCK = BAGEL_ADAMW_BLOCK;
 constexpr float LARGEST = 448.0f;            // of float8 e4m3
 
@@ -19,30 +21,81 @@ struct adamw_tensor {
     void *copy;
     int64_t count;
     float keep;                  // 1 - lr weight_decay
-    uint32_t first;              // its first block of 256
+    int pack;                    // whether four entries at a time are aligned in all of them
 };
 
 struct adamw_args {
     adamw_tensor tensor[TENSORS];
+    uint32_t first[TENSORS];     // the first piece of each
     const float *grad_scale;
     int n, grad_dtype, copy_dtype;
-    uint32_t blocks, key;        // of all tensors
+    uint32_t pieces, key;        // of all tensors
+    int each;                    // blocks of 256 that a wave takes of a piece: a piece is 4 each
     float beta1, rest1, beta2, rest2, rate, root, eps;       // rate = lr / (1 - beta1^step), root = 1 / sqrt(1 - beta2^step)
 };
 static_assert(sizeof(adamw_args) <= 4096, "kernel arguments");
 
-__device__ __forceinline__ float load_as(const void *p, int64_t i, int dtype)
+// Four entries of a block, in a row (PACK) or 64 apart; those from `rest` on are not there.
+template <bool PACK> __device__ __forceinline__ int place(int i) { return PACK ? 4 * (threadIdx.x & 63) + i : 64 * i + (threadIdx.x & 63); }
+
+template <bool PACK, typename T> __device__ __forceinline__ void load_four(const void *p, int64_t from, int64_t rest, float (&v)[4])
 {
-    if (dtype == BAGEL_FLOAT32) return ((const float *)p)[i];
-    if (dtype == BAGEL_BFLOAT16) return (float)((const __bf16 *)p)[i];
-    return (float)((const _Float16 *)p)[i];
+    const T *q = (const T *)p + from;
+    if constexpr (PACK) bagel_load<T, 4>(q + place<true>(0), v);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = place<false>(i) < rest ? (float)q[place<false>(i)] : 0.0f;
 }
 
-__device__ __forceinline__ void store_as(void *p, int64_t i, float v, int dtype)
+template <bool PACK, typename T> __device__ __forceinline__ void store_four(void *p, int64_t from, int64_t rest, const float (&v)[4])
 {
-    if (dtype == BAGEL_FLOAT32) ((float *)p)[i] = v;
-    else if (dtype == BAGEL_BFLOAT16) ((__bf16 *)p)[i] = (__bf16)v;
-    else ((_Float16 *)p)[i] = (_Float16)v;
+    T *q = (T *)p + from;
+    if constexpr (PACK) bagel_store<T, 4>(q + place<true>(0), v);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (place<false>(i) < rest) q[place<false>(i)] = (T)v[i];
+}
+
+template <bool PACK> __device__ __forceinline__ void load_as(const void *p, int64_t from, int64_t rest, int dtype, float (&v)[4])
+{
+    if (dtype == BAGEL_FLOAT32) load_four<PACK, float>(p, from, rest, v);
+    else if (dtype == BAGEL_BFLOAT16) load_four<PACK, __bf16>(p, from, rest, v);
+    else load_four<PACK, _Float16>(p, from, rest, v);
+}
+
+template <bool PACK> __device__ __forceinline__ void store_as(void *p, int64_t from, int64_t rest, int dtype, const float (&v)[4])
+{
+    if (dtype == BAGEL_FLOAT32) store_four<PACK, float>(p, from, rest, v);
+    else if (dtype == BAGEL_BFLOAT16) store_four<PACK, __bf16>(p, from, rest, v);
+    else store_four<PACK, _Float16>(p, from, rest, v);
+}
+
+template <bool PACK> __device__ __forceinline__ void load_codes(const void *p, int64_t from, int64_t rest, float (&v)[4])
+{
+    const uint8_t *q = (const uint8_t *)p + from;
+    int bytes = 0;
+    if constexpr (PACK) bytes = *(const int *)(q + place<true>(0));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (place<false>(i) < rest) bytes |= (int)q[place<false>(i)] << 8 * i;
+    v[0] = __builtin_amdgcn_cvt_f32_fp8(bytes, 0);
+    v[1] = __builtin_amdgcn_cvt_f32_fp8(bytes, 1);
+    v[2] = __builtin_amdgcn_cvt_f32_fp8(bytes, 2);
+    v[3] = __builtin_amdgcn_cvt_f32_fp8(bytes, 3);
+}
+
+template <bool PACK> __device__ __forceinline__ void store_codes(void *p, int64_t from, int64_t rest, const float (&v)[4])
+{
+    uint8_t *q = (uint8_t *)p + from;
+    int bytes = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+    bytes = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], bytes, true);
+    if constexpr (PACK) *(int *)(q + place<true>(0)) = bytes;
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (place<false>(i) < rest) q[place<false>(i)] = (uint8_t)(bytes >> 8 * i);
 }
 
 // 32 random bits for every place of a tensor: a product with an odd number near 2^32 / golden ratio spreads the places, two rounds of shift
@@ -65,76 +118,98 @@ __device__ __forceinline__ float code_of(float y, uint32_t r)
     return fminf(y >= 1.0f / 64.0f ? normal : small, LARGEST);
 }
 
-__device__ __forceinline__ uint8_t byte_of(float code) { return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(code, code, 0, false); }
-__device__ __forceinline__ float value_of(uint8_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
-
-// fmaxf that keeps a NaN
-__device__ __forceinline__ float larger(float a, float b) { return a != a || a > b ? a : b; }
-
-__device__ __forceinline__ float group_max(float v, float *shared)
+// The largest magnitude in a wave.  As whole numbers the bits of magnitudes have the same order, and NaN is the largest of all: it is kept.
+__device__ __forceinline__ float largest(const float (&v)[4])
 {
-#pragma unroll
-    for (int i = 32; i > 0; i >>= 1) v = larger(__shfl_xor(v, i), v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return larger(larger(shared[0], shared[1]), larger(shared[2], shared[3]));
+    const auto bits = [](float x) { return __float_as_uint(x) & 0x7FFFFFFFu; };
+    const auto moved = [](uint32_t x, auto move) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(move)::value, 0xF, 0xF, false); };
+    uint32_t x = max(max(bits(v[0]), bits(v[1])), max(bits(v[2]), bits(v[3])));
+    x = max(x, moved(x, std::integral_constant<int, 0xB1>()));
+    x = max(x, moved(x, std::integral_constant<int, 0x4E>()));
+    x = max(x, moved(x, std::integral_constant<int, 0x141>()));
+    x = max(x, moved(x, std::integral_constant<int, 0x140>()));
+    const int i = (int)x;
+    return __uint_as_float(max(max((uint32_t)__builtin_amdgcn_readlane(i, 0), (uint32_t)__builtin_amdgcn_readlane(i, 16)),
+                               max((uint32_t)__builtin_amdgcn_readlane(i, 32), (uint32_t)__builtin_amdgcn_readlane(i, 48))));
 }
 
-template <int BITS> __global__ __launch_bounds__(BLOCK) void adamw_kernel(adamw_args a)
+// Codes of a block, and its scale in every lane.  ROOT: of roots, of which none above zero becomes zero.
+template <bool ROOT> __device__ __forceinline__ float encode(float (&v)[4], const uint32_t (&bits)[4])
 {
-    __shared__ float shared[4];
+    float top = largest(v);
+    if (top < 1e-30f) top = 0.0f;
+    const float scale = top > 0.0f ? 1.0f / top * LARGEST : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float code = code_of(fminf(fabsf(v[i]) * scale, LARGEST), ROOT ? bits[i] >> 16 : bits[i] & 0xFFFFu);
+        v[i] = !ROOT ? copysignf(code, v[i]) : v[i] > 0.0f && top > 0.0f ? fmaxf(code, 1.0f / 512.0f) : code;
+    }
+    return top * (1.0f / LARGEST);
+}
+
+template <int BITS, bool PACK> __device__ __forceinline__ void update_block(const adamw_args &a, const adamw_tensor &w, int64_t block, float gs)
+{
+    const int64_t from = block * BLOCK, rest = w.count - from;
+    float g[4], p[4], m[4], v[4], r[4];
+    load_as<PACK>(w.grad, from, rest, a.grad_dtype, g);
+    load_four<PACK, float>(w.param, from, rest, p);
+    if (BITS == 32) {
+        load_four<PACK, float>(w.m, from, rest, m);
+        load_four<PACK, float>(w.v, from, rest, v);
+    } else {
+        const float sm = w.m_scale[block], sv = w.v_scale[block];
+        load_codes<PACK>(w.m, from, rest, m);
+        load_codes<PACK>(w.v, from, rest, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] *= sm;
+            v[i] *= sv;
+            v[i] *= v[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        g[i] *= gs;
+        m[i] = m[i] * a.beta1 + g[i] * a.rest1;
+        v[i] = v[i] * a.beta2 + g[i] * a.rest2 * g[i];
+        r[i] = sqrtf(v[i]);
+        p[i] = p[i] * w.keep - m[i] * a.rate / (r[i] * a.root + a.eps);
+    }
+    store_four<PACK, float>(w.param, from, rest, p);
+    if (w.copy) store_as<PACK>(w.copy, from, rest, a.copy_dtype, p);
+    if (BITS == 32) {
+        store_four<PACK, float>(w.m, from, rest, m);
+        store_four<PACK, float>(w.v, from, rest, v);
+    } else {
+        uint32_t bits[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits[i] = chance((uint32_t)from + place<PACK>(i), a.key);
+        const float sm = encode<false>(m, bits), sv = encode<true>(r, bits);
+        store_codes<PACK>(w.m, from, rest, m);
+        store_codes<PACK>(w.v, from, rest, r);
+        if ((threadIdx.x & 63) == 0) {
+            w.m_scale[block] = sm;
+            w.v_scale[block] = sv;
+        }
+    }
+}
+
+// A wave takes a block of 256 at a time, four entries a lane: the block's largest magnitude is a matter of one wave.
+template <int BITS> __global__ __launch_bounds__(256) void adamw_kernel(adamw_args a)
+{
     const float gs = a.grad_scale ? a.grad_scale[0] : 1.0f;
     if (!isfinite(gs)) return;
-    for (uint32_t at = blockIdx.x; at < a.blocks; at += gridDim.x) {
-        int k = 0;
-        for (int i = 1; i < a.n; ++i)
-            if (a.tensor[i].first <= at) k = i;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t mine = lane < a.n ? a.first[lane] : 0xFFFFFFFFu;
+    for (uint32_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
+        const int k = __popcll(__ballot(mine <= piece)) - 1;     // the last tensor that does not begin behind it
         const adamw_tensor &w = a.tensor[k];
-        const int64_t block = at - w.first, i = block * BLOCK + threadIdx.x;
-        const bool here = i < w.count;
-        float m = 0.0f, v = 0.0f, g = 0.0f, p = 0.0f;
-        if (here) {
-            g = load_as(w.grad, i, a.grad_dtype) * gs;
-            p = w.param[i];
-            if (BITS == 32) {
-                m = ((const float *)w.m)[i];
-                v = ((const float *)w.v)[i];
-            } else {
-                m = value_of(((const uint8_t *)w.m)[i]) * w.m_scale[block];
-                v = value_of(((const uint8_t *)w.v)[i]) * w.v_scale[block];
-                v *= v;
-            }
+        const int64_t blocks = (w.count + BLOCK - 1) / BLOCK;
+        int64_t block = (int64_t)(piece - a.first[k]) * 4 * a.each + wave;
+        for (int i = 0; i < a.each && block < blocks; ++i, block += 4) {
+            if (w.pack && (block + 1) * BLOCK <= w.count) update_block<BITS, true>(a, w, block, gs);
+            else update_block<BITS, false>(a, w, block, gs);
         }
-        m = m * a.beta1 + g * a.rest1;
-        v = v * a.beta2 + g * a.rest2 * g;
-        const float r = sqrtf(v);
-        p = p * w.keep - m * a.rate / (r * a.root + a.eps);
-        if (here) {
-            w.param[i] = p;
-            if (w.copy) store_as(w.copy, i, p, a.copy_dtype);
-        }
-        if (BITS == 32) {
-            if (here) {
-                ((float *)w.m)[i] = m;
-                ((float *)w.v)[i] = v;
-            }
-            continue;
-        }
-        const uint32_t c = chance((uint32_t)i, a.key);
-        float top = group_max(fabsf(m), shared);
-        if (top < 1e-30f) top = 0.0f;
-        float scale = top > 0.0f ? 1.0f / top * LARGEST : 0.0f;
-        float code = code_of(fminf(fabsf(m) * scale, LARGEST), c & 0xFFFFu);
-        if (here) ((uint8_t *)w.m)[i] = byte_of(copysignf(code, m));
-        if (threadIdx.x == 0) w.m_scale[block] = top * (1.0f / LARGEST);
-        top = group_max(r, shared);
-        if (top < 1e-30f) top = 0.0f;
-        scale = top > 0.0f ? 1.0f / top * LARGEST : 0.0f;
-        code = code_of(fminf(r * scale, LARGEST), c >> 16);
-        if (r > 0.0f && top > 0.0f) code = fmaxf(code, 1.0f / 512.0f);
-        if (here) ((uint8_t *)w.v)[i] = byte_of(code);
-        if (threadIdx.x == 0) w.v_scale[block] = top * (1.0f / LARGEST);
     }
 }
 
@@ -179,25 +254,34 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
     a.rate = (float)(o->lr / (1.0 - pow(o->beta1, (double)o->step)));
     a.root = (float)(1.0 / sqrt(1.0 - pow(o->beta2, (double)o->step)));
     a.eps = (float)o->eps;
-    uint32_t blocks = 0;
+    // Few blocks are spread over as many waves as there are; of many, a wave takes four one after the other.
+    int64_t all = 0;
+    for (int i = 0; i < n_tensors; ++i) all += (tensors[i].count + BLOCK - 1) / BLOCK;
+    a.each = all < 16384 ? 1 : 4;
     a.n = 0;
-    auto launch = [&]() {
-        a.blocks = blocks;
-        const unsigned groups = blocks < 1u << 20 ? blocks : 1u << 20;
-        if (o->state_bits == 8) adamw_kernel<8><<<groups, BLOCK, 0, (hipStream_t)hip_stream>>>(a);
-        else adamw_kernel<32><<<groups, BLOCK, 0, (hipStream_t)hip_stream>>>(a);
+    a.pieces = 0;
+    const auto launch = [&]() {
+        const unsigned groups = a.pieces < 1u << 20 ? a.pieces : 1u << 20;
+        if (o->state_bits == 8) adamw_kernel<8><<<groups, 256, 0, (hipStream_t)hip_stream>>>(a);
+        else adamw_kernel<32><<<groups, 256, 0, (hipStream_t)hip_stream>>>(a);
         a.n = 0;
-        blocks = 0;
+        a.pieces = 0;
         return hipGetLastError();
     };
+    const int state_bytes = o->state_bits == 32 ? 4 : 1;
     hipError_t e = hipSuccess;
     for (int i = 0; i < n_tensors && e == hipSuccess; ++i) {
         const bagel_adamw_tensor &t = tensors[i];
         if (t.count == 0) continue;
-        const uint32_t more = (uint32_t)((t.count + BLOCK - 1) / BLOCK);
-        if (a.n == TENSORS || (a.n > 0 && blocks + more > 1u << 30)) e = launch();
-        a.tensor[a.n++] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay), blocks};
-        blocks += more;
+        const uint32_t pieces = (uint32_t)((t.count + 4 * a.each * BLOCK - 1) / (4 * a.each * BLOCK));
+        if (a.n == TENSORS || (a.n > 0 && a.pieces + pieces > 1u << 30)) {
+            if ((e = launch()) != hipSuccess) break;
+        }
+        const uintptr_t off = ((uintptr_t)t.param & 15) | ((uintptr_t)t.grad & (4 * bagel_type_bytes(o->grad_dtype) - 1)) |
+                              (((uintptr_t)t.m | (uintptr_t)t.v) & (4 * state_bytes - 1)) | ((uintptr_t)t.copy & (4 * bagel_type_bytes(o->copy_dtype) - 1));
+        a.tensor[a.n] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay), off == 0};
+        a.first[a.n++] = a.pieces;
+        a.pieces += pieces;
     }
     if (e == hipSuccess && a.n > 0) e = launch();
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_adamw_step: %s", hipGetErrorString(e));

@@ -12,162 +12,336 @@ namespace {
 
 template <typename T> struct join_args {
     int64_t rows;
-    int width;
+    int width, act;
     float eps;
     bagel_rows<T> branch, gate, resid, out, normed, d_out, d_normed, d_branch, d_gate, d_resid;
     const float *post_weight, *scale, *pre_weight;
-    float *sums;                 // [workgroups][3][width]: d_post_weight, d_scale, d_pre_weight of a workgroup's rows
+    float *sums;                 // [workgroups][2][width]: sums over a workgroup's rows of dx a n (d_post_weight without its factor c, and d_scale
+                                 // without w) and of d_normed out ro (d_pre_weight)
 };
 
 // act(g) and its derivative.  For an infinite g the logistic function is 0 or 1 exactly, and so is its derivative.
-template <int ACT> __device__ __forceinline__ float act(float g, float &slope)
+__device__ __forceinline__ float act(int kind, float g, float &slope)
 {
-    if constexpr (ACT == BAGEL_ACT_NONE) {
-        slope = 0.0f;
-        return 1.0f;
-    } else if constexpr (ACT == BAGEL_ACT_IDENTITY) {
+    if (kind == BAGEL_ACT_IDENTITY) {
         slope = 1.0f;
         return g;
-    } else {
-        const float sig = 1.0f / (1.0f + __expf(-g));
-        const float rest = 1.0f / (1.0f + __expf(g));        // 1 - sig without cancellation
-        if constexpr (ACT == BAGEL_ACT_LOGISTIC) {
-            slope = sig * rest;
-            return sig;
-        }
-        slope = sig + g * sig * rest;
-        return g * sig;
     }
+    const float e = __expf(-fabsf(g)), r = 1.0f / (1.0f + e), s = e * r;         // logistic(|g|) and logistic(-|g|), both without cancellation
+    const float sig = g < 0.0f ? s : r, rest = g < 0.0f ? r : s;
+    const bool silu = kind == BAGEL_ACT_SILU;
+    slope = silu ? sig + g * sig * rest : sig * rest;
+    return silu ? g * sig : sig;
 }
 
-// Sums of N values over a workgroup, in a fixed order.
-template <int N> __device__ __forceinline__ void group_sum(float (&v)[N], float (*shared)[N])
+// Sums of N values over the WAVES waves that share a row, in a fixed order.  Two buffers take turns (`turn`), so that one barrier is enough: a
+// wave that is ahead writes the other one, and cannot come back to this one before all have read it.
+template <int WAVES, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float (*shared)[WAVES][4], int &turn)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = bagel_wave_sum(v[i]);
-    __syncthreads();
-    if (lane == 0)
+    if constexpr (WAVES > 1) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
 #pragma unroll
-        for (int i = 0; i < N; ++i) shared[wave][i] = v[i];
-    __syncthreads();
+            for (int i = 0; i < N; ++i) shared[turn][wave][i] = v[i];
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = 0.0f;
-        for (int k = 0; k < waves; ++k) v[i] += shared[k][i];
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) v[i] += shared[turn][k][i];
+        }
+        turn ^= 1;
     }
 }
 
-__device__ __forceinline__ float at(const float *p, int i) { return p ? p[i] : 1.0f; }
-
-template <typename T, int ACT> __device__ __forceinline__ float join_out(const join_args<T> &a, int64_t r, int i, float rz)
-{
-    float v = a.resid.data ? (float)a.resid.row(r)[i] : 0.0f;
-    if (a.branch.data) {
-        float slope;
-        const float g = ACT == BAGEL_ACT_NONE ? 0.0f : (float)a.gate.row(r)[i];
-        v += at(a.scale, i) * act<ACT>(g, slope) * ((float)a.branch.row(r)[i] * rz * at(a.post_weight, i));
+// A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i.  One wave to a row leaves four rows to a
+// workgroup, which need nothing of each other.
+template <int V, int K, int WAVES> struct tile {
+    static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, rows = WAVES == 1 ? 4 : 1;
+    __device__ static __forceinline__ int column(int k) { return V * (64 * WAVES * k + (WAVES == 1 ? threadIdx.x & 63 : threadIdx.x)); }
+    __device__ static __forceinline__ int64_t first_row() { return WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x; }
+    __device__ static __forceinline__ int64_t next_row() { return (int64_t)gridDim.x * rows; }
+    // vectors of the row's width, ones where there is none
+    __device__ static __forceinline__ void vector(const float *p, int width, float (&v)[K][V])
+    {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] = p && column(k) < width ? p[column(k) + i] : 1.0f;
     }
-    return v;
-}
+    __device__ static __forceinline__ void product(const float *p, const float *q, int width, float (&v)[K][V])
+    {
+        float w[K][V];
+        vector(p, width, v);
+        vector(q, width, w);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] *= w[k][i];
+    }
+    template <typename T> __device__ static __forceinline__ void load(const T *row, int width, float (&v)[K][V])
+    {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (row && column(k) < width) bagel_load<T, V>(row + column(k), v[k]);
+            else
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[k][i] = 0.0f;
+        }
+    }
+    template <typename T> __device__ static __forceinline__ void store(T *row, int width, const float (&v)[K][V])
+    {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (column(k) < width) bagel_store<T, V>(row + column(k), v[k]);
+    }
+};
 
-template <typename T, int ACT> __global__ __launch_bounds__(256) void join_kernel(join_args<T> a)
+template <typename T, int V, int K, int WAVES, bool GATED>
+__global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join_args<T> a)
 {
-    __shared__ float shared[4][1];
-    extern __shared__ float row_out[];
-    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        float s[1] = {0.0f};
+    using tl = tile<V, K, WAVES>;
+    __shared__ float shared[2][WAVES][4];
+    int turn = 0;
+    const float per = 1.0f / a.width;
+    float cw[K][V], u[K][V];
+    tl::product(a.scale, a.post_weight, a.width, cw);
+    tl::vector(a.pre_weight, a.width, u);
+    for (int64_t r = tl::first_row(); r < a.rows; r += tl::next_row()) {
+        float z[K][V], g[K][V], v[K][V], s[1] = {0.0f};
+        tl::load(a.branch.data ? a.branch.row(r) : nullptr, a.width, z);
+        if (GATED) tl::load(a.gate.row(r), a.width, g);
+        tl::load(a.resid.data ? a.resid.row(r) : nullptr, a.width, v);
         if (a.branch.data) {
-            for (int i = threadIdx.x; i < a.width; i += 256) {
-                const float z = (float)a.branch.row(r)[i];
-                s[0] += z * z;
-            }
-            group_sum(s, shared);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s[0] += z[k][i] * z[k][i];
+            row_sum<WAVES>(s, shared, turn);
+            const float rz = 1.0f / sqrtf(s[0] * per + a.eps);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    float n = z[k][i] * rz, slope;
+                    if (GATED) n *= act(a.act, g[k][i], slope);
+                    v[k][i] += cw[k][i] * n;
+                }
         }
-        const float rz = 1.0f / sqrtf(s[0] / a.width + a.eps);
-        s[0] = 0.0f;
-        for (int i = threadIdx.x; i < a.width; i += 256) {
-            const float v = join_out<T, ACT>(a, r, i, rz);
-            row_out[i] = v;
-            if (a.out.data) a.out.row(r)[i] = (T)v;
-            s[0] += v * v;
-        }
+        if (a.out.data) tl::store(a.out.row(r), a.width, v);
         if (!a.normed.data) continue;
-        group_sum(s, shared);
-        const float ro = 1.0f / sqrtf(s[0] / a.width + a.eps);
-        for (int i = threadIdx.x; i < a.width; i += 256) a.normed.row(r)[i] = (T)(row_out[i] * ro * at(a.pre_weight, i));
+        s[0] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s[0] += v[k][i] * v[k][i];
+        row_sum<WAVES>(s, shared, turn);
+        const float ro = 1.0f / sqrtf(s[0] * per + a.eps);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] = v[k][i] * ro * u[k][i];
+        tl::store(a.normed.row(r), a.width, v);
     }
 }
 
-template <typename T, int ACT> __global__ __launch_bounds__(256) void join_grad_kernel(join_args<T> a)
+template <typename T, int V, int K, int WAVES, bool GATED>
+__global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_grad_kernel(join_args<T> a)
 {
-    __shared__ float shared[4][3];
-    float *sums = a.sums ? a.sums + (size_t)blockIdx.x * 3 * a.width : nullptr;
+    using tl = tile<V, K, WAVES>;
+    __shared__ float shared[2][WAVES][4];
+    int turn = 0;
+    const float per = 1.0f / a.width;
+    float cw[K][V], u[K][V], sw[K][V], su[K][V];
+    tl::product(a.scale, a.post_weight, a.width, cw);
+    tl::vector(a.pre_weight, a.width, u);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < V; ++i) sw[k][i] = su[k][i] = 0.0f;
+    for (int64_t r = tl::first_row(); r < a.rows; r += tl::next_row()) {
+        float z[K][V], g[K][V], o[K][V], dy[K][V], dx[K][V], s[3] = {0.0f, 0.0f, 0.0f};
+        tl::load(a.out.row(r), a.width, o);
+        tl::load(a.d_normed.data ? a.d_normed.row(r) : nullptr, a.width, dy);
+        tl::load(a.branch.data ? a.branch.row(r) : nullptr, a.width, z);
+        if (GATED) tl::load(a.gate.row(r), a.width, g);
+        tl::load(a.d_out.data ? a.d_out.row(r) : nullptr, a.width, dx);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s[0] += z[k][i] * z[k][i];
+                s[1] += o[k][i] * o[k][i];
+                s[2] += dy[k][i] * u[k][i] * o[k][i];
+            }
+        row_sum<WAVES>(s, shared, turn);
+        const float rz = 1.0f / sqrtf(s[0] * per + a.eps), ro = 1.0f / sqrtf(s[1] * per + a.eps);
+        const float co = s[2] * per * ro * ro;
+        float t[1] = {0.0f};
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float n = o[k][i] * ro;
+                dx[k][i] += ro * (dy[k][i] * u[k][i]) - n * co;
+                su[k][i] += dy[k][i] * n;
+                float av = 1.0f, slope = 0.0f;
+                if (GATED) av = act(a.act, g[k][i], slope);
+                const float zn = z[k][i] * rz, x = dx[k][i] * cw[k][i];
+                sw[k][i] += dx[k][i] * av * zn;              // times c: d_post_weight, times w: d_scale
+                g[k][i] = x * zn * slope;
+                dy[k][i] = x * av;                           // gradient of R(branch)
+                t[0] += dy[k][i] * zn;
+            }
+        if (a.d_resid.data) tl::store(a.d_resid.row(r), a.width, dx);
+        if (GATED && a.d_gate.data) tl::store(a.d_gate.row(r), a.width, g);
+        if (!a.d_branch.data) continue;
+        row_sum<WAVES>(t, shared, turn);
+        const float cz = t[0] * per * rz;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) z[k][i] = rz * (dy[k][i] - z[k][i] * cz);
+        tl::store(a.d_branch.row(r), a.width, z);
+    }
+    if (!a.sums) return;
+    float *sums = a.sums + (size_t)blockIdx.x * 2 * a.width;
+    if constexpr (WAVES == 1) {              // four waves with sums of the same columns: added up in order
+        __shared__ float all[2][64 * K * V];
+        for (int wave = 0; wave < 4; ++wave) {
+            if ((int)(threadIdx.x >> 6) == wave)
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int j = tl::column(k) + i;
+                        all[0][j] = wave ? all[0][j] + sw[k][i] : sw[k][i];
+                        all[1][j] = wave ? all[1][j] + su[k][i] : su[k][i];
+                    }
+            __syncthreads();
+        }
+        for (int j = threadIdx.x; j < a.width; j += 256)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) sums[(size_t)q * a.width + j] = all[q][j];
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (tl::column(k) < a.width)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const int j = tl::column(k) + i;
+                    sums[j] = sw[k][i];
+                    sums[a.width + j] = su[k][i];
+                }
+    }
+}
+
+// Rows that registers do not hold (sixteen waves leave 128 to a lane): three passes over a row, the second and third out of the cache, and the sums
+// of a workgroup in its part of the work space.
+template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void join_grad_wide_kernel(join_args<T> a)
+{
+    __shared__ float shared[2][16][4];
+    int turn = 0;
+    const float per = 1.0f / a.width;
+    float *sums = a.sums ? a.sums + (size_t)blockIdx.x * 2 * a.width : nullptr;
+    const int first = V * threadIdx.x;
     if (sums)
-        for (int i = threadIdx.x; i < 3 * a.width; i += 256) sums[i] = 0.0f;
+        for (int j = first; j < a.width; j += 1024 * V)
+#pragma unroll
+            for (int i = 0; i < V; ++i) sums[j + i] = sums[a.width + j + i] = 0.0f;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const T *branch = a.branch.data ? a.branch.row(r) : nullptr, *d_normed = a.d_normed.data ? a.d_normed.row(r) : nullptr;
+        const T *d_out = a.d_out.data ? a.d_out.row(r) : nullptr;
+        const auto read = [&](const T *row, int j, float (&v)[V]) {
+            if (row) bagel_load<T, V>(row + j, v);
+            else
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = 0.0f;
+        };
         float s[3] = {0.0f, 0.0f, 0.0f};
-        for (int i = threadIdx.x; i < a.width; i += 256) {
-            const float z = a.branch.data ? (float)a.branch.row(r)[i] : 0.0f, out = (float)a.out.row(r)[i];
-            s[0] += z * z;
-            s[1] += out * out;
-            if (a.d_normed.data) s[2] += (float)a.d_normed.row(r)[i] * at(a.pre_weight, i) * out;
+        for (int j = first; j < a.width; j += 1024 * V) {
+            float z[V], o[V], dy[V];
+            read(branch, j, z);
+            read(a.out.row(r), j, o);
+            read(d_normed, j, dy);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                s[0] += z[i] * z[i];
+                s[1] += o[i] * o[i];
+                s[2] += dy[i] * (a.pre_weight ? a.pre_weight[j + i] : 1.0f) * o[i];
+            }
         }
-        group_sum(s, shared);
-        const float rz = 1.0f / sqrtf(s[0] / a.width + a.eps), ro = 1.0f / sqrtf(s[1] / a.width + a.eps);
-        const float co = s[2] / a.width * ro * ro * ro;
-        float cz = 0.0f;
+        row_sum<16>(s, shared, turn);
+        const float rz = 1.0f / sqrtf(s[0] * per + a.eps), ro = 1.0f / sqrtf(s[1] * per + a.eps);
+        const float co = s[2] * per * ro * ro;
+        float t[1] = {0.0f};
+#pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
-            float k1[1] = {0.0f};
-            for (int i = threadIdx.x; i < a.width; i += 256) {
-                const float out = (float)a.out.row(r)[i], dy = a.d_normed.data ? (float)a.d_normed.row(r)[i] : 0.0f;
-                const float dx = (a.d_out.data ? (float)a.d_out.row(r)[i] : 0.0f) + ro * dy * at(a.pre_weight, i) - out * co;
-                float z = 0.0f, g = 0.0f, slope, k = 0.0f, n = 0.0f, av = 1.0f;
-                const float c = at(a.scale, i), w = at(a.post_weight, i);
-                if (a.branch.data) {
-                    z = (float)a.branch.row(r)[i];
-                    if (ACT != BAGEL_ACT_NONE) g = (float)a.gate.row(r)[i];
-                    av = act<ACT>(g, slope);
-                    n = z * rz;
-                    k = dx * c * av * w;
+            const float cz = t[0] * per * rz;
+            for (int j = first; j < a.width; j += 1024 * V) {
+                float z[V], g[V], o[V], dy[V], dx[V];
+                read(branch, j, z);
+                if (GATED) read(a.gate.row(r), j, g);
+                read(a.out.row(r), j, o);
+                read(d_normed, j, dy);
+                read(d_out, j, dx);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float n = o[i] * ro, cw = (a.scale ? a.scale[j + i] : 1.0f) * (a.post_weight ? a.post_weight[j + i] : 1.0f);
+                    dx[i] += ro * (dy[i] * (a.pre_weight ? a.pre_weight[j + i] : 1.0f)) - n * co;
+                    float av = 1.0f, slope = 0.0f;
+                    if (GATED) av = act(a.act, g[i], slope);
+                    const float zn = z[i] * rz, x = dx[i] * cw, k = x * av;
+                    if (pass == 0) {
+                        t[0] += k * zn;
+                        continue;
+                    }
+                    if (sums) {
+                        sums[j + i] += dx[i] * av * zn;
+                        sums[a.width + j + i] += dy[i] * n;
+                    }
+                    g[i] = x * zn * slope;
+                    z[i] = rz * (k - z[i] * cz);
                 }
-                if (pass == 0) {
-                    k1[0] += k * z;
-                    continue;
-                }
-                if (a.branch.data) {
-                    if (a.d_branch.data) a.d_branch.row(r)[i] = (T)(rz * k - z * cz);
-                    if (ACT != BAGEL_ACT_NONE && a.d_gate.data) a.d_gate.row(r)[i] = (T)(dx * c * w * n * slope);
-                }
-                if (sums) {
-                    sums[i] += dx * c * av * n;
-                    sums[a.width + i] += dx * av * w * n;
-                    sums[2 * a.width + i] += dy * out * ro;
-                }
-                if (a.d_resid.data) a.d_resid.row(r)[i] = (T)dx;
+                if (pass == 0) continue;
+                if (a.d_resid.data) bagel_store<T, V>(a.d_resid.row(r) + j, dx);
+                if (GATED && a.d_gate.data) bagel_store<T, V>(a.d_gate.row(r) + j, g);
+                if (a.d_branch.data) bagel_store<T, V>(a.d_branch.row(r) + j, z);
             }
-            if (pass == 0) {
-                group_sum(k1, reinterpret_cast<float (*)[1]>(shared));
-                cz = k1[0] / a.width * rz * rz * rz;
-                __syncthreads();
-            }
+            if (pass == 0) row_sum<16>(t, shared, turn);
         }
     }
 }
 
-// The gradients of the vectors: sums over the workgroups of the pass over the rows.
-__global__ __launch_bounds__(256) void join_sums_kernel(const float *sums, int groups, int width, float *d_post, float *d_scale, float *d_pre)
+// The gradients of the vectors: sums over the workgroups of the pass over the rows.  16 threads to a column, each with a part of the workgroups.
+__global__ __launch_bounds__(1024) void join_sums_kernel(const float *sums, int groups, int width, const float *post, const float *scale, float *d_post,
+                                                         float *d_scale, float *d_pre)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= 3 * width) return;
-    float *to = i < width ? d_post : i < 2 * width ? d_scale : d_pre;
-    if (!to) return;
+    __shared__ float part[16][64];
+    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, i = blockIdx.x * 64 + lane, n = 2 * width;
     float v = 0.0f;
-    for (int k = 0; k < groups; ++k) v += sums[(size_t)k * 3 * width + i];
-    to[i % width] = v;
+    if (i < n) {
+        const int from = groups * slice / 16, to = groups * (slice + 1) / 16;
+#pragma unroll 8
+        for (int k = from; k < to; ++k) v += sums[(size_t)k * n + i];
+    }
+    part[slice][lane] = v;
+    __syncthreads();
+    if (slice > 0 || i >= n) return;
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) v += part[k][lane];
+    if (i >= width) {
+        if (d_pre) d_pre[i - width] = v;
+    } else {
+        if (d_post) d_post[i] = scale ? v * scale[i] : v;
+        if (d_scale) d_scale[i] = post ? v * post[i] : v;
+    }
 }
 
-constexpr int JOIN_GROUPS = 1024;
+constexpr int JOIN_GROUPS = 512;
 int grad_groups(int64_t rows) { return (int)(rows < JOIN_GROUPS ? rows : JOIN_GROUPS); }
 
 template <typename T> join_args<T> args_of(const bagel_join &j)
@@ -175,6 +349,7 @@ template <typename T> join_args<T> args_of(const bagel_join &j)
     join_args<T> a{};
     a.rows = j.rows;
     a.width = j.width;
+    a.act = j.act;
     a.eps = j.eps;
     a.branch = bagel_rows_of<T>(j.branch);
     a.gate = bagel_rows_of<T>(j.gate);
@@ -192,34 +367,80 @@ template <typename T> join_args<T> args_of(const bagel_join &j)
     return a;
 }
 
+// The number of workgroups.
+template <typename T, int V, int K, int WAVES, bool GRAD = true> int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
+{
+    constexpr int threads = tile<V, K, WAVES>::threads, rows = tile<V, K, WAVES>::rows;
+    const int64_t full = (a.rows + rows - 1) / rows, most = grad ? JOIN_GROUPS : 4096;
+    const int groups = (int)(full < most ? full : most);
+    const bool gated = a.act != BAGEL_ACT_NONE && a.branch.data;
+    if (GRAD && grad) {
+        if constexpr (GRAD) {
+            if (gated) join_grad_kernel<T, V, K, WAVES, true><<<groups, threads, 0, stream>>>(a);
+            else join_grad_kernel<T, V, K, WAVES, false><<<groups, threads, 0, stream>>>(a);
+        }
+    } else {
+        if (gated) join_kernel<T, V, K, WAVES, true><<<groups, threads, 0, stream>>>(a);
+        else join_kernel<T, V, K, WAVES, false><<<groups, threads, 0, stream>>>(a);
+    }
+    return groups;
+}
+
+template <typename T, int V> int launch_wide(const join_args<T> &a, hipStream_t stream)
+{
+    const int groups = grad_groups(a.rows);
+    if (a.act != BAGEL_ACT_NONE && a.branch.data) join_grad_wide_kernel<T, V, true><<<groups, 1024, 0, stream>>>(a);
+    else join_grad_wide_kernel<T, V, false><<<groups, 1024, 0, stream>>>(a);
+    return groups;
+}
+
+// A row is spread over as few waves as hold it with two packs a lane: fewer waves mean fewer barriers, more packs fewer waves on a compute unit.
+template <typename T, int V> int launch_width(const join_args<T> &a, bool grad, hipStream_t stream)
+{
+    const int packs = (a.width + V - 1) / V;
+    if constexpr (V > 1) {
+        if (packs <= 64) return launch_tile<T, V, 1, 1>(a, grad, stream);
+        if (packs <= 128) return launch_tile<T, V, 2, 1>(a, grad, stream);
+        if (packs <= 256) return launch_tile<T, V, 1, 4>(a, grad, stream);
+        if (packs <= 512) return launch_tile<T, V, 2, 4>(a, grad, stream);
+        if (packs <= 1024) return launch_tile<T, V, 2, 8>(a, grad, stream);
+        if (grad) return launch_wide<T, V>(a, stream);
+        if (packs <= 2048) return launch_tile<T, V, 2, 16, false>(a, grad, stream);
+        if constexpr (V == 4) return launch_tile<T, V, 4, 16, false>(a, grad, stream);
+        return 0;                            // (16384 entries of 16 bits are 2048 packs)
+    } else {
+        if (packs <= 256) return launch_tile<T, 1, 4, 1>(a, grad, stream);
+        if (packs <= 1024) return launch_tile<T, 1, 4, 4>(a, grad, stream);
+        if (packs <= 2048) return launch_tile<T, 1, 4, 8>(a, grad, stream);
+        if (grad) return launch_wide<T, 1>(a, stream);
+        if (packs <= 4096) return launch_tile<T, 1, 4, 16, false>(a, grad, stream);
+        return launch_tile<T, 1, 16, 16, false>(a, grad, stream);
+    }
+}
+
+template <typename T> int launch_rows(const join_args<T> &a, const bagel_join &j, bool grad, hipStream_t stream)
+{
+    constexpr int V = 16 / sizeof(T);
+    int pack = j.width % V ? 1 : V;
+    const bagel_matrix all[] = {j.branch, j.gate, j.resid, j.out, j.normed, j.d_out, j.d_normed, j.d_branch, j.d_gate, j.d_resid};
+    for (int i = 0; i < (grad ? 10 : 5); ++i) pack = bagel_matrix_pack(all[i], j.rows, j.dtype, pack);
+    return pack == V ? launch_width<T, V>(a, grad, stream) : launch_width<T, 1>(a, grad, stream);
+}
+
 template <typename T> hipError_t launch_join(const bagel_join &j, hipStream_t stream)
 {
-    const join_args<T> a = args_of<T>(j);
-    const int groups = (int)(j.rows < 65536 ? j.rows : 65536);
-    const size_t lds = sizeof(float) * j.width;
-    switch (j.act) {
-    case BAGEL_ACT_NONE: join_kernel<T, BAGEL_ACT_NONE><<<groups, 256, lds, stream>>>(a); break;
-    case BAGEL_ACT_IDENTITY: join_kernel<T, BAGEL_ACT_IDENTITY><<<groups, 256, lds, stream>>>(a); break;
-    case BAGEL_ACT_LOGISTIC: join_kernel<T, BAGEL_ACT_LOGISTIC><<<groups, 256, lds, stream>>>(a); break;
-    default: join_kernel<T, BAGEL_ACT_SILU><<<groups, 256, lds, stream>>>(a);
-    }
+    launch_rows(args_of<T>(j), j, false, stream);
     return hipGetLastError();
 }
 
 template <typename T> hipError_t launch_join_grad(const bagel_join &j, hipStream_t stream)
 {
     join_args<T> a = args_of<T>(j);
-    const int groups = grad_groups(j.rows);
     const bool sums = j.d_post_weight || j.d_scale || j.d_pre_weight;
     a.sums = sums ? (float *)j.workspace : nullptr;
-    if (groups > 0) switch (j.act) {
-        case BAGEL_ACT_NONE: join_grad_kernel<T, BAGEL_ACT_NONE><<<groups, 256, 0, stream>>>(a); break;
-        case BAGEL_ACT_IDENTITY: join_grad_kernel<T, BAGEL_ACT_IDENTITY><<<groups, 256, 0, stream>>>(a); break;
-        case BAGEL_ACT_LOGISTIC: join_grad_kernel<T, BAGEL_ACT_LOGISTIC><<<groups, 256, 0, stream>>>(a); break;
-        default: join_grad_kernel<T, BAGEL_ACT_SILU><<<groups, 256, 0, stream>>>(a);
-        }
+    const int groups = j.rows > 0 ? launch_rows(a, j, true, stream) : 0;
     if (sums)
-        join_sums_kernel<<<(3 * j.width + 255) / 256, 256, 0, stream>>>(a.sums, groups, j.width, j.d_post_weight, j.d_scale, j.d_pre_weight);
+        join_sums_kernel<<<(2 * j.width + 63) / 64, 1024, 0, stream>>>(a.sums, groups, j.width, j.post_weight, j.scale, j.d_post_weight, j.d_scale, j.d_pre_weight);
     return hipGetLastError();
 }
 
@@ -259,7 +480,7 @@ const char *check_join(const bagel_join *j, bool grad)
 extern "C" int64_t bagel_block_join_workspace(int64_t rows, int32_t width)
 {
     if (rows < 0 || width < 1 || width > BAGEL_JOIN_MAX_WIDTH) return BAGEL_EINVAL;
-    return (int64_t)grad_groups(rows) * 3 * width * sizeof(float);
+    return (int64_t)grad_groups(rows) * 2 * width * sizeof(float);
 }
 
 extern "C" int bagel_block_join(const bagel_join *j, void *hip_stream)
