@@ -397,7 +397,8 @@ int bagel_block_join_grad(const bagel_join *args, void *hip_stream);
  *
  * bagel_recurrence_step: one step of `sequences` sequences, whose rows are value, forget and hidden; state[sequences][width] is
  * updated in place, hidden is the new state in the type of the activations (it may be left out).
- * rows >= 0, below 2^31 - BAGEL_RECURRENCE_SPAN; sequences >= 0 (>= 1 where there are rows); width >= 1, below 2^20.  Errors: EINVAL, EHIP.
+ * rows >= 0, rows * ceil(width / 64) below 2^29; 0 <= sequences < 2^28 (>= 1 where there are rows); 1 <= width < 2^20; sequences * width of a
+ * step below 2^38.  Errors: EINVAL, EHIP.
  */
 #define BAGEL_RECURRENCE_SPAN 128
 
