@@ -14,6 +14,8 @@
 //   A published sum is one word of 64 bits a channel, A and H: it is whole as soon as it is there, and nothing else has to be ordered with it.
 //   Spans are handed out by a counter in the order in which they depend on each other.  So a workgroup waits only for spans handed out before
 //   its own, to workgroups that run already and publish their sums before they wait for anything: every wait ends.
+#include <type_traits>
+
 #include "activations.h"
 
 namespace {
@@ -41,11 +43,11 @@ constexpr float CLOSED = -1.0f;
 struct piece {
     float A, H;
 };
-__device__ __forceinline__ float through(const piece &p, float h) { return p.A == CLOSED ? p.H : p.A * h + p.H; }
+__device__ __forceinline__ float through(const piece &p, float h) { return p.A == CLOSED ? p.H : fmaf(p.A, h, p.H); }
 __device__ __forceinline__ piece joined(const piece &first, const piece &then)
 {
     if (then.A == CLOSED) return then;
-    return {first.A == CLOSED ? CLOSED : first.A * then.A, then.A * first.H + then.H};
+    return {first.A == CLOSED ? CLOSED : first.A * then.A, fmaf(then.A, first.H, then.H)};
 }
 
 __device__ __forceinline__ void publish(uint64_t *to, piece p)
@@ -94,7 +96,7 @@ template <int V> __device__ __forceinline__ void look_back(const uint64_t *publi
                 if (!found[v]) {
                     const piece p = {__uint_as_float((uint32_t)word[k][v]), __uint_as_float((uint32_t)(word[k][v] >> 32))};
                     found[v] = p.A == CLOSED;
-                    all[v] = {all[v].A * p.A, all[v].A * p.H + all[v].H};       // (where it is closed, A is of no more use)
+                    all[v] = {all[v].A * p.A, fmaf(all[v].A, p.H, all[v].H)};       // (where it is closed, A is of no more use)
                 }
             }
         }
@@ -112,13 +114,26 @@ template <int V> __device__ __forceinline__ void look_back(const uint64_t *publi
 template <int S> struct segment {
     uint64_t starts;
     int begin, end, sequence;
-    __device__ __forceinline__ bool plain() const { return (starts & ((1ull << S) - 1)) == 0 && begin == 0 && end == S; }
+    static constexpr uint64_t every = (1ull << S) - 1;
+    __device__ __forceinline__ bool whole() const { return begin == 0 && end == S; }
     __device__ __forceinline__ bool outside(int i) const { return i < begin || i >= end; }
-    __device__ __forceinline__ bool start(int i) const { return starts >> i & 1; }
-    __device__ __forceinline__ bool last(int i) const { return starts >> (i + 1) & 1; }
+    __device__ __forceinline__ bool start(int i) const { return !outside(i) && (starts >> i & 1); }
+    __device__ __forceinline__ bool last(int i) const { return !outside(i) && (starts >> (i + 1) & 1); }
+    // the rows that are not just one more of their sequence
+    __device__ __forceinline__ uint64_t special() const { return whole() ? starts | starts >> 1 : every; }
+    // whether what is before (behind) the segment does not reach through it
+    __device__ __forceinline__ bool closed() const { return !whole() || (starts & every); }
+    __device__ __forceinline__ bool closed_back() const { return !whole() || (starts >> 1 & every); }
 };
 
-template <int S, typename A> __device__ __forceinline__ segment<S> segment_at(const A &a, int t0)
+// The first look at the offsets, before the rows are asked for: every lane one, a 64th part of them from the next.
+template <typename A> __device__ __forceinline__ int some_offset(const A &a)
+{
+    const int step = a.sequences / 64 + 1;
+    return a.offsets ? a.offsets[min((int)(threadIdx.x & 63) * step, a.sequences)] : 0;
+}
+
+template <int S, typename A> __device__ __forceinline__ segment<S> segment_at(const A &a, int t0, int o)
 {
     static_assert(S < 64, "one lane to a row");
     const int lane = threadIdx.x & 63, n = a.sequences;
@@ -127,26 +142,24 @@ template <int S, typename A> __device__ __forceinline__ segment<S> segment_at(co
         const uint64_t starts = __ballot(lane <= S && (t0 + lane) % a.each == 0);
         return {starts, 0, max(0, min(S, a.rows - t0)), min(i, n - 1)};
     }
-    // the last offset that is not behind t0, by 64 of them at a time
-    int lo = 0, count = n + 1, found = -1;
-    while (count > 0) {
-        const int step = (count + 63) / 64, i = lo + lane * step;
-        const bool here = lane * step < count && a.offsets[min(i, n)] <= t0;
-        const int k = __popcll(__ballot(here));
-        if (k == 0) break;
-        found = lo + (k - 1) * step;
-        if (step == 1) break;
-        count = min(step, count - (k - 1) * step);
-        lo = found;
+    // Down to 64 offsets in a row, o, from number lo on, of which the first is not behind t0 (or is the first of all)
+    int lo = 0, step = n / 64 + 1;
+    const int first = a.offsets[0], stop = min(a.offsets[n], a.rows);
+    while (step > 1) {
+        const int k = __popcll(__ballot((int64_t)lo + (int64_t)lane * step <= n && o <= t0));
+        lo += max(k - 1, 0) * step;
+        step = (step + 62) / 63;
+        o = a.offsets[min((int64_t)lo + (int64_t)lane * step, (int64_t)n)];
     }
-    uint64_t starts = found >= 0 && a.offsets[found] == t0 ? 1 : 0;
-    for (int k = found + 1; k <= n; k += 64) {
-        const int o = k + lane <= n ? a.offsets[k + lane] : 0x7FFFFFFF;
+    if (lo + lane > n) o = 0x7FFFFFFF;
+    const int found = lo + __popcll(__ballot(o <= t0)) - 1;
+    uint64_t starts = __ballot(o == t0) ? 1 : 0;
+    for (int k = lo;;) {
         for (uint64_t in = __ballot(o > t0 && o <= t0 + S); in; in &= in - 1) starts |= 1ull << (__builtin_amdgcn_readlane(o, __builtin_ctzll(in)) - t0);
-        if (__ballot(o <= t0 + S) != ~0ull) break;
+        if (__ballot(o <= t0 + S) != ~0ull || (k += 64) > n) break;
+        o = k + lane <= n ? a.offsets[k + lane] : 0x7FFFFFFF;
     }
-    const int begin = a.offsets[0], end = min(a.offsets[n], a.rows);
-    return {starts, begin <= t0 ? 0 : min(S, begin - t0), end <= t0 ? 0 : min(S, end - t0), min(found, n - 1)};
+    return {starts, first <= t0 ? 0 : min(S, first - t0), stop <= t0 ? 0 : min(S, stop - t0), min(found, n - 1)};
 }
 
 // The sequence of row t, which begins one, from that of the row before it.
@@ -164,8 +177,17 @@ template <typename A> __device__ __forceinline__ void to_previous(const A &a, in
     sequence = max(sequence, 0);
 }
 
-__device__ __forceinline__ float share(float f) { return __builtin_amdgcn_rcpf(1.0f + __expf(f)); }
+// q for a forget gate f and bias b, which comes times log2(e).
+constexpr float LOG2E = 1.44269504f;
+__device__ __forceinline__ float share(float f, float b) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fmaf(f, LOG2E, b))); }
 __device__ __forceinline__ float at(const float *p, int64_t i) { return p ? p[i] : 0.0f; }
+
+// f(special) with a constant 0 where there is none: most segments lie within one sequence, and a branch at every row costs them a tenth.
+template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, F &&f)
+{
+    if (special == 0) f(std::integral_constant<uint64_t, 0>());
+    else f(special);
+}
 
 // What is the same in both directions: which span and channels a workgroup has, and its reads.
 template <typename T, int V, int S> struct wave_tile {
@@ -189,10 +211,58 @@ template <typename T, int V, int S> struct wave_tile {
 #pragma unroll
         for (int i = 0; i < S; ++i) x[i] = *reinterpret_cast<const pack *>(m.row(min(t0 + i, last)) + ch);
     }
+    // From here on the packs are what they are and not what they were converted to: the converted ones of two channels in 16 bits would take twice
+    // the registers between two passes over the rows.
+    static __device__ __forceinline__ void keep_packed(pack (&x)[S])
+    {
+        if constexpr (sizeof(pack) == 4 && V == 2)
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                uint32_t bits = __builtin_bit_cast(uint32_t, x[i]);
+                asm volatile("" : "+v"(bits));
+                x[i] = __builtin_bit_cast(pack, bits);
+            }
+    }
     static __device__ __forceinline__ float one(const pack &x, int v)
     {
         if constexpr (V == 1) return (float)x[0];
         else return (float)x[v];
+    }
+    // Rows that belong to no sequence: a value and a forget gate of which neither is NaN, so that zero stays zero.
+    __device__ __forceinline__ void clear_outside(const segment<S> &seg, pack (&f)[S], pack (&x)[S]) const
+    {
+        if (seg.whole()) return;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+            if (seg.outside(i)) f[i] = x[i] = (pack)(T)0.0f;
+    }
+    // h before row i, where that is not what the row before left: `h` of pieces or of states
+    __device__ __forceinline__ void enter(const recurrence_args<T> &a, const segment<S> &seg, int i, int &sequence, float (&h)[V]) const
+    {
+        if (seg.outside(i)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = 0.0f;
+        } else if (seg.start(i)) {
+            if (i > 0 || sequence < 0) to_next(a, t0 + i, sequence);
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = at(a.initial, (int64_t)sequence * a.width + ch + v);
+        }
+    }
+    __device__ __forceinline__ void enter(const recurrence_args<T> &a, const segment<S> &seg, int i, int &sequence, piece (&p)[V]) const
+    {
+        float h[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = p[v].H;
+        enter(a, seg, i, sequence, h);
+#pragma unroll
+        for (int v = 0; v < V; ++v) p[v].H = h[v];
+    }
+    // c behind row i, where that is not what the row behind it left
+    __device__ __forceinline__ void enter_back(const recurrence_args<T> &a, const segment<S> &seg, int i, int sequence, float (&c)[V]) const
+    {
+        if (seg.outside(i) || seg.last(i))
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] = seg.outside(i) ? 0.0f : at(a.d_final, (int64_t)sequence * a.width + ch + v);
     }
     __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const { bagel_store<T, V>(m.row(row) + ch, x); }
 };
@@ -229,56 +299,36 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     wt w(work, a);
     w.begin();
     typename wt::pack x[S], f[S];
+    const int some = some_offset(a);
     w.load(a.forget, a.rows - 1, f);
     w.load(a.value, a.rows - 1, x);
-    const segment<S> seg = segment_at<S>(a, w.t0);
-    const bool plain = seg.plain();
-    const auto initial = [&](int sequence, int v) { return at(a.initial, (int64_t)sequence * a.width + w.ch + v); };
-
+    const segment<S> seg = segment_at<S>(a, w.t0, some);
+    const uint64_t special = seg.special();
+    w.clear_outside(seg, f, x);
     float q[S][V], h[V];
     piece mine[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float b = at(a.bias, w.ch + v);
+        const float b = at(a.bias, w.ch + v) * LOG2E;
         mine[v] = {1.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v) + b);
+        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v), b);
     }
-    if (plain) {
-#pragma unroll
-        for (int i = 0; i < S; ++i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                mine[v].H += q[i][v] * (wt::one(x[i], v) - mine[v].H);
-                mine[v].A -= mine[v].A * q[i][v];
-            }
-    } else {
-        int sequence = seg.sequence;
-        bool closed = false;
+    int sequence = seg.sequence;
+    by_rows(special, [&](auto special) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            if (seg.outside(i)) {
-                closed = true;
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine[v].H = 0.0f;
-                continue;
-            }
-            if (seg.start(i)) {
-                closed = true;
-                if (i > 0 || sequence < 0) to_next(a, w.t0 + i, sequence);
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine[v].H = initial(sequence, v);
-            }
+            if (special >> i & 1) w.enter(a, seg, i, sequence, mine);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                mine[v].H += q[i][v] * (wt::one(x[i], v) - mine[v].H);
-                mine[v].A -= mine[v].A * q[i][v];
+                mine[v].H = fmaf(q[i][v], wt::one(x[i], v) - mine[v].H, mine[v].H);
+                mine[v].A = fmaf(-mine[v].A, q[i][v], mine[v].A);
             }
         }
-        if (closed)
+    });
+    if (seg.closed())
 #pragma unroll
-            for (int v = 0; v < V; ++v) mine[v].A = CLOSED;
-    }
+        for (int v = 0; v < V; ++v) mine[v].A = CLOSED;
 #pragma unroll
     for (int v = 0; v < V; ++v) pieces[w.wave][w.lane][v] = mine[v];
     __syncthreads();
@@ -317,39 +367,25 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     if (a.carry && w.t0 % SPAN == 0 && w.t0 < a.rows)
 #pragma unroll
         for (int v = 0; v < V; ++v) a.carry[(int64_t)(w.t0 / SPAN) * a.width + w.ch + v] = h[v];
-    if (plain) {
+    sequence = seg.sequence;
+    by_rows(special, [&](auto special) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] += q[i][v] * (wt::one(x[i], v) - h[v]);
-            w.store(a.hidden, w.t0 + i, h);
-        }
-        if (seg.last(S - 1) && a.final_state)
-#pragma unroll
-            for (int v = 0; v < V; ++v) a.final_state[(int64_t)seg.sequence * a.width + w.ch + v] = h[v];
-        return;
-    }
-    int sequence = seg.sequence;
-#pragma unroll
-    for (int i = 0; i < S; ++i) {
-        if (w.t0 + i >= a.rows) break;
-        if (seg.outside(i)) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = 0.0f;
-        } else {
-            if (seg.start(i)) {
-                if (i > 0 || sequence < 0) to_next(a, w.t0 + i, sequence);
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = initial(sequence, v);
+            if (special >> i & 1) {
+                if (w.t0 + i >= a.rows) break;
+                w.enter(a, seg, i, sequence, h);
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] += q[i][v] * (wt::one(x[i], v) - h[v]);
-            if (seg.last(i) && a.final_state)
+            for (int v = 0; v < V; ++v) h[v] = fmaf(q[i][v], wt::one(x[i], v) - h[v], h[v]);
+            if ((special >> i & 1) && a.final_state && seg.last(i))
 #pragma unroll
                 for (int v = 0; v < V; ++v) a.final_state[(int64_t)sequence * a.width + w.ch + v] = h[v];
+            if ((special >> i & 1) && seg.outside(i))
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = 0.0f;
+            w.store(a.hidden, w.t0 + i, h);
         }
-        w.store(a.hidden, w.t0 + i, h);
-    }
+    });
 }
 
 template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_grad_kernel(recurrence_args<T> a)
@@ -367,6 +403,7 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     w.reverse(a);
     w.begin();
     typename wt::pack x[S], f[S], d[S];
+    const int some = some_offset(a);
     w.load(a.forget, a.rows - 1, f);
     w.load(a.value, a.rows - 1, x);
     w.load(a.d_hidden, a.rows - 1, d);
@@ -374,83 +411,53 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         h[v] = a.carry[(int64_t)w.span * a.width + w.ch + v];
-        b[v] = at(a.bias, w.ch + v);
+        b[v] = at(a.bias, w.ch + v) * LOG2E;
     }
-    const segment<S> seg = segment_at<S>(a, w.t0);
-    const bool plain = seg.plain(), open = plain && !seg.last(S - 1);            // open: no sequence begins, or ends, in the segment
-    const auto initial = [&](int sequence, int v) { return at(a.initial, (int64_t)sequence * a.width + w.ch + v); };
-    const auto final = [&](int sequence, int v) { return at(a.d_final, (int64_t)sequence * a.width + w.ch + v); };
-    piece mine[V], mine_back[V];
-    int last_sequence = seg.sequence;                                            // of the segment's last row
+    const segment<S> seg = segment_at<S>(a, w.t0, some);
+    const uint64_t special = seg.special();
+    w.clear_outside(seg, f, x);
+    w.clear_outside(seg, f, d);
+    piece mine[V];
+    float reach[V];                          // A and H, of the way back
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        mine[v] = mine_back[v] = {1.0f, 0.0f};
+        mine[v] = {1.0f, 0.0f};
+        reach[v] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v) + b[v]);
+        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v), b[v]);
     }
-    if (open) {
-#pragma unroll
-        for (int i = 0; i < S; ++i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                mine[v].H += q[i][v] * (wt::one(x[i], v) - mine[v].H);
-                mine[v].A -= mine[v].A * q[i][v];
-                const float g = wt::one(d[S - 1 - i], v) + mine_back[v].H;
-                mine_back[v].H = g - q[S - 1 - i][v] * g;
-            }
-#pragma unroll
-        for (int v = 0; v < V; ++v) mine_back[v].A = mine[v].A;
-    } else {
-        bool closed = false;
+    int sequence = seg.sequence;
+    by_rows(special, [&](auto special) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            if (seg.outside(i)) {
-                closed = true;
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine[v].H = 0.0f;
-                continue;
-            }
-            if (seg.start(i)) {
-                closed = true;
-                if (i > 0 || last_sequence < 0) to_next(a, w.t0 + i, last_sequence);
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine[v].H = initial(last_sequence, v);
-            }
+            if (special >> i & 1) w.enter(a, seg, i, sequence, mine);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                mine[v].H += q[i][v] * (wt::one(x[i], v) - mine[v].H);
-                mine[v].A -= mine[v].A * q[i][v];
+                mine[v].H = fmaf(q[i][v], wt::one(x[i], v) - mine[v].H, mine[v].H);
+                mine[v].A = fmaf(-mine[v].A, q[i][v], mine[v].A);
             }
         }
-        if (closed)
-#pragma unroll
-            for (int v = 0; v < V; ++v) mine[v].A = CLOSED;
-        closed = false;
-        int sequence = last_sequence;
+    });
+    const int last_sequence = sequence;      // of the segment's last row
+    by_rows(special, [&](auto special) {
 #pragma unroll
         for (int i = S - 1; i >= 0; --i) {
-            if (seg.outside(i)) {
-                closed = true;
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine_back[v].H = 0.0f;
-                continue;
-            }
-            if (seg.last(i)) {
-                closed = true;
-#pragma unroll
-                for (int v = 0; v < V; ++v) mine_back[v].H = final(sequence, v);
-            }
+            if (special >> i & 1) w.enter_back(a, seg, i, sequence, reach);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float g = wt::one(d[i], v) + mine_back[v].H;
-                mine_back[v].H = g - q[i][v] * g;
-                mine_back[v].A -= mine_back[v].A * q[i][v];
+                const float g = wt::one(d[i], v) + reach[v];
+                reach[v] = fmaf(-q[i][v], g, g);
             }
-            if (seg.start(i)) to_previous(a, w.t0 + i, sequence);
+            if ((special >> i & 1) && seg.start(i)) to_previous(a, w.t0 + i, sequence);
         }
-        if (closed)
+    });
+    w.keep_packed(x);
+    w.keep_packed(d);
+    piece mine_back[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) mine_back[v].A = CLOSED;
+    for (int v = 0; v < V; ++v) {
+        mine_back[v] = {seg.closed_back() ? CLOSED : mine[v].A, reach[v]};
+        if (seg.closed()) mine[v].A = CLOSED;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -488,22 +495,18 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     for (int k = 0; k < w.wave; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = through(pieces[k][w.lane][v], h[v]);
-    {
-        int sequence = seg.sequence;
+    sequence = seg.sequence;
+    by_rows(special, [&](auto special) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            if (!plain && !seg.outside(i) && seg.start(i)) {
-                if (i > 0 || sequence < 0) to_next(a, w.t0 + i, sequence);
-#pragma unroll
-                for (int v = 0; v < V; ++v) h[v] = initial(sequence, v);
-            }
+            if (special >> i & 1) w.enter(a, seg, i, sequence, h);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 hx[i][v] = h[v] - wt::one(x[i], v);
-                h[v] -= q[i][v] * hx[i][v];
+                h[v] = fmaf(-q[i][v], hx[i][v], h[v]);
             }
         }
-    }
+    });
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -514,40 +517,39 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
         for (int v = 0; v < V; ++v) c[v] = through(back[k][w.lane][v], c[v]);
     const bool write_x = w.here && a.d_value.data, write_f = w.here && a.d_forget.data;
-    int sequence = last_sequence;
+    sequence = last_sequence;
+    by_rows(special, [&](auto special) {
 #pragma unroll
-    for (int i = S - 1; i >= 0; --i) {
-        float dx[V], df[V];
-        if (!open) {
-            if (w.t0 + i >= a.rows) continue;
-            if (seg.outside(i)) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) c[v] = dx[v] = 0.0f;
-                if (write_x) w.store(a.d_value, w.t0 + i, dx);
-                if (write_f) w.store(a.d_forget, w.t0 + i, dx);
-                continue;
+        for (int i = S - 1; i >= 0; --i) {
+            float dx[V], df[V];
+            if (special >> i & 1) {
+                if (w.t0 + i >= a.rows) continue;
+                w.enter_back(a, seg, i, sequence, c);
             }
-            if (seg.last(i))
 #pragma unroll
-                for (int v = 0; v < V; ++v) c[v] = final(sequence, v);
-        }
+            for (int v = 0; v < V; ++v) {
+                const float g = wt::one(d[i], v) + c[v];
+                dx[v] = q[i][v] * g;
+                c[v] = g - dx[v];
+                df[v] = hx[i][v] * fmaf(-q[i][v], dx[v], dx[v]);
+            }
+            if (special >> i & 1) {
+                if (seg.outside(i))
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float g = wt::one(d[i], v) + c[v];
-            dx[v] = q[i][v] * g;
-            c[v] = g - dx[v];
-            df[v] = hx[i][v] * (dx[v] - q[i][v] * dx[v]);
-            sum[v] += df[v];
-        }
-        if (write_x) w.store(a.d_value, w.t0 + i, dx);
-        if (write_f) w.store(a.d_forget, w.t0 + i, df);
-        if (!open && seg.start(i)) {
-            if (a.d_initial && w.here)
+                    for (int v = 0; v < V; ++v) dx[v] = df[v] = 0.0f;
+                if (seg.start(i)) {
+                    if (a.d_initial && w.here)
 #pragma unroll
-                for (int v = 0; v < V; ++v) a.d_initial[(int64_t)sequence * a.width + w.ch + v] = c[v];
-            to_previous(a, w.t0 + i, sequence);
+                        for (int v = 0; v < V; ++v) a.d_initial[(int64_t)sequence * a.width + w.ch + v] = c[v];
+                    to_previous(a, w.t0 + i, sequence);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += df[v];
+            if (write_x) w.store(a.d_value, w.t0 + i, dx);
+            if (write_f) w.store(a.d_forget, w.t0 + i, df);
         }
-    }
+    });
     if (!a.bias_sums) return;
 #pragma unroll
     for (int v = 0; v < V; ++v) sums[w.wave][w.lane][v] = sum[v];
@@ -588,9 +590,9 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int width, bage
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * width; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / width;
         const int ch = (int)(i - r * width);
-        const float q = share((float)forget.row(r)[ch] + at(bias, ch));
+        const float q = share((float)forget.row(r)[ch], at(bias, ch) * LOG2E);
         float h = state[i];
-        h += q * ((float)value.row(r)[ch] - h);
+        h = fmaf(q, (float)value.row(r)[ch] - h, h);
         state[i] = h;
         if (hidden.data) hidden.row(r)[ch] = (T)h;
     }
@@ -625,6 +627,7 @@ template <typename T> recurrence_args<T> args_of(const bagel_gated_recurrence &r
 
 template <typename T, int V, int S, bool GRAD> void launch_spans(recurrence_args<T> &a, const bagel_gated_recurrence &r, hipStream_t stream)
 {
+    static_assert(S * WAVES % SPAN == 0, "the work space has room for a word a channel and SPAN rows");
     a.spans = (int)((r.rows + S * WAVES - 1) / (S * WAVES));
     a.groups = (r.width + 64 * V - 1) / (64 * V);
     const bool empty = r.sequences > 0 && (r.offsets || r.rows == 0) && (GRAD ? r.d_initial : r.final_state);
@@ -654,7 +657,7 @@ template <typename T, bool GRAD> hipError_t launch_pass(const bagel_gated_recurr
     const bagel_matrix all[] = {r.value, r.forget, r.hidden, r.d_hidden, r.d_value, r.d_forget};
     for (int i = 0; i < 6; ++i)
         if (GRAD ? i != 2 : i < 3) pack = bagel_matrix_pack(all[i], r.rows, r.dtype, pack);
-    if (pack == 2) launch_spans<T, 2, S, GRAD>(a, r, stream);
+    if (pack == 2 && sizeof(T) == 2) launch_spans<T, 2, S, GRAD>(a, r, stream);
     else launch_spans<T, 1, S, GRAD>(a, r, stream);
     if (GRAD && r.d_bias) bias_kernel<<<(r.width + 63) / 64, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
     return hipGetLastError();
