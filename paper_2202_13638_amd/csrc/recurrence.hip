@@ -64,49 +64,50 @@ __global__ __launch_bounds__(256) void nothing_kernel(uint64_t *published, int64
     for (int64_t i = first; i < cells; i += (int64_t)gridDim.x * 256) published[i] = NOTHING;
 }
 
-// The state before a span, for one wave's channels: through the published pieces from the nearest (`span`, which goes on by `step`) to the first
-// that is closed.  The span that all others come after publishes its state, so that there is one.
-template <int V> __device__ __forceinline__ void look_back(const uint64_t *published, int width, int ch, int span, int step, int spans, float (&h)[V])
+// The state before span number `order` (in the order in which they depend on each other; `spans` is where that of number 0 is, and the next `step`
+// cells on).  Spans are in blocks of BLOCK: the last of a block publishes the state behind it, CLOSED, and the others what they are
+// themselves.  So the state before a span is that before its block, taken through the spans of the block before it, in groups of GROUP for each
+// wave: always the same operations, whoever was fast, and one wait for another's state in BLOCK spans.
+constexpr int GROUP = 4, BLOCK = GROUP * WAVES;
+
+__device__ __forceinline__ bool publishes_state(int order) { return order % BLOCK == BLOCK - 1; }
+
+template <int V>
+__device__ __forceinline__ void look_back(const uint64_t *spans, int64_t step, int order, int wave, piece (*seen)[64][V], float (&h)[V])
 {
-    constexpr int WINDOW = 8 / V;            // spans that are looked at together
-    piece all[V];
-    bool found[V];
+    const int lane = threadIdx.x & 63, block = order / BLOCK * BLOCK, first = block + wave * GROUP, count = min(order - first, GROUP);
+    uint64_t word[GROUP + 1][V];
+#pragma unroll
+    for (int k = 0; k < GROUP; ++k)
+        if (k < count)
+#pragma unroll
+            for (int v = 0; v < V; ++v) word[k][v] = look(spans + (first + k) * step + v);
+    const bool state = wave == 0 && block > 0;
+    if (state)
+#pragma unroll
+        for (int v = 0; v < V; ++v) word[GROUP][v] = look(spans + (block - 1) * step + v);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        all[v] = {1.0f, 0.0f};
-        found[v] = false;
-    }
-    for (;; span += WINDOW * step) {
-        uint64_t word[WINDOW][V];
-#pragma unroll
-        for (int k = 0; k < WINDOW; ++k) {
-            const int at = min(max(span + k * step, 0), spans - 1);
-#pragma unroll
-            for (int v = 0; v < V; ++v) word[k][v] = look(published + (int64_t)at * width + ch + v);
+        piece p = {1.0f, 0.0f};
+        if (state) {
+            while ((float)__uint_as_float((uint32_t)word[GROUP][v]) != CLOSED) word[GROUP][v] = look(spans + (block - 1) * step + v);
+            p.H = __uint_as_float((uint32_t)(word[GROUP][v] >> 32));
         }
 #pragma unroll
-        for (int k = 0; k < WINDOW; ++k) {
-            const int at = min(max(span + k * step, 0), spans - 1);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                while (!found[v] && (uint32_t)word[k][v] == NOTHING) {
-                    __builtin_amdgcn_s_sleep(1);
-                    word[k][v] = look(published + (int64_t)at * width + ch + v);
-                }
-                if (!found[v]) {
-                    const piece p = {__uint_as_float((uint32_t)word[k][v]), __uint_as_float((uint32_t)(word[k][v] >> 32))};
-                    found[v] = p.A == CLOSED;
-                    all[v] = {all[v].A * p.A, fmaf(all[v].A, p.H, all[v].H)};       // (where it is closed, A is of no more use)
-                }
+        for (int k = 0; k < GROUP; ++k)
+            if (k < count) {
+                while ((uint32_t)word[k][v] == NOTHING) word[k][v] = look(spans + (first + k) * step + v);
+                p = joined(p, {__uint_as_float((uint32_t)word[k][v]), __uint_as_float((uint32_t)(word[k][v] >> 32))});
             }
-        }
-        bool every = true;
-#pragma unroll
-        for (int v = 0; v < V; ++v) every = every && found[v];
-        if (__all(every)) break;
+        seen[wave][lane][v] = p;
     }
+    __syncthreads();
+    const int waves = min((order - block + GROUP - 1) / GROUP, WAVES);
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = all[v].H;
+    for (int v = 0; v < V; ++v) h[v] = seen[0][lane][v].H;       // the state before the block is in it
+    for (int k = 1; k < waves; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = through(seen[k][lane][v], h[v]);
 }
 
 // The rows t0 to t0 + S - 1 of a wave: which of them begin a sequence (bit i of `starts` for t0 + i, bit S for the row behind them; the end of the
@@ -192,8 +193,12 @@ template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, 
 // What is the same in both directions: which span and channels a workgroup has, and its reads.
 template <typename T, int V, int S> struct wave_tile {
     using pack = bagel_pack<T, V>;
+    struct __attribute__((packed, aligned(sizeof(T)))) loose {               // rows of an odd width or stride: packs need not be aligned
+        pack x;
+    };
     static constexpr int rows = S * WAVES;
-    int span, wave, lane, t0, ch;            // ch: a channel to read from, also where this lane has none
+    int span, wave, lane, t0, ch;            // ch: its first channel.  A lane that has none, or only one of two, takes the last ones: it does once
+                                             // more what another lane does.
     bool here;
     __device__ __forceinline__ wave_tile(int work, const recurrence_args<T> &a)
     {
@@ -209,7 +214,7 @@ template <typename T, int V, int S> struct wave_tile {
     template <typename Q> __device__ __forceinline__ void load(const bagel_rows<Q> &m, int last, pack (&x)[S]) const
     {
 #pragma unroll
-        for (int i = 0; i < S; ++i) x[i] = *reinterpret_cast<const pack *>(m.row(min(t0 + i, last)) + ch);
+        for (int i = 0; i < S; ++i) x[i] = reinterpret_cast<const loose *>(m.row(min(t0 + i, last)) + ch)->x;
     }
     // From here on the packs are what they are and not what they were converted to: the converted ones of two channels in 16 bits would take twice
     // the registers between two passes over the rows.
@@ -264,7 +269,13 @@ template <typename T, int V, int S> struct wave_tile {
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = seg.outside(i) ? 0.0f : at(a.d_final, (int64_t)sequence * a.width + ch + v);
     }
-    __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const { bagel_store<T, V>(m.row(row) + ch, x); }
+    __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const
+    {
+        pack y;
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[v] = (T)x[v];
+        reinterpret_cast<loose *>(m.row(row) + ch)->x = y;
+    }
 };
 
 // The number of the work that this workgroup takes.
@@ -288,8 +299,7 @@ template <typename A> __device__ __forceinline__ void pass_through(const A &a, i
 
 template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(recurrence_args<T> a)
 {
-    __shared__ piece pieces[WAVES][64][V];
-    __shared__ float before[64][V];
+    __shared__ piece pieces[WAVES][64][V], seen[WAVES][64][V];
     const int work = next_work(a.counter);
     if (work >= a.spans * a.groups) {
         if (a.final_state) pass_through(a, work - a.spans * a.groups, a.initial, a.final_state);
@@ -332,34 +342,27 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
     for (int v = 0; v < V; ++v) pieces[w.wave][w.lane][v] = mine[v];
     __syncthreads();
-    if (w.wave == 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = 0.0f;
+    if (a.spans > 1) {
+        const bool writes = w.wave == 0 && w.here;
+        uint64_t *to = a.published + (int64_t)w.span * a.width + w.ch;
         piece all[V];
+        if (w.wave == 0)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            all[v] = pieces[0][w.lane][v];
+            for (int v = 0; v < V; ++v) {
+                all[v] = pieces[0][w.lane][v];
 #pragma unroll
-            for (int k = 1; k < WAVES; ++k) all[v] = joined(all[v], pieces[k][w.lane][v]);
-            h[v] = 0.0f;
-        }
-        if (a.spans > 1) {
-            uint64_t *to = a.published + (int64_t)w.span * a.width + w.ch;
-            if (w.span > 0) {
-                if (w.here)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) publish(to + v, all[v]);
-                look_back<V>(a.published, a.width, w.ch, w.span - 1, -1, a.spans, h);
+                for (int k = 1; k < WAVES; ++k) all[v] = joined(all[v], pieces[k][w.lane][v]);
             }
-            if (w.here)
+        if (writes && !publishes_state(w.span))
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (w.span == 0 || all[v].A != CLOSED) publish(to + v, {CLOSED, through(all[v], h[v])});
-        }
+            for (int v = 0; v < V; ++v) publish(to + v, all[v]);
+        if (w.span > 0) look_back<V>(a.published + w.ch, a.width, w.span, w.wave, seen, h);
+        if (writes && publishes_state(w.span))
 #pragma unroll
-        for (int v = 0; v < V; ++v) before[w.lane][v] = h[v];
+            for (int v = 0; v < V; ++v) publish(to + v, {CLOSED, through(all[v], h[v])});
     }
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = before[w.lane][v];
     for (int k = 0; k < w.wave; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = through(pieces[k][w.lane][v], h[v]);
@@ -391,8 +394,8 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_grad_kernel(recurrence_args<T> a)
 {
     static_assert(S * WAVES == SPAN, "a span begins with a row of the carry");
-    __shared__ piece pieces[WAVES][64][V], back[WAVES][64][V];
-    __shared__ float after[64][V], sums[WAVES][64][V];
+    __shared__ piece pieces[WAVES][64][V], back[WAVES][64][V], seen[WAVES][64][V];
+    __shared__ float sums[WAVES][64][V];
     const int work = next_work(a.counter);
     if (work >= a.spans * a.groups) {
         if (a.d_initial) pass_through(a, work - a.spans * a.groups, a.d_final, a.d_initial);
@@ -407,7 +410,7 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     w.load(a.forget, a.rows - 1, f);
     w.load(a.value, a.rows - 1, x);
     w.load(a.d_hidden, a.rows - 1, d);
-    float h[V], c[V], q[S][V], b[V];
+    float h[V], c[V], q[S][V], b[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         h[v] = a.carry[(int64_t)w.span * a.width + w.ch + v];
@@ -465,33 +468,30 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
         back[w.wave][w.lane][v] = mine_back[v];
     }
     __syncthreads();
-    if (w.wave == 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) c[v] = sum[v] = 0.0f;
+    if (a.spans > 1) {
+        const bool writes = w.wave == 0 && w.here;
+        const int order = a.spans - 1 - w.span;
+        uint64_t *to = a.published + (int64_t)order * a.width + w.ch;
         piece all[V];
+        if (w.wave == 0)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            all[v] = back[WAVES - 1][w.lane][v];
+            for (int v = 0; v < V; ++v) {
+                all[v] = back[WAVES - 1][w.lane][v];
 #pragma unroll
-            for (int k = WAVES - 2; k >= 0; --k) all[v] = joined(all[v], back[k][w.lane][v]);
-            c[v] = 0.0f;
-        }
-        if (a.spans > 1) {
-            uint64_t *to = a.published + (int64_t)w.span * a.width + w.ch;
-            if (w.span < a.spans - 1) {
-                if (w.here)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) publish(to + v, all[v]);
-                look_back<V>(a.published, a.width, w.ch, w.span + 1, 1, a.spans, c);
+                for (int k = WAVES - 2; k >= 0; --k) all[v] = joined(all[v], back[k][w.lane][v]);
             }
-            if (w.here)
+        if (writes && !publishes_state(order))
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    if (w.span == a.spans - 1 || all[v].A != CLOSED) publish(to + v, {CLOSED, through(all[v], c[v])});
-        }
+            for (int v = 0; v < V; ++v) publish(to + v, all[v]);
+        if (order > 0) look_back<V>(a.published + w.ch, a.width, order, w.wave, seen, c);
+        if (writes && publishes_state(order))
 #pragma unroll
-        for (int v = 0; v < V; ++v) after[w.lane][v] = c[v];
+            for (int v = 0; v < V; ++v) publish(to + v, {CLOSED, through(all[v], c[v])});
     }
     // h before every row, less its value
-    float hx[S][V], sum[V];
+    float hx[S][V];
     for (int k = 0; k < w.wave; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = through(pieces[k][w.lane][v], h[v]);
@@ -507,12 +507,6 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
             }
         }
     });
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        c[v] = after[w.lane][v];
-        sum[v] = 0.0f;
-    }
     for (int k = WAVES - 1; k > w.wave; --k)
 #pragma unroll
         for (int v = 0; v < V; ++v) c[v] = through(back[k][w.lane][v], c[v]);
@@ -648,17 +642,13 @@ template <typename T, int V, int S, bool GRAD> void launch_spans(recurrence_args
     }
 }
 
-// Two channels a lane where every row of every matrix begins at a multiple of two entries.
+// Two channels a lane in 16 bits, one in 32: a wave reads 256 bytes of a row either way.  (One in 16 bits took 252 and 403 us for 131072 x 1024 where
+// two took 220 and 306, two in 32 bits 335 and 682 where one took 311 and 511.)
 template <typename T, bool GRAD> hipError_t launch_pass(const bagel_gated_recurrence &r, hipStream_t stream)
 {
     recurrence_args<T> a = args_of<T>(r, GRAD);
-    constexpr int S = GRAD ? 16 : 16;
-    int pack = r.width % 2 ? 1 : 2;
-    const bagel_matrix all[] = {r.value, r.forget, r.hidden, r.d_hidden, r.d_value, r.d_forget};
-    for (int i = 0; i < 6; ++i)
-        if (GRAD ? i != 2 : i < 3) pack = bagel_matrix_pack(all[i], r.rows, r.dtype, pack);
-    if (pack == 2 && sizeof(T) == 2) launch_spans<T, 2, S, GRAD>(a, r, stream);
-    else launch_spans<T, 1, S, GRAD>(a, r, stream);
+    if (sizeof(T) == 2 && r.width > 1) launch_spans<T, 4 / sizeof(T), 16, GRAD>(a, r, stream);
+    else launch_spans<T, 1, 16, GRAD>(a, r, stream);
     if (GRAD && r.d_bias) bias_kernel<<<(r.width + 63) / 64, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
     return hipGetLastError();
 }
