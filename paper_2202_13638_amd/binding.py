@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -95,6 +96,9 @@ class _Recurrence(C.Structure):
 class _AdamWTensor(C.Structure):
     _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64), ("weight_decay", C.c_double)]
+
+
+_ADAMW_TENSOR = "7Pqd"           # the same for struct.pack
 
 
 class _AdamW(C.Structure):
@@ -211,75 +215,87 @@ def bagel_sample_eval_static(dims: Dims, X, lengthscale, signal_var, omega, phas
 
 # ---------------------------------------------------------------------------- operators of a policy with memory
 # Outputs are tensors of the caller; what is None is left out.  `stream` None: torch's current one.  All tensors are on the current device.
+# (A call of a few rows takes about as long on the host as on the GPU: arguments are looked at once, in the order of the structure.)
 JOIN_MAX_WIDTH, RECURRENCE_SPAN, ADAMW_BLOCK = 16384, 128, 256
 _ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
-_DTYPES = None
+_torch = _DTYPES = None
+
+
+def _load():
+    """The library, with torch and its types looked up once."""
+    global _torch, _DTYPES
+    if _DTYPES is None:
+        import torch as _torch
+        _DTYPES = {_torch.float32: 0, _torch.bfloat16: 1, _torch.float16: 2}
+    return _lib or load()
 
 
 def _dtype_code(t, name):
-    global _DTYPES
-    import torch
-    if _DTYPES is None:
-        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    code = _DTYPES.get(t.dtype) if isinstance(t, _torch.Tensor) else None
     if code is None:
         raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor")
     return code
 
 
-def _matrix(args, name, t, like):
-    """A matrix argument: shape, type and device of `like`, the entries of a row next to each other, any row stride."""
-    if t is None:
-        return
-    import torch
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name} must be a tensor")
-    if t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape != like.shape:
-        raise ValueError(f"{name} must be a {like.dtype} tensor of shape {tuple(like.shape)} on {like.device}, "
-                         f"not {t.dtype} of {tuple(t.shape)} on {t.device}")
-    rows, width = like.shape
-    stride, step = t.stride()
-    if step != 1 and width > 1 and rows > 0:
-        raise ValueError(f"{name}: the entries of a row must be next to each other")
-    setattr(args, name, t.data_ptr())
-    setattr(args, name + "_stride", stride if rows > 1 else width)
+def _stream(stream):
+    if stream is None:
+        return _torch.cuda.current_stream()
+    if stream.device_index != _torch.cuda.current_device():
+        raise ValueError("the stream must be one of the current GPU")
+    return stream
 
 
-def _vector(args, name, t, shape, device):
-    if t is not None:
-        setattr(args, name, _ptr(t, shape, name))
-        if t.get_device() != device:
-            raise ValueError(f"{name} must be on cuda:{device}")
-
-
-def _first_matrix(t, name):
-    """(rows, width, type, device) of the matrix that the others of a call are held to."""
-    import torch
+def _first_matrix(t, name, stream):
+    """(shape, type, its code, device) of the matrix that the others of a call are held to, and the call's stream."""
     code = _dtype_code(t, name)
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    stream = _stream(stream)
+    if t.get_device() != stream.device_index:
         raise ValueError(f"{name} must be on the current GPU")
-    if t.dim() != 2:
-        raise ValueError(f"{name} must have two dimensions, rows and width, not {t.dim()}")
-    return t.shape[0], t.shape[1], code, t.get_device()
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must have two dimensions, rows and width, not {len(shape)}")
+    return shape, t.dtype, code, t.get_device(), stream
 
 
-def _workspace(args, workspace, need, device, stream):
-    """The caller's work space, or one from torch's allocator on the call's stream."""
-    import torch
+def _matrix(t, name, shape, dtype, device):
+    """(pointer, row stride) of a matrix: any row stride, the entries of a row next to each other."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, _torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{device}, not {t.dtype} of {tuple(t.shape)} on {t.device}")
+    stride, step = t.stride()
+    if step != 1 and shape[1] > 1 and shape[0] > 0:
+        raise ValueError(f"{name}: the entries of a row must be next to each other")
+    return t.data_ptr(), stride if shape[0] > 1 else shape[1]
+
+
+def _vector(t, name, shape, device):
+    """Pointer of a contiguous float32 tensor."""
+    if t is None:
+        return None
+    p = _ptr(t, shape, name)
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}")
+    return p
+
+
+def _workspace(workspace, need, device, stream):
+    """The caller's work space, or one from torch's allocator on the call's stream (`stream` as the caller gave it)."""
     if workspace is None:
-        with torch.cuda.stream(stream):
-            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
-    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
+        if stream is None:
+            return _torch.empty(max(need, 16), dtype=_torch.uint8, device=device)
+        with _torch.cuda.stream(stream):
+            return _torch.empty(max(need, 16), dtype=_torch.uint8, device=device)
+    if not isinstance(workspace, _torch.Tensor) or workspace.dtype != _torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{device}")
-    args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
     return workspace
 
 
-def _run(lib, call, args, stream):
-    if stream is None:
-        import torch
-        stream = torch.cuda.current_stream()
-    rc = call(args, stream.cuda_stream)
+def _done(lib, rc):
     if rc != OK:
         raise BagelError(rc, lib.bagel_last_error(None).decode())
 
@@ -289,49 +305,45 @@ def bagel_block_join_workspace(rows: int, width: int) -> int:
     return int(load().bagel_block_join_workspace(rows, width))
 
 
-def _join_args(first, name, gate, act, eps, post_weight, scale, pre_weight):
+def _act(act):
     if act not in _ACTS:
         raise ValueError(f"act must be one of {sorted(_ACTS)}")
-    args = _Join()
-    args.rows, args.width, args.dtype, device = _first_matrix(first, name)
-    args.act, args.eps = _ACTS[act], eps
-    _matrix(args, "gate", gate, first)
-    shape = (args.width,)
-    _vector(args, "post_weight", post_weight, shape, device)
-    _vector(args, "scale", scale, shape, device)
-    _vector(args, "pre_weight", pre_weight, shape, device)
-    return args, device
+    return _ACTS[act]
 
 
 def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None, eps=1e-6,
                      stream=None):
     """out = resid + scale * act(gate) * (R(branch) * post_weight), normed = R(out) * pre_weight (see include/bagel.h)."""
-    lib = load()
-    first, name = (resid, "resid") if resid is not None else (branch, "branch")
-    args, _ = _join_args(first, name, gate, act, eps, post_weight, scale, pre_weight)
-    for key, t in (("branch", branch), ("resid", resid), ("out", out), ("normed", normed)):
-        _matrix(args, key, t, first)
-    _run(lib, lib.bagel_block_join, args, stream)
+    lib = _load()
+    kind = _act(act)
+    shape, dtype, code, device, on = _first_matrix(*((resid, "resid") if resid is not None else (branch, "branch")), stream)
+    vector = shape[1:]
+    args = _Join(shape[0], shape[1], code, kind, eps, *_matrix(branch, "branch", shape, dtype, device), *_matrix(gate, "gate", shape, dtype, device),
+                 *_matrix(resid, "resid", shape, dtype, device), *_matrix(out, "out", shape, dtype, device),
+                 *_matrix(normed, "normed", shape, dtype, device), _vector(post_weight, "post_weight", vector, device),
+                 _vector(scale, "scale", vector, device), _vector(pre_weight, "pre_weight", vector, device))
+    _done(lib, lib.bagel_block_join(args, on.cuda_stream))
 
 
 def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None,
                           eps=1e-6, d_branch=None, d_gate=None, d_resid=None, d_post_weight=None, d_scale=None, d_pre_weight=None,
                           workspace=None, stream=None):
     """The gradient of bagel_block_join at the `out` it stored (see include/bagel.h)."""
-    lib = load()
-    args, device = _join_args(out, "out", gate, act, eps, post_weight, scale, pre_weight)
-    for key, t in (("branch", branch), ("out", out), ("d_out", d_out), ("d_normed", d_normed), ("d_branch", d_branch), ("d_gate", d_gate),
-                   ("d_resid", d_resid)):
-        _matrix(args, key, t, out)
-    shape = (args.width,)
-    _vector(args, "d_post_weight", d_post_weight, shape, device)
-    _vector(args, "d_scale", d_scale, shape, device)
-    _vector(args, "d_pre_weight", d_pre_weight, shape, device)
-    keep = None
+    lib = _load()
+    kind = _act(act)
+    shape, dtype, code, device, on = _first_matrix(out, "out", stream)
+    vector = shape[1:]
+    args = _Join(shape[0], shape[1], code, kind, eps, *_matrix(branch, "branch", shape, dtype, device), *_matrix(gate, "gate", shape, dtype, device),
+                 None, 0, *_matrix(out, "out", shape, dtype, device), None, 0, _vector(post_weight, "post_weight", vector, device),
+                 _vector(scale, "scale", vector, device), _vector(pre_weight, "pre_weight", vector, device),
+                 *_matrix(d_out, "d_out", shape, dtype, device), *_matrix(d_normed, "d_normed", shape, dtype, device),
+                 *_matrix(d_branch, "d_branch", shape, dtype, device), *_matrix(d_gate, "d_gate", shape, dtype, device),
+                 *_matrix(d_resid, "d_resid", shape, dtype, device), _vector(d_post_weight, "d_post_weight", vector, device),
+                 _vector(d_scale, "d_scale", vector, device), _vector(d_pre_weight, "d_pre_weight", vector, device))
     if d_post_weight is not None or d_scale is not None or d_pre_weight is not None:
-        keep = _workspace(args, workspace, lib.bagel_block_join_workspace(args.rows, args.width), device, stream)
-    _run(lib, lib.bagel_block_join_grad, args, stream)
-    del keep
+        workspace = _workspace(workspace, lib.bagel_block_join_workspace(shape[0], shape[1]), device, stream)
+        args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _done(lib, lib.bagel_block_join_grad(args, on.cuda_stream))
 
 
 def bagel_recurrence_carry_rows(rows: int) -> int:
@@ -344,70 +356,66 @@ def bagel_recurrence_workspace(rows: int, width: int) -> int:
     return int(load().bagel_recurrence_workspace(rows, width))
 
 
-def _recurrence_args(value, forget, offsets, bias):
-    """`offsets`: an int32 tensor on the GPU, or the number of sequences of equal length."""
-    import torch
-    args = _Recurrence()
-    args.rows, args.width, args.dtype, device = _first_matrix(value, "value")
-    if isinstance(offsets, torch.Tensor):
-        if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
-            raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
-        args.sequences, args.offsets = offsets.numel() - 1, offsets.data_ptr()
-    else:
-        args.sequences = int(offsets)
-    _matrix(args, "value", value, value)
-    if forget is None:
-        raise ValueError("forget is required")
-    _matrix(args, "forget", forget, value)
-    _vector(args, "bias", bias, (args.width,), device)
-    return args, device
+def _sequences(offsets, device):
+    """(number of sequences, pointer of their offsets): an int32 tensor on the GPU, or the number of sequences of equal length."""
+    if not isinstance(offsets, _torch.Tensor):
+        return int(offsets), None
+    if offsets.dtype != _torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
+        raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
+    return offsets.numel() - 1, offsets.data_ptr()
+
+
+def _needed(t, name):
+    if t is None:
+        raise ValueError(f"{name} is required")
+    return t
 
 
 def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None, final=None, carry=None, workspace=None, stream=None):
     """h_t = h_{t-1} + q_t (value_t - h_{t-1}), q_t = 1 / (1 + exp(forget_t + bias)), along packed sequences (see include/bagel.h)."""
-    lib = load()
-    args, device = _recurrence_args(value, forget, offsets, bias)
-    _matrix(args, "hidden", hidden, value)
-    shape = (args.sequences, args.width)
-    _vector(args, "initial", initial, shape, device)
-    _vector(args, "final", final, shape, device)
-    _vector(args, "carry", carry, (lib.bagel_recurrence_carry_rows(args.rows), args.width), device)
-    keep = _workspace(args, workspace, lib.bagel_recurrence_workspace(args.rows, args.width), device, stream)
-    _run(lib, lib.bagel_recurrence, args, stream)
-    del keep
+    lib = _load()
+    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
+    rows, width = shape
+    n, at = _sequences(offsets, device)
+    state = (n, width)
+    workspace = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
+    args = _Recurrence(rows, width, code, n, at, *_matrix(value, "value", shape, dtype, device),
+                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device),
+                       *_matrix(_needed(hidden, "hidden"), "hidden", shape, dtype, device), _vector(bias, "bias", shape[1:], device),
+                       _vector(initial, "initial", state, device), _vector(final, "final", state, device),
+                       _vector(carry, "carry", (lib.bagel_recurrence_carry_rows(rows), width), device) if carry is not None else None, None,
+                       None, 0, None, 0, None, 0, None, None, None, workspace.data_ptr(), workspace.numel())
+    _done(lib, lib.bagel_recurrence(args, on.cuda_stream))
 
 
 def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, carry, *, bias=None, initial=None, d_final=None, d_initial=None,
                           d_bias=None, workspace=None, stream=None):
     """The gradient of bagel_recurrence, with the `carry` it wrote (see include/bagel.h)."""
-    lib = load()
-    args, device = _recurrence_args(value, forget, offsets, bias)
-    for key, t in (("d_hidden", d_hidden), ("d_value", d_value), ("d_forget", d_forget)):
-        _matrix(args, key, t, value)
-    shape = (args.sequences, args.width)
-    _vector(args, "initial", initial, shape, device)
-    _vector(args, "d_final", d_final, shape, device)
-    _vector(args, "d_initial", d_initial, shape, device)
-    _vector(args, "d_bias", d_bias, (args.width,), device)
-    _vector(args, "carry", carry, (lib.bagel_recurrence_carry_rows(args.rows), args.width), device)
-    keep = _workspace(args, workspace, lib.bagel_recurrence_workspace(args.rows, args.width), device, stream)
-    _run(lib, lib.bagel_recurrence_grad, args, stream)
-    del keep
+    lib = _load()
+    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
+    rows, width = shape
+    n, at = _sequences(offsets, device)
+    state = (n, width)
+    workspace = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
+    args = _Recurrence(rows, width, code, n, at, *_matrix(value, "value", shape, dtype, device),
+                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device), None, 0, _vector(bias, "bias", shape[1:], device),
+                       _vector(initial, "initial", state, device), None,
+                       _vector(_needed(carry, "carry"), "carry", (lib.bagel_recurrence_carry_rows(rows), width), device), None,
+                       *_matrix(_needed(d_hidden, "d_hidden"), "d_hidden", shape, dtype, device), *_matrix(d_value, "d_value", shape, dtype, device),
+                       *_matrix(d_forget, "d_forget", shape, dtype, device), _vector(d_final, "d_final", state, device),
+                       _vector(d_initial, "d_initial", state, device), _vector(d_bias, "d_bias", shape[1:], device),
+                       workspace.data_ptr(), workspace.numel())
+    _done(lib, lib.bagel_recurrence_grad(args, on.cuda_stream))
 
 
 def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, stream=None):
     """One step of as many sequences as there are rows, the float32 state updated in place (see include/bagel.h)."""
-    lib = load()
-    if forget is None or state is None:
-        raise ValueError("forget and state are required")
-    args = _Recurrence()
-    rows, args.width, args.dtype, device = _first_matrix(value, "value")
-    args.sequences = rows
-    for key, t in (("value", value), ("forget", forget), ("hidden", hidden)):
-        _matrix(args, key, t, value)
-    _vector(args, "bias", bias, (args.width,), device)
-    _vector(args, "state", state, (rows, args.width), device)
-    _run(lib, lib.bagel_recurrence_step, args, stream)
+    lib = _load()
+    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
+    args = _Recurrence(0, shape[1], code, shape[0], None, *_matrix(value, "value", shape, dtype, device),
+                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device), *_matrix(hidden, "hidden", shape, dtype, device),
+                       _vector(bias, "bias", shape[1:], device), None, None, None, _vector(_needed(state, "state"), "state", shape, device))
+    _done(lib, lib.bagel_recurrence_step(args, on.cuda_stream))
 
 
 def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, copy=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
@@ -417,47 +425,46 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
     params: contiguous float32 tensors; grads, m, v, copy (None: none): lists of tensors of the same shapes.  grads are all of one
     type, and so are the entries of copy.  m and v are float32, or float8_e4m3fn with m_scale and v_scale, lists of float32 tensors
     with an entry for every ADAMW_BLOCK values.  weight_decay: a number, or one for every tensor."""
-    import torch
-    lib = load()
+    lib = _load()
     n = len(params)
-    eight = n > 0 and m[0].dtype == torch.float8_e4m3fn
-    state = torch.float8_e4m3fn if eight else torch.float32
+    eight = n > 0 and len(m) > 0 and m[0].dtype is _torch.float8_e4m3fn
     decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
     lists = [params, grads, m, v, decay] + ([copy] if copy is not None else []) + ([m_scale, v_scale] if eight else [])
     if any(x is None or len(x) != n for x in lists):
         raise ValueError("the lists of one update must have an entry for every tensor (moments in 8 bits need m_scale and v_scale)")
-    options = _AdamW()
-    options.step, options.lr, options.beta1, options.beta2, options.eps, options.seed = int(step), lr, beta1, beta2, eps, int(seed) & 0xFFFFFFFF
-    options.state_bits = 8 if eight else 32
-    if n:
-        device = torch.cuda.current_device()
-        options.grad_dtype = _dtype_code(grads[0], "grads")
-        types = [torch.float32, grads[0].dtype, state, state]
-        columns = [params, grads, m, v]
+    on = _stream(stream)
+    device = on.device_index
+    f32, grad_type = _torch.float32, grads[0].dtype if n else None
+    state = _torch.float8_e4m3fn if eight else f32
+    scale = None
+    if grad_scale is not None:
+        scale = _ptr(grad_scale, grad_scale.shape, "grad_scale")
+        if grad_scale.numel() != 1 or grad_scale.get_device() != device:
+            raise ValueError("grad_scale must hold one value and be on the current GPU")
+    options = _AdamW(int(step), lr, beta1, beta2, eps, scale, _dtype_code(grads[0], "grads") if n else 0,
+                     _dtype_code(copy[0], "copy") if n and copy is not None else 0, 8 if eight else 32, int(seed) & 0xFFFFFFFF)
+    table = []
+    for i in range(n):
+        p, g, mi, vi = params[i], grads[i], m[i], v[i]
+        shape = p.shape
+        if not (p.dtype is f32 and g.dtype is grad_type and mi.dtype is state and vi.dtype is state and g.shape == shape and mi.shape == shape and
+                vi.shape == shape and p.is_contiguous() and g.is_contiguous() and mi.is_contiguous() and vi.is_contiguous() and
+                p.get_device() == g.get_device() == mi.get_device() == vi.get_device() == device):
+            raise ValueError(f"tensor {i} of an update: contiguous tensors of shape {tuple(shape)} on cuda:{device} are needed, a float32 parameter, a "
+                             f"{grad_type} gradient and {state} moments, not " + ", ".join(f"{x.dtype} of {tuple(x.shape)} on {x.device}"
+                                                                                           for x in (p, g, mi, vi)))
+        count = p.numel()
+        ms = vs = ci = 0
+        if eight:
+            blocks = (-(-count // ADAMW_BLOCK),)
+            ms, vs = _vector(_needed(m_scale[i], "m_scale"), "m_scale", blocks, device), _vector(_needed(v_scale[i], "v_scale"), "v_scale", blocks, device)
         if copy is not None:
-            options.copy_dtype = _dtype_code(copy[0], "copy")
-            types.append(copy[0].dtype)
-            columns.append(copy)
-        if grad_scale is not None:
-            options.grad_scale = _ptr(grad_scale, tuple(grad_scale.shape), "grad_scale")
-            if grad_scale.numel() != 1 or grad_scale.get_device() != device:
-                raise ValueError("grad_scale must hold one value and be on the current GPU")
-        table = (_AdamWTensor * n)()
-        for i in range(n):
-            shape = params[i].shape
-            for x, t in zip(columns, types):
-                x = x[i]
-                if x.dtype != t or x.shape != shape or not x.is_contiguous() or x.get_device() != device:
-                    raise ValueError(f"tensor {i} of an update: a contiguous {t} tensor of shape {tuple(shape)} on cuda:{device} is needed, "
-                                     f"not {x.dtype} of {tuple(x.shape)} on {x.device}")
-            count = params[i].numel()
-            scales = (None, None)
-            if eight:
-                blocks = (-(-count // ADAMW_BLOCK),)
-                scales = (_ptr(m_scale[i], blocks, "m_scale"), _ptr(v_scale[i], blocks, "v_scale"))
-            table[i] = (params[i].data_ptr(), grads[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr(), *scales,
-                        copy[i].data_ptr() if copy is not None else None, count, decay[i])
-        _run(lib, lambda o, s: lib.bagel_adamw_step(table, n, o, s), options, stream)
+            c = copy[i]
+            if c.dtype is not copy[0].dtype or c.shape != shape or not c.is_contiguous() or c.get_device() != device:
+                raise ValueError(f"copy {i} of an update: a contiguous {copy[0].dtype} tensor of shape {tuple(shape)} on cuda:{device} is needed")
+            ci = c.data_ptr()
+        table += (p.data_ptr(), g.data_ptr(), mi.data_ptr(), vi.data_ptr(), ms, vs, ci, count, decay[i])
+    _done(lib, lib.bagel_adamw_step(struct.pack(_ADAMW_TENSOR * n, *table), n, options, on.cuda_stream))
 
 
 class Bagel:
