@@ -19,15 +19,6 @@ inline bool bagel_matrix_ok(const bagel_matrix &m, int64_t rows, int64_t width, 
     return !m.data || (((uintptr_t)m.data & (bagel_type_bytes(dtype) - 1)) == 0 && (rows <= 1 || (m.stride >= width && m.stride < (1ll << 40))));
 }
 
-// The largest power of two up to `most` such that packs of so many entries are aligned in every row of m.
-inline int bagel_matrix_pack(const bagel_matrix &m, int64_t rows, int dtype, int most)
-{
-    if (!m.data) return most;
-    const uint64_t places = (uint64_t)(uintptr_t)m.data / bagel_type_bytes(dtype) | (rows > 1 ? (uint64_t)m.stride : 0);
-    while (most > 1 && (places & (most - 1))) most /= 2;
-    return most;
-}
-
 // Launches f<type>() for the type that `dtype` says.
 template <typename T> struct bagel_type { using type = T; };
 template <typename F> hipError_t bagel_by_type(int dtype, F &&f)
@@ -47,27 +38,24 @@ template <typename T> inline bagel_rows<T> bagel_rows_of(const bagel_matrix &m) 
 // V entries of a row, one load or store of up to 16 bytes.
 template <typename T, int V> using bagel_pack = T __attribute__((ext_vector_type(V)));
 
+// one at any place of its type (the loads and stores of the hardware need no more)
+template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) bagel_loose_pack {
+    bagel_pack<T, V> x;
+};
+
 template <typename T, int V> __device__ __forceinline__ void bagel_load(const T *p, float (&v)[V])
 {
-    if constexpr (V == 1) {
-        v[0] = (float)*p;
-    } else {
-        const bagel_pack<T, V> x = *reinterpret_cast<const bagel_pack<T, V> *>(p);
+    const bagel_pack<T, V> x = reinterpret_cast<const bagel_loose_pack<T, V> *>(p)->x;
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)x[i];
-    }
+    for (int i = 0; i < V; ++i) v[i] = (float)x[i];
 }
 
 template <typename T, int V> __device__ __forceinline__ void bagel_store(T *p, const float (&v)[V])
 {
-    if constexpr (V == 1) {
-        *p = (T)v[0];
-    } else {
-        bagel_pack<T, V> x;
+    bagel_pack<T, V> x;
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = (T)v[i];
-        *reinterpret_cast<bagel_pack<T, V> *>(p) = x;
-    }
+    for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+    reinterpret_cast<bagel_loose_pack<T, V> *>(p)->x = x;
 }
 
 // Data-parallel moves within 16 lanes: 0xB1 swaps neighbours, 0x4E pairs, 0x141 mirrors 8 lanes, 0x140 all 16.

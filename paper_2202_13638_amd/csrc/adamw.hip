@@ -21,7 +21,6 @@ struct adamw_tensor {
     void *copy;
     int64_t count;
     float keep;                  // 1 - lr weight_decay
-    int pack;                    // whether four entries at a time are aligned in all of them
 };
 
 struct adamw_args {
@@ -35,47 +34,51 @@ struct adamw_args {
 };
 static_assert(sizeof(adamw_args) <= 4096, "kernel arguments");
 
-// Four entries of a block, in a row (PACK) or 64 apart; those from `rest` on are not there.
-template <bool PACK> __device__ __forceinline__ int place(int i) { return PACK ? 4 * (threadIdx.x & 63) + i : 64 * i + (threadIdx.x & 63); }
+// Four entries of a block, in a row (WHOLE: a block of 256, at any alignment) or 64 apart, where those from `rest` on are not there.
+template <bool WHOLE> __device__ __forceinline__ int place(int i) { return WHOLE ? 4 * (threadIdx.x & 63) + i : 64 * i + (threadIdx.x & 63); }
 
-template <bool PACK, typename T> __device__ __forceinline__ void load_four(const void *p, int64_t from, int64_t rest, float (&v)[4])
+template <bool WHOLE, typename T> __device__ __forceinline__ void load_four(const void *p, int64_t from, int64_t rest, float (&v)[4])
 {
     const T *q = (const T *)p + from;
-    if constexpr (PACK) bagel_load<T, 4>(q + place<true>(0), v);
+    if constexpr (WHOLE) bagel_load<T, 4>(q + place<true>(0), v);
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = place<false>(i) < rest ? (float)q[place<false>(i)] : 0.0f;
 }
 
-template <bool PACK, typename T> __device__ __forceinline__ void store_four(void *p, int64_t from, int64_t rest, const float (&v)[4])
+template <bool WHOLE, typename T> __device__ __forceinline__ void store_four(void *p, int64_t from, int64_t rest, const float (&v)[4])
 {
     T *q = (T *)p + from;
-    if constexpr (PACK) bagel_store<T, 4>(q + place<true>(0), v);
+    if constexpr (WHOLE) bagel_store<T, 4>(q + place<true>(0), v);
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (place<false>(i) < rest) q[place<false>(i)] = (T)v[i];
 }
 
-template <bool PACK> __device__ __forceinline__ void load_as(const void *p, int64_t from, int64_t rest, int dtype, float (&v)[4])
+template <bool WHOLE> __device__ __forceinline__ void load_as(const void *p, int64_t from, int64_t rest, int dtype, float (&v)[4])
 {
-    if (dtype == BAGEL_FLOAT32) load_four<PACK, float>(p, from, rest, v);
-    else if (dtype == BAGEL_BFLOAT16) load_four<PACK, __bf16>(p, from, rest, v);
-    else load_four<PACK, _Float16>(p, from, rest, v);
+    if (dtype == BAGEL_FLOAT32) load_four<WHOLE, float>(p, from, rest, v);
+    else if (dtype == BAGEL_BFLOAT16) load_four<WHOLE, __bf16>(p, from, rest, v);
+    else load_four<WHOLE, _Float16>(p, from, rest, v);
 }
 
-template <bool PACK> __device__ __forceinline__ void store_as(void *p, int64_t from, int64_t rest, int dtype, const float (&v)[4])
+template <bool WHOLE> __device__ __forceinline__ void store_as(void *p, int64_t from, int64_t rest, int dtype, const float (&v)[4])
 {
-    if (dtype == BAGEL_FLOAT32) store_four<PACK, float>(p, from, rest, v);
-    else if (dtype == BAGEL_BFLOAT16) store_four<PACK, __bf16>(p, from, rest, v);
-    else store_four<PACK, _Float16>(p, from, rest, v);
+    if (dtype == BAGEL_FLOAT32) store_four<WHOLE, float>(p, from, rest, v);
+    else if (dtype == BAGEL_BFLOAT16) store_four<WHOLE, __bf16>(p, from, rest, v);
+    else store_four<WHOLE, _Float16>(p, from, rest, v);
 }
 
-template <bool PACK> __device__ __forceinline__ void load_codes(const void *p, int64_t from, int64_t rest, float (&v)[4])
+struct __attribute__((packed, aligned(1))) loose_int {
+    int x;
+};
+
+template <bool WHOLE> __device__ __forceinline__ void load_codes(const void *p, int64_t from, int64_t rest, float (&v)[4])
 {
     const uint8_t *q = (const uint8_t *)p + from;
     int bytes = 0;
-    if constexpr (PACK) bytes = *(const int *)(q + place<true>(0));
+    if constexpr (WHOLE) bytes = reinterpret_cast<const loose_int *>(q + place<true>(0))->x;
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -86,12 +89,12 @@ template <bool PACK> __device__ __forceinline__ void load_codes(const void *p, i
     v[3] = __builtin_amdgcn_cvt_f32_fp8(bytes, 3);
 }
 
-template <bool PACK> __device__ __forceinline__ void store_codes(void *p, int64_t from, int64_t rest, const float (&v)[4])
+template <bool WHOLE> __device__ __forceinline__ void store_codes(void *p, int64_t from, int64_t rest, const float (&v)[4])
 {
     uint8_t *q = (uint8_t *)p + from;
     int bytes = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
     bytes = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], bytes, true);
-    if constexpr (PACK) *(int *)(q + place<true>(0)) = bytes;
+    if constexpr (WHOLE) reinterpret_cast<loose_int *>(q + place<true>(0))->x = bytes;
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -147,19 +150,19 @@ template <bool ROOT> __device__ __forceinline__ float encode(float (&v)[4], cons
     return top * (1.0f / LARGEST);
 }
 
-template <int BITS, bool PACK> __device__ __forceinline__ void update_block(const adamw_args &a, const adamw_tensor &w, int64_t block, float gs)
+template <int BITS, bool WHOLE> __device__ __forceinline__ void update_block(const adamw_args &a, const adamw_tensor &w, int64_t block, float gs)
 {
     const int64_t from = block * BLOCK, rest = w.count - from;
     float g[4], p[4], m[4], v[4], r[4];
-    load_as<PACK>(w.grad, from, rest, a.grad_dtype, g);
-    load_four<PACK, float>(w.param, from, rest, p);
+    load_as<WHOLE>(w.grad, from, rest, a.grad_dtype, g);
+    load_four<WHOLE, float>(w.param, from, rest, p);
     if (BITS == 32) {
-        load_four<PACK, float>(w.m, from, rest, m);
-        load_four<PACK, float>(w.v, from, rest, v);
+        load_four<WHOLE, float>(w.m, from, rest, m);
+        load_four<WHOLE, float>(w.v, from, rest, v);
     } else {
         const float sm = w.m_scale[block], sv = w.v_scale[block];
-        load_codes<PACK>(w.m, from, rest, m);
-        load_codes<PACK>(w.v, from, rest, v);
+        load_codes<WHOLE>(w.m, from, rest, m);
+        load_codes<WHOLE>(w.v, from, rest, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             m[i] *= sm;
@@ -175,18 +178,18 @@ template <int BITS, bool PACK> __device__ __forceinline__ void update_block(cons
         r[i] = sqrtf(v[i]);
         p[i] = p[i] * w.keep - m[i] * a.rate / (r[i] * a.root + a.eps);
     }
-    store_four<PACK, float>(w.param, from, rest, p);
-    if (w.copy) store_as<PACK>(w.copy, from, rest, a.copy_dtype, p);
+    store_four<WHOLE, float>(w.param, from, rest, p);
+    if (w.copy) store_as<WHOLE>(w.copy, from, rest, a.copy_dtype, p);
     if (BITS == 32) {
-        store_four<PACK, float>(w.m, from, rest, m);
-        store_four<PACK, float>(w.v, from, rest, v);
+        store_four<WHOLE, float>(w.m, from, rest, m);
+        store_four<WHOLE, float>(w.v, from, rest, v);
     } else {
         uint32_t bits[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bits[i] = chance((uint32_t)from + place<PACK>(i), a.key);
+        for (int i = 0; i < 4; ++i) bits[i] = chance((uint32_t)from + place<WHOLE>(i), a.key);
         const float sm = encode<false>(m, bits), sv = encode<true>(r, bits);
-        store_codes<PACK>(w.m, from, rest, m);
-        store_codes<PACK>(w.v, from, rest, r);
+        store_codes<WHOLE>(w.m, from, rest, m);
+        store_codes<WHOLE>(w.v, from, rest, r);
         if ((threadIdx.x & 63) == 0) {
             w.m_scale[block] = sm;
             w.v_scale[block] = sv;
@@ -207,7 +210,7 @@ template <int BITS> __global__ __launch_bounds__(256) void adamw_kernel(adamw_ar
         const int64_t blocks = (w.count + BLOCK - 1) / BLOCK;
         int64_t block = (int64_t)(piece - a.first[k]) * 4 * a.each + wave;
         for (int i = 0; i < a.each && block < blocks; ++i, block += 4) {
-            if (w.pack && (block + 1) * BLOCK <= w.count) update_block<BITS, true>(a, w, block, gs);
+            if ((block + 1) * BLOCK <= w.count) update_block<BITS, true>(a, w, block, gs);
             else update_block<BITS, false>(a, w, block, gs);
         }
     }
@@ -268,7 +271,6 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
         a.pieces = 0;
         return hipGetLastError();
     };
-    const int state_bytes = o->state_bits == 32 ? 4 : 1;
     hipError_t e = hipSuccess;
     for (int i = 0; i < n_tensors && e == hipSuccess; ++i) {
         const bagel_adamw_tensor &t = tensors[i];
@@ -277,9 +279,7 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
         if (a.n == TENSORS || (a.n > 0 && a.pieces + pieces > 1u << 30)) {
             if ((e = launch()) != hipSuccess) break;
         }
-        const uintptr_t off = ((uintptr_t)t.param & 15) | ((uintptr_t)t.grad & (4 * bagel_type_bytes(o->grad_dtype) - 1)) |
-                              (((uintptr_t)t.m | (uintptr_t)t.v) & (4 * state_bytes - 1)) | ((uintptr_t)t.copy & (4 * bagel_type_bytes(o->copy_dtype) - 1));
-        a.tensor[a.n] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay), off == 0};
+        a.tensor[a.n] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay)};
         a.first[a.n++] = a.pieces;
         a.pieces += pieces;
     }

@@ -57,10 +57,14 @@ template <int WAVES, int N> __device__ __forceinline__ void row_sum(float (&v)[N
 }
 
 // A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i.  One wave to a row leaves four rows to a
-// workgroup, which need nothing of each other.
+// workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end of the row is moved back to end there:
+// its first entries are another pack's, and count as zero here.
 template <int V, int K, int WAVES> struct tile {
     static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, rows = WAVES == 1 ? 4 : 1;
-    __device__ static __forceinline__ int column(int k) { return V * (64 * WAVES * k + (WAVES == 1 ? threadIdx.x & 63 : threadIdx.x)); }
+    __device__ static __forceinline__ int place(int k) { return V * (64 * WAVES * k + (WAVES == 1 ? threadIdx.x & 63 : threadIdx.x)); }
+    __device__ static __forceinline__ bool here(int k, int width) { return place(k) < width; }
+    __device__ static __forceinline__ int column(int k, int width) { return min(place(k), width - V); }
+    __device__ static __forceinline__ int twice(int k, int width) { return max(place(k) + V - width, 0); }    // entries that are another pack's
     __device__ static __forceinline__ int64_t first_row() { return WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x; }
     __device__ static __forceinline__ int64_t next_row() { return (int64_t)gridDim.x * rows; }
     // vectors of the row's width, ones where there is none
@@ -69,7 +73,7 @@ template <int V, int K, int WAVES> struct tile {
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[k][i] = p && column(k) < width ? p[column(k) + i] : 1.0f;
+            for (int i = 0; i < V; ++i) v[k][i] = p && here(k, width) ? p[column(k, width) + i] : 1.0f;
     }
     __device__ static __forceinline__ void product(const float *p, const float *q, int width, float (&v)[K][V])
     {
@@ -81,21 +85,57 @@ template <int V, int K, int WAVES> struct tile {
 #pragma unroll
             for (int i = 0; i < V; ++i) v[k][i] *= w[k][i];
     }
-    template <typename T> __device__ static __forceinline__ void load(const T *row, int width, float (&v)[K][V])
-    {
+    // a row on its way, and what it is
+    template <typename T> struct packed {
+        bagel_pack<T, V> x[K];
+        __device__ __forceinline__ void load(const bagel_rows<T> &m, int64_t r, int width)
+        {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (row && column(k) < width) bagel_load<T, V>(row + column(k), v[k]);
-            else
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[k][i] = 0.0f;
+            for (int k = 0; k < K; ++k) {
+                if (m.data && here(k, width)) x[k] = reinterpret_cast<const bagel_loose_pack<T, V> *>(m.row(r) + column(k, width))->x;
+                else x[k] = (bagel_pack<T, V>)(T)0.0f;
+            }
         }
+        __device__ __forceinline__ void arrived(int width)
+        {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (V > 1 && here(k, width) && twice(k, width))
+#pragma unroll
+                    for (int i = 0; i < V - 1; ++i) x[k][i] = i < twice(k, width) ? (T)0.0f : x[k][i];
+        }
+        __device__ __forceinline__ float operator()(int k, int i) const { return (float)x[k][i]; }
+        // From here on the packs are what they are and not what they were converted to, which would be twice the registers.
+        __device__ __forceinline__ void keep()
+        {
+            if constexpr (sizeof(T) == 2 && V > 1) {
+                using words = uint32_t __attribute__((ext_vector_type(V / 2)));
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    words w = __builtin_bit_cast(words, x[k]);
+                    asm volatile("" : "+v"(w));
+                    x[k] = __builtin_bit_cast(bagel_pack<T, V>, w);
+                }
+            }
+        }
+    };
+    template <typename T> __device__ static __forceinline__ void store(T *row, int width, int k, const float (&v)[V])
+    {
+        if (!here(k, width)) return;
+        T *to = row + column(k, width);
+        bagel_pack<T, V> x;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+        if (V == 1 || !twice(k, width)) reinterpret_cast<bagel_loose_pack<T, V> *>(to)->x = x;
+        else
+#pragma unroll
+            for (int i = 1; i < V; ++i)
+                if (i >= twice(k, width)) to[i] = x[i];
     }
     template <typename T> __device__ static __forceinline__ void store(T *row, int width, const float (&v)[K][V])
     {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (column(k) < width) bagel_store<T, V>(row + column(k), v[k]);
+        for (int k = 0; k < K; ++k) store(row, width, k, v[k]);
     }
 };
 
@@ -111,9 +151,21 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join
     tl::vector(a.pre_weight, a.width, u);
     for (int64_t r = tl::first_row(); r < a.rows; r += tl::next_row()) {
         float z[K][V], g[K][V], v[K][V], s[1] = {0.0f};
-        tl::load(a.branch.data ? a.branch.row(r) : nullptr, a.width, z);
-        if (GATED) tl::load(a.gate.row(r), a.width, g);
-        tl::load(a.resid.data ? a.resid.row(r) : nullptr, a.width, v);
+        typename tl::template packed<T> pz, pg, px;
+        pz.load(a.branch, r, a.width);
+        if (GATED) pg.load(a.gate, r, a.width);
+        px.load(a.resid, r, a.width);
+        pz.arrived(a.width);
+        if (GATED) pg.arrived(a.width);
+        px.arrived(a.width);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                z[k][i] = pz(k, i);
+                if (GATED) g[k][i] = pg(k, i);
+                v[k][i] = px(k, i);
+            }
         if (a.branch.data) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
@@ -147,8 +199,8 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join
     }
 }
 
-template <typename T, int V, int K, int WAVES, bool GATED>
-__global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_grad_kernel(join_args<T> a)
+template <typename T, int V, int K, int WAVES, bool GATED, int ON_SIMD>
+__global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_grad_kernel(join_args<T> a)
 {
     using tl = tile<V, K, WAVES>;
     __shared__ float shared[2][WAVES][4];
@@ -161,50 +213,71 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_grad_kernel
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) sw[k][i] = su[k][i] = 0.0f;
+    struct row {
+        typename tl::template packed<T> o, y, z, g, x;
+    } next;
+    const auto ask = [&](int64_t r) {
+        next.o.load(a.out, r, a.width);
+        next.y.load(a.d_normed, r, a.width);
+        next.z.load(a.branch, r, a.width);
+        if (GATED) next.g.load(a.gate, r, a.width);
+        next.x.load(a.d_out, r, a.width);
+    };
+    constexpr bool ahead = WAVES < 16;       // sixteen waves leave 128 registers to a lane: no room for two rows
+    if (ahead && tl::first_row() < a.rows) ask(tl::first_row());
     for (int64_t r = tl::first_row(); r < a.rows; r += tl::next_row()) {
-        float z[K][V], g[K][V], o[K][V], dy[K][V], dx[K][V], s[3] = {0.0f, 0.0f, 0.0f};
-        tl::load(a.out.row(r), a.width, o);
-        tl::load(a.d_normed.data ? a.d_normed.row(r) : nullptr, a.width, dy);
-        tl::load(a.branch.data ? a.branch.row(r) : nullptr, a.width, z);
-        if (GATED) tl::load(a.gate.row(r), a.width, g);
-        tl::load(a.d_out.data ? a.d_out.row(r) : nullptr, a.width, dx);
+        if (!ahead) ask(r);
+        row p = next;
+        p.o.arrived(a.width);
+        p.y.arrived(a.width);
+        p.z.arrived(a.width);
+        if (GATED) p.g.arrived(a.width);
+        p.x.arrived(a.width);
+        if (ahead && r + tl::next_row() < a.rows) ask(r + tl::next_row());       // on its way while this row waits for its sums
+        float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                s[0] += z[k][i] * z[k][i];
-                s[1] += o[k][i] * o[k][i];
-                s[2] += dy[k][i] * u[k][i] * o[k][i];
+                s[0] += p.z(k, i) * p.z(k, i);
+                s[1] += p.o(k, i) * p.o(k, i);
+                s[2] += p.y(k, i) * u[k][i] * p.o(k, i);
             }
+        p.o.keep();
+        p.y.keep();
+        p.z.keep();
         row_sum<WAVES>(s, shared, turn);
         const float rz = 1.0f / sqrtf(s[0] * per + a.eps), ro = 1.0f / sqrtf(s[1] * per + a.eps);
         const float co = s[2] * per * ro * ro;
-        float t[1] = {0.0f};
+        float t[1] = {0.0f}, dn[K][V];                               // dn: gradient of R(branch)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            float dx[V], dg[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const float n = o[k][i] * ro;
-                dx[k][i] += ro * (dy[k][i] * u[k][i]) - n * co;
-                su[k][i] += dy[k][i] * n;
+                const float n = p.o(k, i) * ro, dy = p.y(k, i);
+                dx[i] = p.x(k, i) + (ro * (dy * u[k][i]) - n * co);
+                su[k][i] += dy * n;
                 float av = 1.0f, slope = 0.0f;
-                if (GATED) av = act(a.act, g[k][i], slope);
-                const float zn = z[k][i] * rz, x = dx[k][i] * cw[k][i];
-                sw[k][i] += dx[k][i] * av * zn;              // times c: d_post_weight, times w: d_scale
-                g[k][i] = x * zn * slope;
-                dy[k][i] = x * av;                           // gradient of R(branch)
-                t[0] += dy[k][i] * zn;
+                if (GATED) av = act(a.act, p.g(k, i), slope);
+                const float zn = p.z(k, i) * rz, x = dx[i] * cw[k][i];
+                sw[k][i] += dx[i] * av * zn;                 // times c: d_post_weight, times w: d_scale
+                dg[i] = x * zn * slope;
+                dn[k][i] = x * av;
+                t[0] += dn[k][i] * zn;
             }
-        if (a.d_resid.data) tl::store(a.d_resid.row(r), a.width, dx);
-        if (GATED && a.d_gate.data) tl::store(a.d_gate.row(r), a.width, g);
+            if (a.d_resid.data) tl::store(a.d_resid.row(r), a.width, k, dx);
+            if (GATED && a.d_gate.data) tl::store(a.d_gate.row(r), a.width, k, dg);
+        }
+        p.z.keep();
         if (!a.d_branch.data) continue;
         row_sum<WAVES>(t, shared, turn);
         const float cz = t[0] * per * rz;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[k][i] = rz * (dy[k][i] - z[k][i] * cz);
-        tl::store(a.d_branch.row(r), a.width, z);
+            for (int i = 0; i < V; ++i) dn[k][i] = rz * (dn[k][i] - p.z(k, i) * cz);
+        tl::store(a.d_branch.row(r), a.width, dn);
     }
     if (!a.sums) return;
     float *sums = a.sums + (size_t)blockIdx.x * 2 * a.width;
@@ -216,22 +289,26 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_grad_kernel
                 for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
-                        const int j = tl::column(k) + i;
+                        const int j = tl::place(k) + i;
                         all[0][j] = wave ? all[0][j] + sw[k][i] : sw[k][i];
                         all[1][j] = wave ? all[1][j] + su[k][i] : su[k][i];
                     }
             __syncthreads();
         }
-        for (int j = threadIdx.x; j < a.width; j += 256)
+        for (int j = threadIdx.x; j < a.width; j += 256) {
+            const int last = a.width - a.width % V;      // from here on the entries of the pack that was moved back
+            const int from = j < last ? j : j + V - a.width % V;
 #pragma unroll
-            for (int q = 0; q < 2; ++q) sums[(size_t)q * a.width + j] = all[q][j];
+            for (int q = 0; q < 2; ++q) sums[(size_t)q * a.width + j] = all[q][from];
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (tl::column(k) < a.width)
+            if (tl::here(k, a.width))
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const int j = tl::column(k) + i;
+                    const int j = tl::column(k, a.width) + i;
+                    if (i < tl::twice(k, a.width)) continue;
                     sums[j] = sw[k][i];
                     sums[a.width + j] = su[k][i];
                 }
@@ -250,16 +327,31 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
     if (sums)
         for (int j = first; j < a.width; j += 1024 * V)
 #pragma unroll
-            for (int i = 0; i < V; ++i) sums[j + i] = sums[a.width + j + i] = 0.0f;
+            for (int i = 0; i < V; ++i)
+                if (j + i < a.width) sums[j + i] = sums[a.width + j + i] = 0.0f;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *branch = a.branch.data ? a.branch.row(r) : nullptr, *d_normed = a.d_normed.data ? a.d_normed.row(r) : nullptr;
         const T *d_out = a.d_out.data ? a.d_out.row(r) : nullptr;
         const auto read = [&](const T *row, int j, float (&v)[V]) {
-            if (row) bagel_load<T, V>(row + j, v);
+            const int c = min(j, a.width - V), again = j - c;        // a pack that is moved back to the end of the row: entries before j are zero
+            bagel_pack<T, V> x = (bagel_pack<T, V>)(T)0.0f;
+            if (row) x = reinterpret_cast<const bagel_loose_pack<T, V> *>(row + c)->x;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = i < again ? 0.0f : (float)x[i];
+        };
+        const auto write = [&](const bagel_rows<T> &m, int j, const float (&v)[V]) {
+            const int c = min(j, a.width - V), again = j - c;
+            bagel_pack<T, V> x;
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = (T)v[i];
+            if (!m.data) return;
+            if (!again) reinterpret_cast<bagel_loose_pack<T, V> *>(m.row(r) + c)->x = x;
             else
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = 0.0f;
+                for (int i = 1; i < V; ++i)
+                    if (i >= again) m.row(r)[c + i] = x[i];
         };
+        const auto entry = [&](const float *p, int j, int i) { return p ? p[min(j, a.width - V) + i] : 1.0f; };
         float s[3] = {0.0f, 0.0f, 0.0f};
         for (int j = first; j < a.width; j += 1024 * V) {
             float z[V], o[V], dy[V];
@@ -270,7 +362,7 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
             for (int i = 0; i < V; ++i) {
                 s[0] += z[i] * z[i];
                 s[1] += o[i] * o[i];
-                s[2] += dy[i] * (a.pre_weight ? a.pre_weight[j + i] : 1.0f) * o[i];
+                s[2] += dy[i] * entry(a.pre_weight, j, i) * o[i];
             }
         }
         row_sum<16>(s, shared, turn);
@@ -289,8 +381,8 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
                 read(d_out, j, dx);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float n = o[i] * ro, cw = (a.scale ? a.scale[j + i] : 1.0f) * (a.post_weight ? a.post_weight[j + i] : 1.0f);
-                    dx[i] += ro * (dy[i] * (a.pre_weight ? a.pre_weight[j + i] : 1.0f)) - n * co;
+                    const float n = o[i] * ro, cw = entry(a.scale, j, i) * entry(a.post_weight, j, i);
+                    dx[i] += ro * (dy[i] * entry(a.pre_weight, j, i)) - n * co;
                     float av = 1.0f, slope = 0.0f;
                     if (GATED) av = act(a.act, g[i], slope);
                     const float zn = z[i] * rz, x = dx[i] * cw, k = x * av;
@@ -298,17 +390,18 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
                         t[0] += k * zn;
                         continue;
                     }
-                    if (sums) {
-                        sums[j + i] += dx[i] * av * zn;
-                        sums[a.width + j + i] += dy[i] * n;
+                    if (sums && i >= j - min(j, a.width - V)) {
+                        const int at = min(j, a.width - V) + i;
+                        sums[at] += dx[i] * av * zn;
+                        sums[a.width + at] += dy[i] * n;
                     }
                     g[i] = x * zn * slope;
                     z[i] = rz * (k - z[i] * cz);
                 }
                 if (pass == 0) continue;
-                if (a.d_resid.data) bagel_store<T, V>(a.d_resid.row(r) + j, dx);
-                if (GATED && a.d_gate.data) bagel_store<T, V>(a.d_gate.row(r) + j, g);
-                if (a.d_branch.data) bagel_store<T, V>(a.d_branch.row(r) + j, z);
+                write(a.d_resid, j, dx);
+                if (GATED) write(a.d_gate, j, g);
+                write(a.d_branch, j, z);
             }
             if (pass == 0) row_sum<16>(t, shared, turn);
         }
@@ -341,8 +434,10 @@ __global__ __launch_bounds__(1024) void join_sums_kernel(const float *sums, int 
     }
 }
 
-constexpr int JOIN_GROUPS = 512;
-int grad_groups(int64_t rows) { return (int)(rows < JOIN_GROUPS ? rows : JOIN_GROUPS); }
+// Workgroups of the backward pass: two to a compute unit, four where rows are short (256 x 262144 in bf16: 262 us with two, 226 with four; 1024 x
+// 64000 in f32: 392 and 452).
+constexpr int most_groups(int width) { return width <= 256 ? 1024 : 512; }
+int grad_groups(int64_t rows, int width) { return (int)(rows < most_groups(width) ? rows : most_groups(width)); }
 
 template <typename T> join_args<T> args_of(const bagel_join &j)
 {
@@ -368,16 +463,16 @@ template <typename T> join_args<T> args_of(const bagel_join &j)
 }
 
 // The number of workgroups.
-template <typename T, int V, int K, int WAVES, bool GRAD = true> int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
+template <typename T, int V, int K, int WAVES, bool GRAD = true, int ON_SIMD = 1> int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
 {
     constexpr int threads = tile<V, K, WAVES>::threads, rows = tile<V, K, WAVES>::rows;
-    const int64_t full = (a.rows + rows - 1) / rows, most = grad ? JOIN_GROUPS : 4096;
+    const int64_t full = (a.rows + rows - 1) / rows, most = grad ? most_groups(a.width) : 4096;
     const int groups = (int)(full < most ? full : most);
     const bool gated = a.act != BAGEL_ACT_NONE && a.branch.data;
     if (GRAD && grad) {
         if constexpr (GRAD) {
-            if (gated) join_grad_kernel<T, V, K, WAVES, true><<<groups, threads, 0, stream>>>(a);
-            else join_grad_kernel<T, V, K, WAVES, false><<<groups, threads, 0, stream>>>(a);
+            if (gated) join_grad_kernel<T, V, K, WAVES, true, ON_SIMD><<<groups, threads, 0, stream>>>(a);
+            else join_grad_kernel<T, V, K, WAVES, false, ON_SIMD><<<groups, threads, 0, stream>>>(a);
         }
     } else {
         if (gated) join_kernel<T, V, K, WAVES, true><<<groups, threads, 0, stream>>>(a);
@@ -388,48 +483,38 @@ template <typename T, int V, int K, int WAVES, bool GRAD = true> int launch_tile
 
 template <typename T, int V> int launch_wide(const join_args<T> &a, hipStream_t stream)
 {
-    const int groups = grad_groups(a.rows);
+    const int groups = grad_groups(a.rows, a.width);
     if (a.act != BAGEL_ACT_NONE && a.branch.data) join_grad_wide_kernel<T, V, true><<<groups, 1024, 0, stream>>>(a);
     else join_grad_wide_kernel<T, V, false><<<groups, 1024, 0, stream>>>(a);
     return groups;
 }
 
-// A row is spread over as few waves as hold it with two packs a lane: fewer waves mean fewer barriers, more packs fewer waves on a compute unit.
-template <typename T, int V> int launch_width(const join_args<T> &a, bool grad, hipStream_t stream)
-{
-    const int packs = (a.width + V - 1) / V;
-    if constexpr (V > 1) {
-        if (packs <= 64) return launch_tile<T, V, 1, 1>(a, grad, stream);
-        if (packs <= 128) return launch_tile<T, V, 2, 1>(a, grad, stream);
-        if (packs <= 256) return launch_tile<T, V, 1, 4>(a, grad, stream);
-        if (packs <= 512) return launch_tile<T, V, 2, 4>(a, grad, stream);
-        if (packs <= 1024) return launch_tile<T, V, 2, 8>(a, grad, stream);
-        if (grad) return launch_wide<T, V>(a, stream);
-        if (packs <= 2048) return launch_tile<T, V, 2, 16, false>(a, grad, stream);
-        if constexpr (V == 4) return launch_tile<T, V, 4, 16, false>(a, grad, stream);
-        return 0;                            // (16384 entries of 16 bits are 2048 packs)
-    } else {
-        if (packs <= 256) return launch_tile<T, 1, 4, 1>(a, grad, stream);
-        if (packs <= 1024) return launch_tile<T, 1, 4, 4>(a, grad, stream);
-        if (packs <= 2048) return launch_tile<T, 1, 4, 8>(a, grad, stream);
-        if (grad) return launch_wide<T, 1>(a, stream);
-        if (packs <= 4096) return launch_tile<T, 1, 4, 16, false>(a, grad, stream);
-        return launch_tile<T, 1, 16, 16, false>(a, grad, stream);
-    }
-}
-
-template <typename T> int launch_rows(const join_args<T> &a, const bagel_join &j, bool grad, hipStream_t stream)
+// Packs of 16 bytes, of 8 where those would leave half of a wave without any, single entries where the row is shorter than a pack.  Up to 128 packs a row
+// takes one wave (no barrier).  Above, the way back takes one pack a lane while eight waves hold the row: with the packs of the next row on their way
+// beside those of this one there is little room for more (4096 x 65536 in bf16: 979 us with two packs on four waves, 832 with one on eight); where
+// some of the eight have nothing, four waves on a SIMD at the price of a few spilled registers (2500 x 20000: 278 us, 221; 4096: 832, 891).
+// Forward, two packs on four waves and one on eight are alike up to 512.
+template <typename T> int launch_rows(const join_args<T> &a, bool grad, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(T);
-    int pack = j.width % V ? 1 : V;
-    const bagel_matrix all[] = {j.branch, j.gate, j.resid, j.out, j.normed, j.d_out, j.d_normed, j.d_branch, j.d_gate, j.d_resid};
-    for (int i = 0; i < (grad ? 10 : 5); ++i) pack = bagel_matrix_pack(all[i], j.rows, j.dtype, pack);
-    return pack == V ? launch_width<T, V>(a, grad, stream) : launch_width<T, 1>(a, grad, stream);
+    const int packs = (a.width + V - 1) / V;
+    if (a.width < V) return launch_tile<T, 1, 1, 1>(a, grad, stream);
+    if (packs <= 32) return launch_tile<T, V / 2, 1, 1>(a, grad, stream);
+    if (packs <= 64) return launch_tile<T, V, 1, 1>(a, grad, stream);
+    if (packs <= 128) return launch_tile<T, V, 2, 1>(a, grad, stream);
+    if (packs <= 256) return launch_tile<T, V, 1, 4>(a, grad, stream);
+    if (packs <= 384 && grad) return launch_tile<T, V, 1, 8, true, 4>(a, true, stream);
+    if (packs <= 512) return grad ? launch_tile<T, V, 1, 8>(a, true, stream) : launch_tile<T, V, 2, 4, false>(a, false, stream);
+    if (packs <= 1024) return launch_tile<T, V, 2, 8>(a, grad, stream);
+    if (packs <= 2048 && (V == 4 || !grad)) return launch_tile<T, V, 2, 16, V == 4>(a, grad, stream);
+    if (grad) return launch_wide<T, V>(a, stream);
+    if constexpr (V == 4) return launch_tile<T, V, 4, 16, false>(a, grad, stream);
+    return 0;                                // (16384 entries of 16 bits are 2048 packs)
 }
 
 template <typename T> hipError_t launch_join(const bagel_join &j, hipStream_t stream)
 {
-    launch_rows(args_of<T>(j), j, false, stream);
+    launch_rows(args_of<T>(j), false, stream);
     return hipGetLastError();
 }
 
@@ -438,7 +523,7 @@ template <typename T> hipError_t launch_join_grad(const bagel_join &j, hipStream
     join_args<T> a = args_of<T>(j);
     const bool sums = j.d_post_weight || j.d_scale || j.d_pre_weight;
     a.sums = sums ? (float *)j.workspace : nullptr;
-    const int groups = j.rows > 0 ? launch_rows(a, j, true, stream) : 0;
+    const int groups = j.rows > 0 ? launch_rows(a, true, stream) : 0;
     if (sums)
         join_sums_kernel<<<(2 * j.width + 63) / 64, 1024, 0, stream>>>(a.sums, groups, j.width, j.post_weight, j.scale, j.d_post_weight, j.d_scale, j.d_pre_weight);
     return hipGetLastError();
@@ -480,7 +565,7 @@ const char *check_join(const bagel_join *j, bool grad)
 extern "C" int64_t bagel_block_join_workspace(int64_t rows, int32_t width)
 {
     if (rows < 0 || width < 1 || width > BAGEL_JOIN_MAX_WIDTH) return BAGEL_EINVAL;
-    return (int64_t)grad_groups(rows) * 2 * width * sizeof(float);
+    return (int64_t)grad_groups(rows, width) * 2 * width * sizeof(float);
 }
 
 extern "C" int bagel_block_join(const bagel_join *j, void *hip_stream)

@@ -193,9 +193,6 @@ template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, 
 // What is the same in both directions: which span and channels a workgroup has, and its reads.
 template <typename T, int V, int S> struct wave_tile {
     using pack = bagel_pack<T, V>;
-    struct __attribute__((packed, aligned(sizeof(T)))) loose {               // rows of an odd width or stride: packs need not be aligned
-        pack x;
-    };
     static constexpr int rows = S * WAVES;
     int span, wave, lane, t0, ch;            // ch: its first channel.  A lane that has none, or only one of two, takes the last ones: it does once
                                              // more what another lane does.
@@ -214,7 +211,7 @@ template <typename T, int V, int S> struct wave_tile {
     template <typename Q> __device__ __forceinline__ void load(const bagel_rows<Q> &m, int last, pack (&x)[S]) const
     {
 #pragma unroll
-        for (int i = 0; i < S; ++i) x[i] = reinterpret_cast<const loose *>(m.row(min(t0 + i, last)) + ch)->x;
+        for (int i = 0; i < S; ++i) x[i] = reinterpret_cast<const bagel_loose_pack<T, V> *>(m.row(min(t0 + i, last)) + ch)->x;
     }
     // From here on the packs are what they are and not what they were converted to: the converted ones of two channels in 16 bits would take twice
     // the registers between two passes over the rows.
@@ -269,13 +266,7 @@ template <typename T, int V, int S> struct wave_tile {
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = seg.outside(i) ? 0.0f : at(a.d_final, (int64_t)sequence * a.width + ch + v);
     }
-    __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const
-    {
-        pack y;
-#pragma unroll
-        for (int v = 0; v < V; ++v) y[v] = (T)x[v];
-        reinterpret_cast<loose *>(m.row(row) + ch)->x = y;
-    }
+    __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const { bagel_store<T, V>(m.row(row) + ch, x); }
 };
 
 // The number of the work that this workgroup takes.
