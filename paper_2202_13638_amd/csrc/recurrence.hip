@@ -145,7 +145,15 @@ template <int S, typename A> __device__ __forceinline__ segment<S> segment_at(co
     }
     // Down to 64 offsets in a row, o, from number lo on, of which the first is not behind t0 (or is the first of all)
     int lo = 0, step = n / 64 + 1;
-    const int first = a.offsets[0], stop = min(a.offsets[n], a.rows);
+    int first, stop;
+    if (step == 1) {
+        first = __builtin_amdgcn_readlane(o, 0);
+        stop = __builtin_amdgcn_readlane(o, n);
+    } else {
+        first = a.offsets[0];
+        stop = a.offsets[n];
+    }
+    stop = min(stop, a.rows);
     while (step > 1) {
         const int k = __popcll(__ballot((int64_t)lo + (int64_t)lane * step <= n && o <= t0));
         lo += max(k - 1, 0) * step;
@@ -549,22 +557,22 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     }
 }
 
-// The sum over the spans, 16 threads to a channel.
+// The sum over the spans, 64 threads to a channel: with 16 of 64 channels a workgroup it is spread over four times as many of them.
 __global__ __launch_bounds__(1024) void bias_kernel(const float *sums, int spans, int width, float *d_bias)
 {
-    __shared__ float part[16][64];
-    const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, ch = blockIdx.x * 64 + lane;
-    const int from = (int)((int64_t)spans * slice / 16), to = (int)((int64_t)spans * (slice + 1) / 16);
+    __shared__ float part[64][17];
+    const int lane = threadIdx.x & 15, slice = threadIdx.x >> 4, ch = blockIdx.x * 16 + lane;
+    const int from = (int)((int64_t)spans * slice / 64), to = (int)((int64_t)spans * (slice + 1) / 64);
     float v = 0.0f;
     if (ch < width)
 #pragma unroll 8
         for (int k = from; k < to; ++k) v += sums[(int64_t)k * width + ch];
     part[slice][lane] = v;
     __syncthreads();
-    if (slice > 0 || ch >= width) return;
+    if (threadIdx.x >= 16 || ch >= width) return;
     v = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v += part[k][lane];
+    for (int k = 0; k < 64; ++k) v += part[k][lane];
     d_bias[ch] = v;
 }
 
@@ -640,7 +648,7 @@ template <typename T, bool GRAD> hipError_t launch_pass(const bagel_gated_recurr
     recurrence_args<T> a = args_of<T>(r, GRAD);
     if (sizeof(T) == 2 && r.width > 1) launch_spans<T, 4 / sizeof(T), 16, GRAD>(a, r, stream);
     else launch_spans<T, 1, 16, GRAD>(a, r, stream);
-    if (GRAD && r.d_bias) bias_kernel<<<(r.width + 63) / 64, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
+    if (GRAD && r.d_bias) bias_kernel<<<(r.width + 15) / 16, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
     return hipGetLastError();
 }
 
