@@ -218,14 +218,16 @@ def bagel_sample_eval_static(dims: Dims, X, lengthscale, signal_var, omega, phas
 # (A call of a few rows takes about as long on the host as on the GPU: arguments are looked at once, in the order of the structure.)
 JOIN_MAX_WIDTH, RECURRENCE_SPAN, ADAMW_BLOCK = 16384, 128, 256
 _ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
-_torch = _DTYPES = None
+_torch = _DTYPES = _raw_stream = None
 
 
 def _load():
     """The library, with torch and its types looked up once."""
-    global _torch, _DTYPES
+    global _torch, _DTYPES, _raw_stream
     if _DTYPES is None:
         import torch as _torch
+        # the handle of the current stream, in 0.1 us where torch.cuda.current_stream() takes 2.7
+        _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: _torch.cuda.current_stream(device).cuda_stream)
         _DTYPES = {_torch.float32: 0, _torch.bfloat16: 1, _torch.float16: 2}
     return _lib or load()
 
@@ -238,25 +240,27 @@ def _dtype_code(t, name):
 
 
 def _stream(stream):
+    """(handle of the call's stream, current device)"""
+    device = _torch.cuda.current_device()
     if stream is None:
-        return _torch.cuda.current_stream()
-    if stream.device_index != _torch.cuda.current_device():
+        return _raw_stream(device), device
+    if stream.device_index != device:
         raise ValueError("the stream must be one of the current GPU")
-    return stream
+    return stream.cuda_stream, device
 
 
 def _first_matrix(t, name, stream):
-    """(shape, type, its code, device) of the matrix that the others of a call are held to, and the call's stream."""
+    """(shape, type, its code, device) of the matrix that the others of a call are held to, and the handle of the call's stream."""
     code = _dtype_code(t, name)
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
-    stream = _stream(stream)
-    if t.get_device() != stream.device_index:
+    on, device = _stream(stream)
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on the current GPU")
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{name} must have two dimensions, rows and width, not {len(shape)}")
-    return shape, t.dtype, code, t.get_device(), stream
+    return shape, t.dtype, code, device, on
 
 
 def _matrix(t, name, shape, dtype, device):
@@ -322,7 +326,7 @@ def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="no
                  *_matrix(resid, "resid", shape, dtype, device), *_matrix(out, "out", shape, dtype, device),
                  *_matrix(normed, "normed", shape, dtype, device), _vector(post_weight, "post_weight", vector, device),
                  _vector(scale, "scale", vector, device), _vector(pre_weight, "pre_weight", vector, device))
-    _done(lib, lib.bagel_block_join(args, on.cuda_stream))
+    _done(lib, lib.bagel_block_join(args, on))
 
 
 def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None,
@@ -343,7 +347,7 @@ def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, 
     if d_post_weight is not None or d_scale is not None or d_pre_weight is not None:
         workspace = _workspace(workspace, lib.bagel_block_join_workspace(shape[0], shape[1]), device, stream)
         args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _done(lib, lib.bagel_block_join_grad(args, on.cuda_stream))
+    _done(lib, lib.bagel_block_join_grad(args, on))
 
 
 def bagel_recurrence_carry_rows(rows: int) -> int:
@@ -385,7 +389,7 @@ def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None,
                        _vector(initial, "initial", state, device), _vector(final, "final", state, device),
                        _vector(carry, "carry", (lib.bagel_recurrence_carry_rows(rows), width), device) if carry is not None else None, None,
                        None, 0, None, 0, None, 0, None, None, None, workspace.data_ptr(), workspace.numel())
-    _done(lib, lib.bagel_recurrence(args, on.cuda_stream))
+    _done(lib, lib.bagel_recurrence(args, on))
 
 
 def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, carry, *, bias=None, initial=None, d_final=None, d_initial=None,
@@ -405,7 +409,7 @@ def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, c
                        *_matrix(d_forget, "d_forget", shape, dtype, device), _vector(d_final, "d_final", state, device),
                        _vector(d_initial, "d_initial", state, device), _vector(d_bias, "d_bias", shape[1:], device),
                        workspace.data_ptr(), workspace.numel())
-    _done(lib, lib.bagel_recurrence_grad(args, on.cuda_stream))
+    _done(lib, lib.bagel_recurrence_grad(args, on))
 
 
 def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, stream=None):
@@ -415,7 +419,7 @@ def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, strea
     args = _Recurrence(0, shape[1], code, shape[0], None, *_matrix(value, "value", shape, dtype, device),
                        *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device), *_matrix(hidden, "hidden", shape, dtype, device),
                        _vector(bias, "bias", shape[1:], device), None, None, None, _vector(_needed(state, "state"), "state", shape, device))
-    _done(lib, lib.bagel_recurrence_step(args, on.cuda_stream))
+    _done(lib, lib.bagel_recurrence_step(args, on))
 
 
 def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, copy=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
@@ -432,8 +436,7 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
     lists = [params, grads, m, v, decay] + ([copy] if copy is not None else []) + ([m_scale, v_scale] if eight else [])
     if any(x is None or len(x) != n for x in lists):
         raise ValueError("the lists of one update must have an entry for every tensor (moments in 8 bits need m_scale and v_scale)")
-    on = _stream(stream)
-    device = on.device_index
+    on, device = _stream(stream)
     f32, grad_type = _torch.float32, grads[0].dtype if n else None
     state = _torch.float8_e4m3fn if eight else f32
     scale = None
@@ -456,15 +459,18 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
         count = p.numel()
         ms = vs = ci = 0
         if eight:
-            blocks = (-(-count // ADAMW_BLOCK),)
-            ms, vs = _vector(_needed(m_scale[i], "m_scale"), "m_scale", blocks, device), _vector(_needed(v_scale[i], "v_scale"), "v_scale", blocks, device)
+            ms, vs, blocks = m_scale[i], v_scale[i], -(-count // ADAMW_BLOCK)
+            if not (ms.dtype is f32 and vs.dtype is f32 and ms.numel() == vs.numel() == blocks and ms.is_contiguous() and vs.is_contiguous() and
+                    ms.get_device() == vs.get_device() == device):
+                raise ValueError(f"tensor {i} of an update: m_scale and v_scale must be contiguous float32 tensors of {blocks} values on cuda:{device}")
+            ms, vs = ms.data_ptr(), vs.data_ptr()
         if copy is not None:
             c = copy[i]
             if c.dtype is not copy[0].dtype or c.shape != shape or not c.is_contiguous() or c.get_device() != device:
                 raise ValueError(f"copy {i} of an update: a contiguous {copy[0].dtype} tensor of shape {tuple(shape)} on cuda:{device} is needed")
             ci = c.data_ptr()
         table += (p.data_ptr(), g.data_ptr(), mi.data_ptr(), vi.data_ptr(), ms, vs, ci, count, decay[i])
-    _done(lib, lib.bagel_adamw_step(struct.pack(_ADAMW_TENSOR * n, *table), n, options, on.cuda_stream))
+    _done(lib, lib.bagel_adamw_step(struct.pack(_ADAMW_TENSOR * n, *table), n, options, on))
 
 
 class Bagel:
