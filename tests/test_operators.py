@@ -337,6 +337,68 @@ def test_recurrence_and_its_gradient(lengths, width, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("width", [70, 131])
+def test_recurrence_over_many_spans_gives_the_same_bits_every_time(width):
+    """Sequences over several blocks of 32 spans, where a span's state comes from others that run beside it."""
+    at = [0, 9000, 9001, 14100]
+    x, f, dh = (_normal((at[-1], width), i, torch.bfloat16).cuda() for i in (1, 2, 3))
+    bias, h0, dl = _normal((width,), 4, mean=3.0).cuda(), _normal((3, width), 5).cuda(), _normal((3, width), 6).cuda()
+    runs = [_run_recurrence(x, f, at, bias, h0, dh, dl) for _ in range(4)]
+    for other in runs[1:]:
+        for k, v in runs[0].items():
+            assert torch.equal(v, other[k]), k
+    want, terms = _recurrence_ref(*(t.cpu() for t in (x, f)), at, *(t.cpu() for t in (bias, h0, dh, dl)))
+    for k, v in want.items():
+        _near(runs[0][k], v, k, terms=terms if k == "d_bias" else None)
+
+
+@gpu
+@pytest.mark.parametrize("count", [62, 63, 64, 65, 700, 5000])
+def test_recurrence_of_many_short_sequences(count):
+    """Numbers of sequences at which the search for a row's sequence takes one look, two and three; a third of them are empty."""
+    g = torch.Generator().manual_seed(count)
+    n = torch.randint(0, 9, (count,), generator=g) * (torch.rand(count, generator=g) > 0.33)
+    at = [0] + torch.cumsum(n, 0).tolist()
+    width = 10
+    x, f, dh = (_normal((at[-1], width), i).cuda() for i in (1, 2, 3))
+    bias, h0, dl = _normal((width,), 4).cuda(), _normal((count, width), 5).cuda(), _normal((count, width), 6).cuda()
+    got = _run_recurrence(x, f, at, bias, h0, dh, dl)
+    want, terms = _recurrence_ref(*(t.cpu() for t in (x, f)), at, *(t.cpu() for t in (bias, h0, dh, dl)))
+    for k, v in want.items():
+        _near(got[k], v, k, terms=terms if k == "d_bias" else None)
+
+
+@gpu
+def test_recurrence_of_every_kind_of_nan():
+    """What is published of a span is told from nothing by a bit pattern: no NaN of the inputs may look like it."""
+    rows, width = 5000, 64
+    x, f, dh = (_normal((rows, width), i).cuda() for i in (1, 2, 3))
+    for k, bits in enumerate((-1, 0x7FFFFFFF, 0x7FC00000, -4194304, 0x7F800001)):
+        nan = torch.tensor([bits], dtype=torch.int32, device="cuda").view(torch.float32)
+        for t in (x, f, dh):
+            t[100 + 300 * k, k] = nan[0]
+    r = _run_recurrence(x, f, [0, rows], None, None, dh, None)
+    assert torch.isnan(r["hidden"][-1, :5]).all() and torch.isfinite(r["hidden"][:, 5:]).all()
+    assert torch.isfinite(r["d_value"][:, 5:]).all() and torch.isnan(r["d_initial"][0, :5]).all()
+
+
+@gpu
+def test_recurrence_rows_beyond_32_bits():
+    rows, width, stride = 600, 6, 1 << 23
+    big = torch.empty(stride * (rows - 1) + 6 * width, dtype=torch.bfloat16, device="cuda")
+    v = [big.as_strided((rows, width), (stride, 1), i * width) for i in range(6)]
+    x, f, dh = (_normal((rows, width), i, torch.bfloat16) for i in (1, 2, 3))
+    for to, src in zip(v, (x, f, dh)):
+        to.copy_(src)
+    carry = torch.empty(binding.bagel_recurrence_carry_rows(rows), width, device="cuda")
+    binding.bagel_recurrence(v[0], v[1], v[3], 1, carry=carry)
+    binding.bagel_recurrence_grad(v[0], v[1], v[2], v[4], v[5], 1, carry)
+    want, _ = _recurrence_ref(x, f, [0, rows], None, None, dh, None)
+    for t, k in zip(v[3:], ("hidden", "d_value", "d_forget")):
+        _near(t.contiguous(), want[k], k)
+
+
+@gpu
 def test_recurrence_equal_lengths_without_offsets():
     rows, n, width = 7 * 93, 7, 66
     x, f, dh = (_normal((rows, width), i).cuda() for i in (1, 2, 3))
