@@ -98,9 +98,6 @@ class _AdamWTensor(C.Structure):
                 ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("count", C.c_int64), ("weight_decay", C.c_double)]
 
 
-_ADAMW_TENSOR = "7Pqd"           # the same for struct.pack
-
-
 class _AdamW(C.Structure):
     _fields_ = [("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("grad_scale", C.c_void_p), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
@@ -162,12 +159,10 @@ def load():
         L.bagel_block_join_workspace.restype = L.bagel_recurrence_workspace.restype = L.bagel_recurrence_carry_rows.restype = C.c_int64
         L.bagel_block_join_workspace.argtypes = L.bagel_recurrence_workspace.argtypes = [C.c_int64, C.c_int32]
         L.bagel_recurrence_carry_rows.argtypes = [C.c_int64]
-        for name in ("bagel_block_join", "bagel_block_join_grad"):
-            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [C.POINTER(_Join), vp]
-        for name in ("bagel_recurrence", "bagel_recurrence_grad", "bagel_recurrence_step"):
-            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [C.POINTER(_Recurrence), vp]
+        for name in ("bagel_block_join", "bagel_block_join_grad", "bagel_recurrence", "bagel_recurrence_grad", "bagel_recurrence_step"):
+            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [vp, vp]
         L.bagel_adamw_step.restype = C.c_int
-        L.bagel_adamw_step.argtypes = [vp, C.c_int32, C.POINTER(_AdamW), vp]
+        L.bagel_adamw_step.argtypes = [vp, C.c_int32, vp, vp]
         L.bagel_last_error.restype = C.c_char_p
         L.bagel_last_error.argtypes = [vp]
         _lib = L
@@ -215,88 +210,50 @@ def bagel_sample_eval_static(dims: Dims, X, lengthscale, signal_var, omega, phas
 
 # ---------------------------------------------------------------------------- operators of a policy with memory
 # Outputs are tensors of the caller; what is None is left out.  `stream` None: torch's current one.  All tensors are on the current device.
-# (A call of a few rows takes about as long on the host as on the GPU: arguments are looked at once, in the order of the structure.)
+# Calls of a few rows take as long on the host as on the GPU, so the tensors are checked and packed by compiled code (csrc/marshal.cpp), which
+# makes the structures above as bytes.
 JOIN_MAX_WIDTH, RECURRENCE_SPAN, ADAMW_BLOCK = 16384, 128, 256
 _ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
-_torch = _DTYPES = _raw_stream = None
+_JOIN_HEAD, _RECURRENCE_HEAD, _ADAMW_OPTIONS, _WORKSPACE = (struct.Struct(f) for f in ("qiiif", "qiii4xP", "qddddPiiiI", "Pq"))
+assert (_JOIN_HEAD.size, _RECURRENCE_HEAD.size, _ADAMW_OPTIONS.size) == (_Join.branch.offset, _Recurrence.value.offset, C.sizeof(_AdamW))
+_NOTHING = bytes(256)
+_torch = _marshal = _raw_stream = None
 
 
 def _load():
-    """The library, with torch and its types looked up once."""
-    global _torch, _DTYPES, _raw_stream
-    if _DTYPES is None:
+    """The library, with torch and the compiled checks looked up once."""
+    global _torch, _marshal, _raw_stream
+    if _raw_stream is None:
         import torch as _torch
+        from . import _marshal
         # the handle of the current stream, in 0.1 us where torch.cuda.current_stream() takes 2.7
         _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: _torch.cuda.current_stream(device).cuda_stream)
-        _DTYPES = {_torch.float32: 0, _torch.bfloat16: 1, _torch.float16: 2}
     return _lib or load()
-
-
-def _dtype_code(t, name):
-    code = _DTYPES.get(t.dtype) if isinstance(t, _torch.Tensor) else None
-    if code is None:
-        raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor")
-    return code
 
 
 def _stream(stream):
     """(handle of the call's stream, current device)"""
-    device = _torch.cuda.current_device()
+    device = _torch.cuda.current_device() if _torch.cuda.is_initialized() or _torch.cuda.is_available() else -1
     if stream is None:
-        return _raw_stream(device), device
+        return _raw_stream(device) if device >= 0 else 0, device
     if stream.device_index != device:
         raise ValueError("the stream must be one of the current GPU")
     return stream.cuda_stream, device
 
 
-def _first_matrix(t, name, stream):
-    """(shape, type, its code, device) of the matrix that the others of a call are held to, and the handle of the call's stream."""
-    code = _dtype_code(t, name)
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on the GPU")
-    on, device = _stream(stream)
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on the current GPU")
-    shape = t.shape
-    if len(shape) != 2:
-        raise ValueError(f"{name} must have two dimensions, rows and width, not {len(shape)}")
-    return shape, t.dtype, code, device, on
-
-
-def _matrix(t, name, shape, dtype, device):
-    """(pointer, row stride) of a matrix: any row stride, the entries of a row next to each other."""
-    if t is None:
-        return None, 0
-    if not isinstance(t, _torch.Tensor):
-        raise ValueError(f"{name} must be a tensor")
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{device}, not {t.dtype} of {tuple(t.shape)} on {t.device}")
-    stride, step = t.stride()
-    if step != 1 and shape[1] > 1 and shape[0] > 0:
-        raise ValueError(f"{name}: the entries of a row must be next to each other")
-    return t.data_ptr(), stride if shape[0] > 1 else shape[1]
-
-
-def _vector(t, name, shape, device):
-    """Pointer of a contiguous float32 tensor."""
-    if t is None:
-        return None
-    p = _ptr(t, shape, name)
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on cuda:{device}")
-    return p
-
-
 def _workspace(workspace, need, device, stream):
     """The caller's work space, or one from torch's allocator on the call's stream (`stream` as the caller gave it)."""
     if workspace is None:
+        if need == 0:
+            return None, bytes(16)
         if stream is None:
-            return _torch.empty(max(need, 16), dtype=_torch.uint8, device=device)
-        with _torch.cuda.stream(stream):
-            return _torch.empty(max(need, 16), dtype=_torch.uint8, device=device)
-    if not isinstance(workspace, _torch.Tensor) or workspace.dtype != _torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
+            workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
+        else:
+            with _torch.cuda.stream(stream):
+                workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
+    elif not isinstance(workspace, _torch.Tensor) or workspace.dtype != _torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{device}")
-    return workspace
+    return workspace, _WORKSPACE.pack(workspace.data_ptr(), workspace.numel())
 
 
 def _done(lib, rc):
@@ -315,17 +272,20 @@ def _act(act):
     return _ACTS[act]
 
 
+_FORWARD, _BACKWARD = ("branch", "gate", "resid", "out", "normed"), ("d_out", "d_normed", "d_branch", "d_gate", "d_resid")
+_VECTORS, _D_VECTORS = ("post_weight", "scale", "pre_weight"), ("d_post_weight", "d_scale", "d_pre_weight")
+
+
 def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="none", post_weight=None, scale=None, pre_weight=None, eps=1e-6,
                      stream=None):
     """out = resid + scale * act(gate) * (R(branch) * post_weight), normed = R(out) * pre_weight (see include/bagel.h)."""
     lib = _load()
     kind = _act(act)
-    shape, dtype, code, device, on = _first_matrix(*((resid, "resid") if resid is not None else (branch, "branch")), stream)
-    vector = shape[1:]
-    args = _Join(shape[0], shape[1], code, kind, eps, *_matrix(branch, "branch", shape, dtype, device), *_matrix(gate, "gate", shape, dtype, device),
-                 *_matrix(resid, "resid", shape, dtype, device), *_matrix(out, "out", shape, dtype, device),
-                 *_matrix(normed, "normed", shape, dtype, device), _vector(post_weight, "post_weight", vector, device),
-                 _vector(scale, "scale", vector, device), _vector(pre_weight, "pre_weight", vector, device))
+    on, device = _stream(stream)
+    like, name = (resid, "resid") if resid is not None else (branch, "branch")
+    rows, width, code = _marshal.first(like, name, device)
+    args = (_JOIN_HEAD.pack(rows, width, code, kind, eps) + _marshal.matrices(like, _FORWARD, (branch, gate, resid, out, normed)) +
+            _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) + _NOTHING)
     _done(lib, lib.bagel_block_join(args, on))
 
 
@@ -335,18 +295,14 @@ def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, 
     """The gradient of bagel_block_join at the `out` it stored (see include/bagel.h)."""
     lib = _load()
     kind = _act(act)
-    shape, dtype, code, device, on = _first_matrix(out, "out", stream)
-    vector = shape[1:]
-    args = _Join(shape[0], shape[1], code, kind, eps, *_matrix(branch, "branch", shape, dtype, device), *_matrix(gate, "gate", shape, dtype, device),
-                 None, 0, *_matrix(out, "out", shape, dtype, device), None, 0, _vector(post_weight, "post_weight", vector, device),
-                 _vector(scale, "scale", vector, device), _vector(pre_weight, "pre_weight", vector, device),
-                 *_matrix(d_out, "d_out", shape, dtype, device), *_matrix(d_normed, "d_normed", shape, dtype, device),
-                 *_matrix(d_branch, "d_branch", shape, dtype, device), *_matrix(d_gate, "d_gate", shape, dtype, device),
-                 *_matrix(d_resid, "d_resid", shape, dtype, device), _vector(d_post_weight, "d_post_weight", vector, device),
-                 _vector(d_scale, "d_scale", vector, device), _vector(d_pre_weight, "d_pre_weight", vector, device))
-    if d_post_weight is not None or d_scale is not None or d_pre_weight is not None:
-        workspace = _workspace(workspace, lib.bagel_block_join_workspace(shape[0], shape[1]), device, stream)
-        args.workspace, args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(out, "out", device)
+    sums = d_post_weight is not None or d_scale is not None or d_pre_weight is not None
+    workspace, space = _workspace(workspace, lib.bagel_block_join_workspace(rows, width) if sums else 0, device, stream)
+    args = (_JOIN_HEAD.pack(rows, width, code, kind, eps) + _marshal.matrices(out, _FORWARD, (branch, gate, None, out, None)) +
+            _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) +
+            _marshal.matrices(out, _BACKWARD, (d_out, d_normed, d_branch, d_gate, d_resid)) +
+            _marshal.vectors(device, (width,), _D_VECTORS, (d_post_weight, d_scale, d_pre_weight)) + space)
     _done(lib, lib.bagel_block_join_grad(args, on))
 
 
@@ -363,7 +319,7 @@ def bagel_recurrence_workspace(rows: int, width: int) -> int:
 def _sequences(offsets, device):
     """(number of sequences, pointer of their offsets): an int32 tensor on the GPU, or the number of sequences of equal length."""
     if not isinstance(offsets, _torch.Tensor):
-        return int(offsets), None
+        return int(offsets), 0
     if offsets.dtype != _torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
         raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
     return offsets.numel() - 1, offsets.data_ptr()
@@ -378,17 +334,14 @@ def _needed(t, name):
 def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None, final=None, carry=None, workspace=None, stream=None):
     """h_t = h_{t-1} + q_t (value_t - h_{t-1}), q_t = 1 / (1 + exp(forget_t + bias)), along packed sequences (see include/bagel.h)."""
     lib = _load()
-    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
-    rows, width = shape
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
-    state = (n, width)
-    workspace = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = _Recurrence(rows, width, code, n, at, *_matrix(value, "value", shape, dtype, device),
-                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device),
-                       *_matrix(_needed(hidden, "hidden"), "hidden", shape, dtype, device), _vector(bias, "bias", shape[1:], device),
-                       _vector(initial, "initial", state, device), _vector(final, "final", state, device),
-                       _vector(carry, "carry", (lib.bagel_recurrence_carry_rows(rows), width), device) if carry is not None else None, None,
-                       None, 0, None, 0, None, 0, None, None, None, workspace.data_ptr(), workspace.numel())
+    workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
+    args = (_RECURRENCE_HEAD.pack(rows, width, code, n, at) +
+            _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), _needed(hidden, "hidden"))) +
+            _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, final)) +
+            _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (carry,)) + bytes(8 + 3 * 16 + 3 * 8) + space)
     _done(lib, lib.bagel_recurrence(args, on))
 
 
@@ -396,29 +349,29 @@ def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, c
                           d_bias=None, workspace=None, stream=None):
     """The gradient of bagel_recurrence, with the `carry` it wrote (see include/bagel.h)."""
     lib = _load()
-    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
-    rows, width = shape
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
-    state = (n, width)
-    workspace = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = _Recurrence(rows, width, code, n, at, *_matrix(value, "value", shape, dtype, device),
-                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device), None, 0, _vector(bias, "bias", shape[1:], device),
-                       _vector(initial, "initial", state, device), None,
-                       _vector(_needed(carry, "carry"), "carry", (lib.bagel_recurrence_carry_rows(rows), width), device), None,
-                       *_matrix(_needed(d_hidden, "d_hidden"), "d_hidden", shape, dtype, device), *_matrix(d_value, "d_value", shape, dtype, device),
-                       *_matrix(d_forget, "d_forget", shape, dtype, device), _vector(d_final, "d_final", state, device),
-                       _vector(d_initial, "d_initial", state, device), _vector(d_bias, "d_bias", shape[1:], device),
-                       workspace.data_ptr(), workspace.numel())
+    workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
+    args = (_RECURRENCE_HEAD.pack(rows, width, code, n, at) +
+            _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), None)) +
+            _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, None)) +
+            _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (_needed(carry, "carry"),)) + bytes(8) +
+            _marshal.matrices(value, ("d_hidden", "d_value", "d_forget"), (_needed(d_hidden, "d_hidden"), d_value, d_forget)) +
+            _marshal.vectors(device, (n, width), ("d_final", "d_initial"), (d_final, d_initial)) +
+            _marshal.vectors(device, (width,), ("d_bias",), (d_bias,)) + space)
     _done(lib, lib.bagel_recurrence_grad(args, on))
 
 
 def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, stream=None):
     """One step of as many sequences as there are rows, the float32 state updated in place (see include/bagel.h)."""
     lib = _load()
-    shape, dtype, code, device, on = _first_matrix(value, "value", stream)
-    args = _Recurrence(0, shape[1], code, shape[0], None, *_matrix(value, "value", shape, dtype, device),
-                       *_matrix(_needed(forget, "forget"), "forget", shape, dtype, device), *_matrix(hidden, "hidden", shape, dtype, device),
-                       _vector(bias, "bias", shape[1:], device), None, None, None, _vector(_needed(state, "state"), "state", shape, device))
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(value, "value", device)
+    args = (_RECURRENCE_HEAD.pack(0, width, code, rows, 0) +
+            _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), hidden)) +
+            _marshal.vectors(device, (width,), ("bias",), (bias,)) + bytes(3 * 8) +
+            _marshal.vectors(device, (rows, width), ("state",), (_needed(state, "state"),)) + _NOTHING)
     _done(lib, lib.bagel_recurrence_step(args, on))
 
 
@@ -430,47 +383,15 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
     type, and so are the entries of copy.  m and v are float32, or float8_e4m3fn with m_scale and v_scale, lists of float32 tensors
     with an entry for every ADAMW_BLOCK values.  weight_decay: a number, or one for every tensor."""
     lib = _load()
-    n = len(params)
-    eight = n > 0 and len(m) > 0 and m[0].dtype is _torch.float8_e4m3fn
-    decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
-    lists = [params, grads, m, v, decay] + ([copy] if copy is not None else []) + ([m_scale, v_scale] if eight else [])
-    if any(x is None or len(x) != n for x in lists):
-        raise ValueError("the lists of one update must have an entry for every tensor (moments in 8 bits need m_scale and v_scale)")
     on, device = _stream(stream)
-    f32, grad_type = _torch.float32, grads[0].dtype if n else None
-    state = _torch.float8_e4m3fn if eight else f32
-    scale = None
+    n, table, grad_type, copy_type, bits = _marshal.adamw(device, params, grads, m, v, m_scale, v_scale, copy, weight_decay)
+    scale = 0
     if grad_scale is not None:
-        scale = _ptr(grad_scale, grad_scale.shape, "grad_scale")
-        if grad_scale.numel() != 1 or grad_scale.get_device() != device:
-            raise ValueError("grad_scale must hold one value and be on the current GPU")
-    options = _AdamW(int(step), lr, beta1, beta2, eps, scale, _dtype_code(grads[0], "grads") if n else 0,
-                     _dtype_code(copy[0], "copy") if n and copy is not None else 0, 8 if eight else 32, int(seed) & 0xFFFFFFFF)
-    table = []
-    for i in range(n):
-        p, g, mi, vi = params[i], grads[i], m[i], v[i]
-        shape = p.shape
-        if not (p.dtype is f32 and g.dtype is grad_type and mi.dtype is state and vi.dtype is state and g.shape == shape and mi.shape == shape and
-                vi.shape == shape and p.is_contiguous() and g.is_contiguous() and mi.is_contiguous() and vi.is_contiguous() and
-                p.get_device() == g.get_device() == mi.get_device() == vi.get_device() == device):
-            raise ValueError(f"tensor {i} of an update: contiguous tensors of shape {tuple(shape)} on cuda:{device} are needed, a float32 parameter, a "
-                             f"{grad_type} gradient and {state} moments, not " + ", ".join(f"{x.dtype} of {tuple(x.shape)} on {x.device}"
-                                                                                           for x in (p, g, mi, vi)))
-        count = p.numel()
-        ms = vs = ci = 0
-        if eight:
-            ms, vs, blocks = m_scale[i], v_scale[i], -(-count // ADAMW_BLOCK)
-            if not (ms.dtype is f32 and vs.dtype is f32 and ms.numel() == vs.numel() == blocks and ms.is_contiguous() and vs.is_contiguous() and
-                    ms.get_device() == vs.get_device() == device):
-                raise ValueError(f"tensor {i} of an update: m_scale and v_scale must be contiguous float32 tensors of {blocks} values on cuda:{device}")
-            ms, vs = ms.data_ptr(), vs.data_ptr()
-        if copy is not None:
-            c = copy[i]
-            if c.dtype is not copy[0].dtype or c.shape != shape or not c.is_contiguous() or c.get_device() != device:
-                raise ValueError(f"copy {i} of an update: a contiguous {copy[0].dtype} tensor of shape {tuple(shape)} on cuda:{device} is needed")
-            ci = c.data_ptr()
-        table += (p.data_ptr(), g.data_ptr(), mi.data_ptr(), vi.data_ptr(), ms, vs, ci, count, decay[i])
-    _done(lib, lib.bagel_adamw_step(struct.pack(_ADAMW_TENSOR * n, *table), n, options, on))
+        if not isinstance(grad_scale, _torch.Tensor) or grad_scale.numel() != 1 or grad_scale.dtype != _torch.float32 or grad_scale.get_device() != device:
+            raise ValueError("grad_scale must hold one float32 value and be on the current GPU")
+        scale = grad_scale.data_ptr()
+    options = _ADAMW_OPTIONS.pack(int(step), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, int(seed) & 0xFFFFFFFF)
+    _done(lib, lib.bagel_adamw_step(table, n, options, on))
 
 
 class Bagel:

@@ -1,4 +1,5 @@
-"""Build libbagel.so (HIP, gfx950) in-tree with hipcc.  ``python -m paper_2202_13638_amd.build``."""
+"""Build libbagel.so (HIP, gfx950) in-tree with hipcc, and _marshal.so (the binding's checks of torch tensors) with g++.
+``python -m paper_2202_13638_amd.build``."""
 from __future__ import annotations
 
 import concurrent.futures as cf
@@ -11,6 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbagel.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["adamw.hip", "backward.hip", "bagel_api.hip", "block_join.hip", "gp_step.hip", "lane.hip", "model.hip", "policy.hip", "policy16.hip", "posterior.hip", "prepare.hip", "recurrence.hip", "rollout.hip"]
 # -packed-fp32-ops is switched off on purpose: no packed float32 VALU instructions in this library
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
@@ -35,10 +37,29 @@ def _compile(src: str, force: bool) -> str:
     return obj
 
 
+def _marshal(force: bool) -> None:
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    path, header = os.path.join(CSRC, "marshal.cpp"), os.path.join(ROOT, "include", "bagel.h")
+    if not force and os.path.exists(MARSHAL) and all(os.path.getmtime(MARSHAL) >= os.path.getmtime(d) for d in (path, header, __file__)):
+        return
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_path("include"),
+           *(f for d in cpp_extension.include_paths() if "torch" in d for f in ("-isystem", d)), path, "-o", MARSHAL,
+           "-L", lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for marshal.cpp:\n{r.stdout}\n{r.stderr}")
+
+
 def build(force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=6) as ex:
+        marshal = ex.submit(_marshal, force)
         objs = list(ex.map(lambda s: _compile(s, force), SOURCES))
+        marshal.result()
     if force or not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
         cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
         subprocess.run(cmd, check=True)

@@ -634,7 +634,7 @@ template <typename T, int V, int S, bool GRAD> void launch_spans(recurrence_args
         nothing_kernel<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, stream>>>(a.published, cells, a.counter);
     }
     if constexpr (GRAD) {
-        a.bias_sums = r.d_bias ? (float *)((char *)r.workspace + cells * 8 + 16) : nullptr;
+        a.bias_sums = !r.d_bias ? nullptr : a.spans == 1 ? r.d_bias : (float *)((char *)r.workspace + cells * 8 + 16);
         recurrence_grad_kernel<T, V, S><<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
     } else {
         recurrence_kernel<T, V, S><<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
@@ -648,7 +648,7 @@ template <typename T, bool GRAD> hipError_t launch_pass(const bagel_gated_recurr
     recurrence_args<T> a = args_of<T>(r, GRAD);
     if (sizeof(T) == 2 && r.width > 1) launch_spans<T, 4 / sizeof(T), 16, GRAD>(a, r, stream);
     else launch_spans<T, 1, 16, GRAD>(a, r, stream);
-    if (GRAD && r.d_bias) bias_kernel<<<(r.width + 15) / 16, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
+    if (GRAD && r.d_bias && a.spans != 1) bias_kernel<<<(r.width + 15) / 16, 1024, 0, stream>>>(a.bias_sums, a.spans, r.width, r.d_bias);
     return hipGetLastError();
 }
 
