@@ -65,49 +65,82 @@ __global__ __launch_bounds__(256) void nothing_kernel(uint64_t *published, int64
 }
 
 // The state before span number `order` (in the order in which they depend on each other; `spans` is where that of number 0 is, and the next `step`
-// cells on).  Spans are in blocks of BLOCK: the last of a block publishes the state behind it, CLOSED, and the others what they are
-// themselves.  So the state before a span is that before its block, taken through the spans of the block before it, in groups of GROUP for each
-// wave: always the same operations, whoever was fast, and one wait for another's state in BLOCK spans.
-constexpr int GROUP = 4, BLOCK = GROUP * WAVES;
+// cells on).  Spans are in blocks of SPANS.  A span publishes what it is itself, but the last of a block the state behind it, CLOSED.  So the state
+// before a span is that before its block, taken through the spans of the block before it: always the same operations, whoever was
+// fast, and one wait for another's state in 32 spans, GROUP for each wave.
+//   With few channels that chain of states is what a long sequence takes.  Then (DEEP) half of the waves look at spans and half at whole blocks, 16 spans
+// to a block and 16 blocks to a state: the last span of a block publishes what its block is, which it knows from the spans before it.
+constexpr int GROUP = 4;
+template <bool DEEP> struct blocks_of {
+    static constexpr int waves = DEEP ? WAVES / 2 : 0;           // that look at blocks
+    static constexpr int spans = GROUP * (WAVES - waves), large = DEEP ? spans * GROUP * waves : spans;
+    static __device__ __forceinline__ bool ends(int order) { return order % spans == spans - 1; }
+    static __device__ __forceinline__ bool ends_large(int order) { return order % large == large - 1; }
+};
 
-__device__ __forceinline__ bool publishes_state(int order) { return order % BLOCK == BLOCK - 1; }
-
-template <int V>
-__device__ __forceinline__ void look_back(const uint64_t *spans, int64_t step, int order, int wave, piece (*seen)[64][V], float (&h)[V])
+// `all`, in wave 0, is the span itself, and `to` where it publishes (null: a lane that does not).
+template <int V, bool DEEP>
+__device__ __forceinline__ void look_back(const uint64_t *spans, int64_t step, int order, int wave, const piece (&all)[V], uint64_t *to,
+                                          piece (*seen)[64][V], float (&h)[V])
 {
-    const int lane = threadIdx.x & 63, block = order / BLOCK * BLOCK, first = block + wave * GROUP, count = min(order - first, GROUP);
+    using in = blocks_of<DEEP>;
+    const int lane = threadIdx.x & 63, large = order / in::large * in::large, block = order / in::spans * in::spans;
+    const bool blocks = wave < in::waves;
+    const int every = blocks ? in::spans : 1, first = (blocks ? wave : wave - in::waves) * GROUP;
+    const int count = min((blocks ? (block - large) / in::spans : order - block) - first, GROUP);
+    const int from = blocks ? large + (first + 1) * in::spans - 1 : block + first;
     uint64_t word[GROUP + 1][V];
 #pragma unroll
     for (int k = 0; k < GROUP; ++k)
         if (k < count)
 #pragma unroll
-            for (int v = 0; v < V; ++v) word[k][v] = look(spans + (first + k) * step + v);
-    const bool state = wave == 0 && block > 0;
+            for (int v = 0; v < V; ++v) word[k][v] = look(spans + (from + k * every) * step + v);
+    const bool state = wave == 0 && large > 0;
     if (state)
 #pragma unroll
-        for (int v = 0; v < V; ++v) word[GROUP][v] = look(spans + (block - 1) * step + v);
+        for (int v = 0; v < V; ++v) word[GROUP][v] = look(spans + (large - 1) * step + v);
+    const auto wait = [&] {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        piece p = {1.0f, 0.0f};
-        if (state) {
-            while ((float)__uint_as_float((uint32_t)word[GROUP][v]) != CLOSED) word[GROUP][v] = look(spans + (block - 1) * step + v);
-            p.H = __uint_as_float((uint32_t)(word[GROUP][v] >> 32));
-        }
-#pragma unroll
-        for (int k = 0; k < GROUP; ++k)
-            if (k < count) {
-                while ((uint32_t)word[k][v] == NOTHING) word[k][v] = look(spans + (first + k) * step + v);
-                p = joined(p, {__uint_as_float((uint32_t)word[k][v]), __uint_as_float((uint32_t)(word[k][v] >> 32))});
+        for (int v = 0; v < V; ++v) {
+            piece p = {1.0f, 0.0f};
+            if (state) {
+                while (__uint_as_float((uint32_t)word[GROUP][v]) != CLOSED) word[GROUP][v] = look(spans + (large - 1) * step + v);
+                p.H = __uint_as_float((uint32_t)(word[GROUP][v] >> 32));
             }
-        seen[wave][lane][v] = p;
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k)
+                if (k < count) {
+                    while ((uint32_t)word[k][v] == NOTHING) word[k][v] = look(spans + (from + k * every) * step + v);
+                    p = joined(p, {__uint_as_float((uint32_t)word[k][v]), __uint_as_float((uint32_t)(word[k][v] >> 32))});
+                }
+            seen[wave][lane][v] = p;
+        }
+    };
+    if constexpr (DEEP) {
+        if (!blocks) wait();
+        __syncthreads();
+        if (in::ends(order) && !in::ends_large(order) && to)     // before it waits for any other block
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                piece p = seen[in::waves][lane][v];
+#pragma unroll
+                for (int k = in::waves + 1; k < WAVES; ++k) p = joined(p, seen[k][lane][v]);
+                publish(to + v, joined(p, all[v]));
+            }
+        if (blocks) wait();
+    } else {
+        wait();
     }
     __syncthreads();
-    const int waves = min((order - block + GROUP - 1) / GROUP, WAVES);
+    const int waves = DEEP ? WAVES : min((order - block + GROUP - 1) / GROUP, WAVES);
 #pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = seen[0][lane][v].H;       // the state before the block is in it
+    for (int v = 0; v < V; ++v) h[v] = seen[0][lane][v].H;       // the state before the large block is in it
     for (int k = 1; k < waves; ++k)
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = through(seen[k][lane][v], h[v]);
+    if (in::ends_large(order) && to)
+#pragma unroll
+        for (int v = 0; v < V; ++v) publish(to + v, {CLOSED, through(all[v], h[v])});
 }
 
 // The rows t0 to t0 + S - 1 of a wave: which of them begin a sequence (bit i of `starts` for t0 + i, bit S for the row behind them; the end of the
@@ -299,7 +332,8 @@ template <typename A> __device__ __forceinline__ void pass_through(const A &a, i
             for (int ch = threadIdx.x & 63; ch < a.width; ch += 64) to[(int64_t)s * a.width + ch] = at(from, (int64_t)s * a.width + ch);
 }
 
-template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(recurrence_args<T> a)
+template <typename T, int V, int S, bool DEEP>
+__global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 8 : 4) void recurrence_kernel(recurrence_args<T> a)
 {
     __shared__ piece pieces[WAVES][64][V], seen[WAVES][64][V];
     const int work = next_work(a.counter);
@@ -347,8 +381,7 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = 0.0f;
     if (a.spans > 1) {
-        const bool writes = w.wave == 0 && w.here;
-        uint64_t *to = a.published + (int64_t)w.span * a.width + w.ch;
+        uint64_t *to = w.wave == 0 && w.here ? a.published + (int64_t)w.span * a.width + w.ch : nullptr;
         piece all[V];
         if (w.wave == 0)
 #pragma unroll
@@ -357,13 +390,10 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
                 for (int k = 1; k < WAVES; ++k) all[v] = joined(all[v], pieces[k][w.lane][v]);
             }
-        if (writes && !publishes_state(w.span))
+        if (to && !blocks_of<DEEP>::ends(w.span))
 #pragma unroll
             for (int v = 0; v < V; ++v) publish(to + v, all[v]);
-        if (w.span > 0) look_back<V>(a.published + w.ch, a.width, w.span, w.wave, seen, h);
-        if (writes && publishes_state(w.span))
-#pragma unroll
-            for (int v = 0; v < V; ++v) publish(to + v, {CLOSED, through(all[v], h[v])});
+        if (w.span > 0) look_back<V, DEEP>(a.published + w.ch, a.width, w.span, w.wave, all, to, seen, h);
     }
     for (int k = 0; k < w.wave; ++k)
 #pragma unroll
@@ -393,7 +423,8 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
     });
 }
 
-template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_grad_kernel(recurrence_args<T> a)
+template <typename T, int V, int S, bool DEEP>
+__global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence_grad_kernel(recurrence_args<T> a)
 {
     static_assert(S * WAVES == SPAN, "a span begins with a row of the carry");
     __shared__ piece pieces[WAVES][64][V], back[WAVES][64][V], seen[WAVES][64][V];
@@ -473,9 +504,8 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
     for (int v = 0; v < V; ++v) c[v] = sum[v] = 0.0f;
     if (a.spans > 1) {
-        const bool writes = w.wave == 0 && w.here;
         const int order = a.spans - 1 - w.span;
-        uint64_t *to = a.published + (int64_t)order * a.width + w.ch;
+        uint64_t *to = w.wave == 0 && w.here ? a.published + (int64_t)order * a.width + w.ch : nullptr;
         piece all[V];
         if (w.wave == 0)
 #pragma unroll
@@ -484,13 +514,10 @@ template <typename T, int V, int S> __global__ __launch_bounds__(64 * WAVES, 4) 
 #pragma unroll
                 for (int k = WAVES - 2; k >= 0; --k) all[v] = joined(all[v], back[k][w.lane][v]);
             }
-        if (writes && !publishes_state(order))
+        if (to && !blocks_of<DEEP>::ends(order))
 #pragma unroll
             for (int v = 0; v < V; ++v) publish(to + v, all[v]);
-        if (order > 0) look_back<V>(a.published + w.ch, a.width, order, w.wave, seen, c);
-        if (writes && publishes_state(order))
-#pragma unroll
-            for (int v = 0; v < V; ++v) publish(to + v, {CLOSED, through(all[v], c[v])});
+        if (order > 0) look_back<V, DEEP>(a.published + w.ch, a.width, order, w.wave, all, to, seen, c);
     }
     // h before every row, less its value
     float hx[S][V];
@@ -636,11 +663,15 @@ template <typename T, int V, int S, bool GRAD> void launch_spans(recurrence_args
         const int64_t groups = (cells + 255) / 256;
         nothing_kernel<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, stream>>>(a.published, cells, a.counter);
     }
+    // Blocks of blocks where there are few groups of channels to hide the chain of states behind, and more than one state.  131072 rows in bf16, forward and
+    // back, us, without and with: 64 channels 75 / 87 and 41 / 53, 256 85 / 114 and 71 / 109, 512 126 / 178 and 124 / 179, 1024 212 / 303 and
+    // 217 / 308; 64 channels of 3000 rows 12.3 / 20.8 and 12.9 / 21.9, of 9000 14.9 / 24.2 and 13.9 / 23.8.
+    const bool deep = a.groups <= 4 && a.spans > blocks_of<false>::spans;
     if constexpr (GRAD) {
         a.bias_sums = !r.d_bias ? nullptr : a.spans == 1 ? r.d_bias : (float *)((char *)r.workspace + cells * 8 + 16);
-        recurrence_grad_kernel<T, V, S><<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
+        (deep ? recurrence_grad_kernel<T, V, S, true> : recurrence_grad_kernel<T, V, S, false>)<<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
     } else {
-        recurrence_kernel<T, V, S><<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
+        (deep ? recurrence_kernel<T, V, S, true> : recurrence_kernel<T, V, S, false>)<<<(unsigned)work, 64 * WAVES, 0, stream>>>(a);
     }
 }
 

@@ -353,6 +353,20 @@ def test_recurrence_over_many_spans_gives_the_same_bits_every_time(width):
 
 
 @gpu
+@pytest.mark.parametrize("rows, width, dtype", [(14100, 600, "bf16"), (14100, 300, "f32"), (70000, 33, "bf16"), (70000, 3, "f32"), (4096, 70, "f16"), (4097, 70, "f16")])
+def test_recurrence_over_blocks_of_spans(rows, width, dtype):
+    """Few channels and many, over more than two of the largest blocks of spans, and at the rows from which blocks of blocks are used."""
+    at = [0, 2000, 2000, rows - 7, rows]
+    x, f, dh = (_normal((rows, width), i, TYPES[dtype]).cuda() for i in (1, 2, 3))
+    bias, h0, dl = _normal((width,), 4, mean=5.0).cuda(), _normal((4, width), 5).cuda(), _normal((4, width), 6).cuda()
+    got, again = (_run_recurrence(x, f, at, bias, h0, dh, dl) for _ in range(2))
+    want, terms = _recurrence_ref(*(t.cpu() for t in (x, f)), at, *(t.cpu() for t in (bias, h0, dh, dl)))
+    for k, v in want.items():
+        assert torch.equal(got[k], again[k]), k
+        _near(got[k], v, k, terms=terms if k == "d_bias" else None)
+
+
+@gpu
 @pytest.mark.parametrize("count", [62, 63, 64, 65, 700, 5000])
 def test_recurrence_of_many_short_sequences(count):
     """Numbers of sequences at which the search for a row's sequence takes one look, two and three; a third of them are empty."""
