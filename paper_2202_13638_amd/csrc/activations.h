@@ -64,14 +64,20 @@ template <int MOVE> __device__ __forceinline__ float bagel_moved(float v)
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), MOVE, 0xF, 0xF, false));
 }
 
-// The sum over the 64 lanes of a wave, the same in all of them.
-__device__ __forceinline__ float bagel_wave_sum(float v)
+// The sum over 16 lanes, the same in all of them.
+__device__ __forceinline__ float bagel_sum_of_16(float v)
 {
     v += bagel_moved<0xB1>(v);
     v += bagel_moved<0x4E>(v);
     v += bagel_moved<0x141>(v);
     v += bagel_moved<0x140>(v);
-    const int i = __float_as_int(v);
+    return v;
+}
+
+// and over the 64 lanes of a wave.
+__device__ __forceinline__ float bagel_wave_sum(float v)
+{
+    const int i = __float_as_int(bagel_sum_of_16(v));
     return (__int_as_float(__builtin_amdgcn_readlane(i, 0)) + __int_as_float(__builtin_amdgcn_readlane(i, 16))) +
            (__int_as_float(__builtin_amdgcn_readlane(i, 32)) + __int_as_float(__builtin_amdgcn_readlane(i, 48)));
 }

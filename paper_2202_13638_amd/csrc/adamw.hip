@@ -197,7 +197,9 @@ template <int BITS, bool WHOLE> __device__ __forceinline__ void update_block(con
     }
 }
 
-// A wave takes a block of 256 at a time, four entries a lane: the block's largest magnitude is a matter of one wave.
+// A wave takes a block of 256 at a time, four entries a lane: the block's largest magnitude is a matter of one wave.  Every byte is read and written once, and
+// memory bounds it: 64 tensors, 33.6 million values, 32 bits, gradients and copy in bf16: 179 us, 5.3 TB/s; 404 million values in 8 bits: 1280 us, 5.1
+// TB/s.  Six small tensors take 4.1 us, latency.
 template <int BITS> __global__ __launch_bounds__(256) void adamw_kernel(adamw_args a)
 {
     const float gs = a.grad_scale ? a.grad_scale[0] : 1.0f;
@@ -257,10 +259,11 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
     a.rate = (float)(o->lr / (1.0 - pow(o->beta1, (double)o->step)));
     a.root = (float)(1.0 / sqrt(1.0 - pow(o->beta2, (double)o->step)));
     a.eps = (float)o->eps;
-    // Few blocks are spread over as many waves as there are; of many, a wave takes four one after the other.
+    // A block to a wave, and in 8 bits four one after the other where there are many, whose scales then come together (one tensor, us with one and with four: in
+    // 8 bits 4096 blocks 7.6 and 8.9, 65536 58 and 51, 1048576 882 and 836; in 32 bits 65536 67.6 and 70.3, 1048576 1334 and 1411).
     int64_t all = 0;
     for (int i = 0; i < n_tensors; ++i) all += (tensors[i].count + BLOCK - 1) / BLOCK;
-    a.each = all < 16384 ? 1 : 4;
+    a.each = o->state_bits == 32 || all < 16384 ? 1 : 4;
     a.n = 0;
     a.pieces = 0;
     const auto launch = [&]() {

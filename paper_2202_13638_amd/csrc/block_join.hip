@@ -6,6 +6,10 @@
 //   dx = d_out + ro e - out ro^3 m(e out)              (= d_resid)
 //   k = dx c a w;  dz = rz k - z rz^3 m(k z);  dg = dx c w n a'(g)
 //   dw = sum_rows dx c a n,  dc = sum_rows dx a w n,  du = sum_rows d_normed out ro
+//
+// Memory bounds both: 10 operations or so an entry and 5 or 8 entries moved.  So a row is read once and held in registers until it is written, and
+// what is summed over it goes from lane to lane (and from wave to wave through shared memory where a row takes several).  All sums are
+// in 32 bits; `out` and `normed` are rounded once, each from the unrounded sum, and the way back starts from the stored `out`.
 #include "activations.h"
 
 namespace {
@@ -36,10 +40,10 @@ __device__ __forceinline__ float act(int kind, float g, float &slope)
 
 // Sums of N values over the WAVES waves that share a row, in a fixed order.  Two buffers take turns (`turn`), so that one barrier is enough: a
 // wave that is ahead writes the other one, and cannot come back to this one before all have read it.
-template <int WAVES, int N> __device__ __forceinline__ void row_sum(float (&v)[N], float (*shared)[WAVES][4], int &turn)
+template <int WAVES, int N, int LANES = 64> __device__ __forceinline__ void row_sum(float (&v)[N], float (*shared)[WAVES][4], int &turn)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = bagel_wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = LANES == 16 ? bagel_sum_of_16(v[i]) : bagel_wave_sum(v[i]);
     if constexpr (WAVES > 1) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0)
@@ -56,16 +60,17 @@ template <int WAVES, int N> __device__ __forceinline__ void row_sum(float (&v)[N
     }
 }
 
-// A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i.  One wave to a row leaves four rows to a
-// workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end of the row is moved back to end there:
+// A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i, or (LANES = 16) by a quarter of a wave.  One
+// wave or less to a row leaves several rows to a workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end of the row is moved back to end there:
 // its first entries are another pack's, and count as zero here.
-template <int V, int K, int WAVES> struct tile {
-    static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, rows = WAVES == 1 ? 4 : 1;
-    __device__ static __forceinline__ int place(int k) { return V * (64 * WAVES * k + (WAVES == 1 ? threadIdx.x & 63 : threadIdx.x)); }
+template <int V, int K, int WAVES, int LANES = 64> struct tile {
+    static_assert(LANES == 64 || (LANES == 16 && WAVES == 1), "a row has whole waves, or 16 lanes of one");
+    static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, lanes = LANES * WAVES, rows = WAVES == 1 ? 256 / LANES : 1;
+    __device__ static __forceinline__ int place(int k) { return V * (lanes * k + (int)threadIdx.x % lanes); }
     __device__ static __forceinline__ bool here(int k, int width) { return place(k) < width; }
     __device__ static __forceinline__ int column(int k, int width) { return min(place(k), width - V); }
     __device__ static __forceinline__ int twice(int k, int width) { return max(place(k) + V - width, 0); }    // entries that are another pack's
-    __device__ static __forceinline__ int64_t first_row() { return WAVES == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x; }
+    __device__ static __forceinline__ int64_t first_row() { return WAVES == 1 ? (int64_t)blockIdx.x * rows + threadIdx.x / LANES : blockIdx.x; }
     __device__ static __forceinline__ int64_t next_row() { return (int64_t)gridDim.x * rows; }
     // vectors of the row's width, ones where there is none
     __device__ static __forceinline__ void vector(const float *p, int width, float (&v)[K][V])
@@ -139,10 +144,12 @@ template <int V, int K, int WAVES> struct tile {
     }
 };
 
-template <typename T, int V, int K, int WAVES, bool GATED>
-__global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join_args<T> a)
+// Forward: reads branch, gate and resid, writes out and normed.  The next row waits for this one's end, and other rows of the same compute unit fill the time:
+// 64000 x 1024 bf16 124 us, 5.3 TB/s (a copy of this size reaches 5.1); 64000 x 512 f32 120 us, 5.4 TB/s; 16 x 512 3.8 us, all of it latency.
+template <typename T, int V, int K, int WAVES, int LANES, bool GATED>
+__global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void join_kernel(join_args<T> a)
 {
-    using tl = tile<V, K, WAVES>;
+    using tl = tile<V, K, WAVES, LANES>;
     __shared__ float shared[2][WAVES][4];
     int turn = 0;
     const float per = 1.0f / a.width;
@@ -171,7 +178,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join
             for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int i = 0; i < V; ++i) s[0] += z[k][i] * z[k][i];
-            row_sum<WAVES>(s, shared, turn);
+            row_sum<WAVES, sizeof(s) / 4, LANES>(s, shared, turn);
             const float rz = 1.0f / sqrtf(s[0] * per + a.eps);
 #pragma unroll
             for (int k = 0; k < K; ++k)
@@ -189,7 +196,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) s[0] += v[k][i] * v[k][i];
-        row_sum<WAVES>(s, shared, turn);
+        row_sum<WAVES, sizeof(s) / 4, LANES>(s, shared, turn);
         const float ro = 1.0f / sqrtf(s[0] * per + a.eps);
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -199,10 +206,13 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads)) void join_kernel(join
     }
 }
 
-template <typename T, int V, int K, int WAVES, bool GATED, int ON_SIMD>
-__global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_grad_kernel(join_args<T> a)
+// Back: reads five rows and writes three.  A workgroup keeps its sums for the vectors' gradients in registers over all its rows, so there are few of them, and
+// the next row is asked for before this one's sums (without: 65536 x 4096 bf16 1490 us).  That is 830 to 845 us, 5.1 TB/s; 64000 x 1024 bf16 212 us,
+// 4.9 TB/s; 9973 x 777 f32 56 us with the sums over the workgroups, 4.4 TB/s, a quarter of whose lanes have nothing.
+template <typename T, int V, int K, int WAVES, int LANES, bool GATED, int ON_SIMD>
+__global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void join_grad_kernel(join_args<T> a)
 {
-    using tl = tile<V, K, WAVES>;
+    using tl = tile<V, K, WAVES, LANES>;
     __shared__ float shared[2][WAVES][4];
     int turn = 0;
     const float per = 1.0f / a.width;
@@ -246,7 +256,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_gr
         p.o.keep();
         p.y.keep();
         p.z.keep();
-        row_sum<WAVES>(s, shared, turn);
+        row_sum<WAVES, sizeof(s) / 4, LANES>(s, shared, turn);
         const float rz = 1.0f / sqrtf(s[0] * per + a.eps), ro = 1.0f / sqrtf(s[1] * per + a.eps);
         const float co = s[2] * per * ro * ro;
         float t[1] = {0.0f}, dn[K][V];                               // dn: gradient of R(branch)
@@ -271,7 +281,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_gr
         }
         p.z.keep();
         if (!a.d_branch.data) continue;
-        row_sum<WAVES>(t, shared, turn);
+        row_sum<WAVES, 1, LANES>(t, shared, turn);
         const float cz = t[0] * per * rz;
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -281,17 +291,17 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_gr
     }
     if (!a.sums) return;
     float *sums = a.sums + (size_t)blockIdx.x * 2 * a.width;
-    if constexpr (WAVES == 1) {              // four waves with sums of the same columns: added up in order
-        __shared__ float all[2][64 * K * V];
-        for (int wave = 0; wave < 4; ++wave) {
-            if ((int)(threadIdx.x >> 6) == wave)
+    if constexpr (WAVES == 1) {              // several rows' lanes with sums of the same columns: added up in order
+        __shared__ float all[2][LANES * K * V];
+        for (int row = 0; row < tl::rows; ++row) {
+            if ((int)threadIdx.x / LANES == row)
 #pragma unroll
                 for (int k = 0; k < K; ++k)
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const int j = tl::place(k) + i;
-                        all[0][j] = wave ? all[0][j] + sw[k][i] : sw[k][i];
-                        all[1][j] = wave ? all[1][j] + su[k][i] : su[k][i];
+                        all[0][j] = row ? all[0][j] + sw[k][i] : sw[k][i];
+                        all[1][j] = row ? all[1][j] + su[k][i] : su[k][i];
                     }
             __syncthreads();
         }
@@ -316,7 +326,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES>::threads), ON_SIMD) void join_gr
 }
 
 // Rows that registers do not hold (sixteen waves leave 128 to a lane): three passes over a row, the second and third out of the cache, and the sums
-// of a workgroup in its part of the work space.
+// of a workgroup in its part of the work space.  8192 x 16384 f32 997 us, 4.3 TB/s of what has to be moved.
 template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void join_grad_wide_kernel(join_args<T> a)
 {
     __shared__ float shared[2][16][4];
@@ -408,7 +418,8 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
     }
 }
 
-// The gradients of the vectors: sums over the workgroups of the pass over the rows.  16 threads to a column, each with a part of the workgroups.
+// The gradients of the vectors: sums over the workgroups of the pass over the rows, in a fixed order.  16 threads to a column, each with a part of the
+// workgroups: 5 us for 512 of them and 1024 columns, most of it latency.
 __global__ __launch_bounds__(1024) void join_sums_kernel(const float *sums, int groups, int width, const float *post, const float *scale, float *d_post,
                                                          float *d_scale, float *d_pre)
 {
@@ -463,20 +474,22 @@ template <typename T> join_args<T> args_of(const bagel_join &j)
 }
 
 // The number of workgroups.
-template <typename T, int V, int K, int WAVES, bool GRAD = true, int ON_SIMD = 1> int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
+template <typename T, int V, int K, int WAVES, bool GRAD = true, int ON_SIMD = 1, int LANES = 64>
+int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
 {
-    constexpr int threads = tile<V, K, WAVES>::threads, rows = tile<V, K, WAVES>::rows;
+    using tl = tile<V, K, WAVES, LANES>;
+    constexpr int threads = tl::threads, rows = tl::rows;
     const int64_t full = (a.rows + rows - 1) / rows, most = grad ? most_groups(a.width) : 4096;
     const int groups = (int)(full < most ? full : most);
     const bool gated = a.act != BAGEL_ACT_NONE && a.branch.data;
     if (GRAD && grad) {
         if constexpr (GRAD) {
-            if (gated) join_grad_kernel<T, V, K, WAVES, true, ON_SIMD><<<groups, threads, 0, stream>>>(a);
-            else join_grad_kernel<T, V, K, WAVES, false, ON_SIMD><<<groups, threads, 0, stream>>>(a);
+            if (gated) join_grad_kernel<T, V, K, WAVES, LANES, true, ON_SIMD><<<groups, threads, 0, stream>>>(a);
+            else join_grad_kernel<T, V, K, WAVES, LANES, false, ON_SIMD><<<groups, threads, 0, stream>>>(a);
         }
     } else {
-        if (gated) join_kernel<T, V, K, WAVES, true><<<groups, threads, 0, stream>>>(a);
-        else join_kernel<T, V, K, WAVES, false><<<groups, threads, 0, stream>>>(a);
+        if (gated) join_kernel<T, V, K, WAVES, LANES, true><<<groups, threads, 0, stream>>>(a);
+        else join_kernel<T, V, K, WAVES, LANES, false><<<groups, threads, 0, stream>>>(a);
     }
     return groups;
 }
@@ -489,16 +502,23 @@ template <typename T, int V> int launch_wide(const join_args<T> &a, hipStream_t 
     return groups;
 }
 
-// Packs of 16 bytes, of 8 where those would leave half of a wave without any, single entries where the row is shorter than a pack.  Up to 128 packs a row
-// takes one wave (no barrier).  Above, the way back takes one pack a lane while eight waves hold the row: with the packs of the next row on their way
-// beside those of this one there is little room for more (4096 x 65536 in bf16: 979 us with two packs on four waves, 832 with one on eight); where
-// some of the eight have nothing, four waves on a SIMD at the price of a few spilled registers (2500 x 20000: 278 us, 221; 4096: 832, 891).
-// Forward, two packs on four waves and one on eight are alike up to 512.
+// Packs of 16 bytes, single entries where the row is shorter than a pack.  Figures are us, forward / back, in bf16 where no type is said.
+//   Up to 16 packs, 16 lanes to a row (200000 x 64: 35 / 69, with a wave to a row 77 / 140; 262144 x 128: 67 / 130, 105 / 193; a wave would have
+// few of its lanes at work and four times the rows to go through).
+//   Up to 32, a wave and packs of 8 bytes (262144 x 256: 134 / 226, of 16 bytes 172 / 327).
+//   Up to 128, a wave, which needs no barrier (64000 x 1024: 124 / 212, by four waves 160 / 379).
+//   Up to 256, four waves (32000 x 2048: 131 / 205, by one 140 / 290).
+//   Above, back, one pack a lane while eight waves hold the row: with the packs of the next row on their way beside those of this one there is little
+// room for more (65536 x 4096: 832, two packs on four waves 979); where some of the eight have nothing, four waves on a SIMD at the price of a few spilled
+// registers (20000 x 2500: 221, without 278; 65536 x 4096: 891, 832).  Forward two packs on four waves and one on eight are alike.
+//   Up to 1024, two packs on eight waves (16384 x 8192: 257 / 441, one on sixteen 335 / 645; 16384 x 4096 in f32 258 / 409, 246 / 417).
+//   Above, what sixteen waves can hold, and for the way back of wider rows three passes over a row.
 template <typename T> int launch_rows(const join_args<T> &a, bool grad, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(T);
     const int packs = (a.width + V - 1) / V;
     if (a.width < V) return launch_tile<T, 1, 1, 1>(a, grad, stream);
+    if (packs <= 16) return launch_tile<T, V, 1, 1, true, 1, 16>(a, grad, stream);
     if (packs <= 32) return launch_tile<T, V / 2, 1, 1>(a, grad, stream);
     if (packs <= 64) return launch_tile<T, V, 1, 1>(a, grad, stream);
     if (packs <= 128) return launch_tile<T, V, 2, 1>(a, grad, stream);

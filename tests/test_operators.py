@@ -97,6 +97,14 @@ def test_join_and_its_gradient(rows, width, dtype):
     _join_grad_case(x, g, out, d_out, d_normed, act, 1e-5)
 
 
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width", [(70001, 40), (17, 100), (15, 8), (16, 9), (33, 121), (2, 4), (20003, 64)])
+def test_join_of_short_rows(rows, width, dtype):
+    """Rows that take a part of a wave, and more of them than there are places."""
+    test_join_and_its_gradient(rows, width, dtype)
+
+
 def _join_grad_ref(x, out, d_out, d_normed, act, eps):
     """Gradients, and the sums of magnitudes of those of the vectors, from the formulas in 64 bits at the stored `out`."""
     width = out.shape[1]
