@@ -208,7 +208,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void join_kern
 
 // Back: reads five rows and writes three.  A workgroup keeps its sums for the vectors' gradients in registers over all its rows, so there are few of them, and
 // the next row is asked for before this one's sums (without: 65536 x 4096 bf16 1490 us).  That is 830 to 845 us, 5.1 TB/s; 64000 x 1024 bf16 212 us,
-// 4.9 TB/s; 9973 x 777 f32 56 us with the sums over the workgroups, 4.4 TB/s, a quarter of whose lanes have nothing.
+// 4.9 TB/s; 9973 x 777 f32 47 us, 5.3 TB/s, a quarter of whose lanes have nothing.
 template <typename T, int V, int K, int WAVES, int LANES, bool GATED, int ON_SIMD>
 __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void join_grad_kernel(join_args<T> a)
 {
@@ -419,7 +419,7 @@ template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void
 }
 
 // The gradients of the vectors: sums over the workgroups of the pass over the rows, in a fixed order.  16 threads to a column, each with a part of the
-// workgroups: 5 us for 512 of them and 1024 columns, most of it latency.
+// workgroups: 6.5 us for 512 of them and 4096 columns, 4.7 us for 777: latency.
 __global__ __launch_bounds__(1024) void join_sums_kernel(const float *sums, int groups, int width, const float *post, const float *scale, float *d_post,
                                                          float *d_scale, float *d_pre)
 {
