@@ -7,7 +7,7 @@
 //   k = dx c a w;  dz = rz k - z rz^3 m(k z);  dg = dx c w n a'(g)
 //   dw = sum_rows dx c a n,  dc = sum_rows dx a w n,  du = sum_rows d_normed out ro
 //
-// Memory bounds both: 10 operations or so an entry and 5 or 8 entries moved.  So a row is read once and held in registers until it is written, and
+// Memory bounds both, the arithmetic not far behind in 16 bits: 25 and 45 instructions an entry, and 5 and 8 entries moved.  So a row is read once and held in registers until it is written, and
 // what is summed over it goes from lane to lane (and from wave to wave through shared memory where a row takes several).  All sums are
 // in 32 bits; `out` and `normed` are rounded once, each from the unrounded sum, and the way back starts from the stored `out`.
 #include "activations.h"
@@ -24,14 +24,16 @@ template <typename T> struct join_args {
                                  // without w) and of d_normed out ro (d_pre_weight)
 };
 
-// act(g) and its derivative.  For an infinite g the logistic function is 0 or 1 exactly, and so is its derivative.
+// act(g) and its derivative.  For an infinite g the logistic function is 0 or 1 exactly, and so is its derivative.  The reciprocal is the
+// hardware's, off by one unit in the last place at most: a division takes ten instructions an entry, and in 16 bits these kernels are near the rate of the
+// arithmetic (65536 x 4096 back: 844 us with it, 807 without; 20000 x 2500 forward: 131 and 113).
 __device__ __forceinline__ float act(int kind, float g, float &slope)
 {
     if (kind == BAGEL_ACT_IDENTITY) {
         slope = 1.0f;
         return g;
     }
-    const float e = __expf(-fabsf(g)), r = 1.0f / (1.0f + e), s = e * r;         // logistic(|g|) and logistic(-|g|), both without cancellation
+    const float e = __expf(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e), s = e * r;         // logistic(|g|) and logistic(-|g|), both without cancellation
     const float sig = g < 0.0f ? s : r, rest = g < 0.0f ? r : s;
     const bool silu = kind == BAGEL_ACT_SILU;
     slope = silu ? sig + g * sig * rest : sig * rest;
@@ -145,7 +147,7 @@ template <int V, int K, int WAVES, int LANES = 64> struct tile {
 };
 
 // Forward: reads branch, gate and resid, writes out and normed.  The next row waits for this one's end, and other rows of the same compute unit fill the time:
-// 64000 x 1024 bf16 124 us, 5.3 TB/s (a copy of this size reaches 5.1); 64000 x 512 f32 120 us, 5.4 TB/s; 16 x 512 3.8 us, all of it latency.
+// 64000 x 1024 bf16 123 us, 5.3 TB/s (a copy of this size reaches 5.1); 64000 x 512 f32 120 us, 5.4 TB/s; 16 x 512 3.8 us, all of it latency.
 template <typename T, int V, int K, int WAVES, int LANES, bool GATED>
 __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void join_kernel(join_args<T> a)
 {
@@ -181,13 +183,15 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void join_kern
             row_sum<WAVES, sizeof(s) / 4, LANES>(s, shared, turn);
             const float rz = 1.0f / sqrtf(s[0] * per + a.eps);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k) {
+                if (!tl::here(k, a.width)) continue;         // a wave of which nothing is there goes by
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     float n = z[k][i] * rz, slope;
                     if (GATED) n *= act(a.act, g[k][i], slope);
                     v[k][i] += cw[k][i] * n;
                 }
+            }
         }
         if (a.out.data) tl::store(a.out.row(r), a.width, v);
         if (!a.normed.data) continue;
@@ -207,9 +211,10 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void join_kern
 }
 
 // Back: reads five rows and writes three.  A workgroup keeps its sums for the vectors' gradients in registers over all its rows, so there are few of them, and
-// the next row is asked for before this one's sums (without: 65536 x 4096 bf16 1490 us).  That is 830 to 845 us, 5.1 TB/s; 64000 x 1024 bf16 212 us,
+// the next row is asked for before this one's sums (without: 65536 x 4096 bf16 1490 us).  That is 808 us, 5.3 TB/s; 64000 x 1024 bf16 213 us,
 // 4.9 TB/s; 9973 x 777 f32 47 us, 5.3 TB/s, a quarter of whose lanes have nothing.
-template <typename T, int V, int K, int WAVES, int LANES, bool GATED, int ON_SIMD>
+// PASS: waves of which nothing is there go by the arithmetic.
+template <typename T, int V, int K, int WAVES, int LANES, bool GATED, int ON_SIMD, bool PASS>
 __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void join_grad_kernel(join_args<T> a)
 {
     using tl = tile<V, K, WAVES, LANES>;
@@ -246,13 +251,15 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void 
         if (ahead && r + tl::next_row() < a.rows) ask(r + tl::next_row());       // on its way while this row waits for its sums
         float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k) {
+            if (PASS && !tl::here(k, a.width)) continue;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 s[0] += p.z(k, i) * p.z(k, i);
                 s[1] += p.o(k, i) * p.o(k, i);
                 s[2] += p.y(k, i) * u[k][i] * p.o(k, i);
             }
+        }
         p.o.keep();
         p.y.keep();
         p.z.keep();
@@ -262,6 +269,7 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void 
         float t[1] = {0.0f}, dn[K][V];                               // dn: gradient of R(branch)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
+            if (PASS && !tl::here(k, a.width)) continue;
             float dx[V], dg[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) {
@@ -474,7 +482,7 @@ template <typename T> join_args<T> args_of(const bagel_join &j)
 }
 
 // The number of workgroups.
-template <typename T, int V, int K, int WAVES, bool GRAD = true, int ON_SIMD = 1, int LANES = 64>
+template <typename T, int V, int K, int WAVES, bool GRAD = true, int ON_SIMD = 1, int LANES = 64, bool PASS = false>
 int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
 {
     using tl = tile<V, K, WAVES, LANES>;
@@ -484,8 +492,8 @@ int launch_tile(const join_args<T> &a, bool grad, hipStream_t stream)
     const bool gated = a.act != BAGEL_ACT_NONE && a.branch.data;
     if (GRAD && grad) {
         if constexpr (GRAD) {
-            if (gated) join_grad_kernel<T, V, K, WAVES, LANES, true, ON_SIMD><<<groups, threads, 0, stream>>>(a);
-            else join_grad_kernel<T, V, K, WAVES, LANES, false, ON_SIMD><<<groups, threads, 0, stream>>>(a);
+            if (gated) join_grad_kernel<T, V, K, WAVES, LANES, true, ON_SIMD, PASS><<<groups, threads, 0, stream>>>(a);
+            else join_grad_kernel<T, V, K, WAVES, LANES, false, ON_SIMD, PASS><<<groups, threads, 0, stream>>>(a);
         }
     } else {
         if (gated) join_kernel<T, V, K, WAVES, LANES, true><<<groups, threads, 0, stream>>>(a);
@@ -509,9 +517,11 @@ template <typename T, int V> int launch_wide(const join_args<T> &a, hipStream_t 
 //   Up to 128, a wave, which needs no barrier (64000 x 1024: 124 / 212, by four waves 160 / 379).
 //   Up to 256, four waves (32000 x 2048: 131 / 205, by one 140 / 290).
 //   Above, back, one pack a lane while eight waves hold the row: with the packs of the next row on their way beside those of this one there is little
-// room for more (65536 x 4096: 832, two packs on four waves 979); where some of the eight have nothing, four waves on a SIMD at the price of a few spilled
-// registers (20000 x 2500: 221, without 278; 65536 x 4096: 891, 832).  Forward two packs on four waves and one on eight are alike.
-//   Up to 1024, two packs on eight waves (16384 x 8192: 257 / 441, one on sixteen 335 / 645; 16384 x 4096 in f32 258 / 409, 246 / 417).
+// room for more (65536 x 4096, all with a division: 832, two packs on four waves 979); where some of the eight have nothing, four waves on a SIMD at the price
+// of a few spilled registers (20000 x 2500: 221, without 278; 65536 x 4096: 891, 832), and up to 320 packs waves without any go by (16384 x 2100: 167, 184;
+// 16384 x 3001: 216, 202).  Forward two packs on four waves and one on eight are alike.
+//   Up to 1024, two packs on eight waves (16384 x 8192: 257 / 441, one on sixteen 335 / 645; 16384 x 4096 in f32 258 / 409, 246 / 417), which back up
+// to 768 go by what is not there (16384 x 4200: 297, 340; 16384 x 6000: 344, 383; 16384 x 8192: 446, 433).
 //   Above, what sixteen waves can hold, and for the way back of wider rows three passes over a row.
 template <typename T> int launch_rows(const join_args<T> &a, bool grad, hipStream_t stream)
 {
@@ -523,8 +533,10 @@ template <typename T> int launch_rows(const join_args<T> &a, bool grad, hipStrea
     if (packs <= 64) return launch_tile<T, V, 1, 1>(a, grad, stream);
     if (packs <= 128) return launch_tile<T, V, 2, 1>(a, grad, stream);
     if (packs <= 256) return launch_tile<T, V, 1, 4>(a, grad, stream);
+    if (packs <= 320 && grad) return launch_tile<T, V, 1, 8, true, 4, 64, true>(a, true, stream);
     if (packs <= 384 && grad) return launch_tile<T, V, 1, 8, true, 4>(a, true, stream);
     if (packs <= 512) return grad ? launch_tile<T, V, 1, 8>(a, true, stream) : launch_tile<T, V, 2, 4, false>(a, false, stream);
+    if (packs <= 768 && grad) return launch_tile<T, V, 2, 8, true, 1, 64, true>(a, true, stream);
     if (packs <= 1024) return launch_tile<T, V, 2, 8>(a, grad, stream);
     if (packs <= 2048 && (V == 4 || !grad)) return launch_tile<T, V, 2, 16, V == 4>(a, grad, stream);
     if (grad) return launch_wide<T, V>(a, stream);
