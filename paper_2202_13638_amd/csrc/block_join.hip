@@ -7,8 +7,8 @@
 //   k = dx c a w;  dz = rz k - z rz^3 m(k z);  dg = dx c w n a'(g)
 //   dw = sum_rows dx c a n,  dc = sum_rows dx a w n,  du = sum_rows d_normed out ro
 //
-// Memory bounds both, the arithmetic not far behind in 16 bits: 25 and 45 instructions an entry, and 5 and 8 entries moved.  So a row is read once and held in registers until it is written, and
-// what is summed over it goes from lane to lane (and from wave to wave through shared memory where a row takes several).  All sums are
+// Memory bounds both, with 5 and 8 entries moved, and the arithmetic is not far behind in 16 bits.  So a row is read once and held in registers until it
+// is written, and what is summed over it goes from lane to lane (and from wave to wave through shared memory where a row takes several).  All sums are
 // in 32 bits; `out` and `normed` are rounded once, each from the unrounded sum, and the way back starts from the stored `out`.
 #include "activations.h"
 
@@ -63,8 +63,8 @@ template <int WAVES, int N, int LANES = 64> __device__ __forceinline__ void row_
 }
 
 // A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i, or (LANES = 16) by a quarter of a wave.  One
-// wave or less to a row leaves several rows to a workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end of the row is moved back to end there:
-// its first entries are another pack's, and count as zero here.
+// wave or less to a row leaves several rows to a workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end
+// of the row is moved back to end there: its first entries are another pack's, and count as zero here.
 template <int V, int K, int WAVES, int LANES = 64> struct tile {
     static_assert(LANES == 64 || (LANES == 16 && WAVES == 1), "a row has whole waves, or 16 lanes of one");
     static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, lanes = LANES * WAVES, rows = WAVES == 1 ? 256 / LANES : 1;
