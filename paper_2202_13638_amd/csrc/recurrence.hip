@@ -1,11 +1,12 @@
 // The gated linear recurrence of a policy with memory (include/bagel.h) and its gradient.
 //
-//   q_t = 1 / (1 + exp(f_t + b)),   h_t = h_{t-1} + q_t (x_t - h_{t-1})
+//   q_t = 1 / (1 + exp(f_t + b)),   h_t = h_{t-1} + q_t (x_t - h_{t-1}) = x_t + (1 - q_t) (h_{t-1} - x_t)
 // Over several rows h goes to A h + H, with A the product of the (1 - q_t), and the H of two pieces one after the other is A2 H1 + H2.  A
 // piece in which a sequence begins does not depend on what was before: it is marked by A = -1, and its A is never multiplied
 // (what another sequence left may be infinite).  Backwards, with g_t the gradient of h_t: g_t = dh_t + c_t, dx_t = q_t g_t,
 // c_{t-1} = g_t - q_t g_t, df_t = (h_{t-1} - x_t) (1 - q_t) q_t g_t: c is a recurrence of the same kind the other way, and h_{t-1} is
-// computed again from the state before the span, which the forward pass kept.
+// computed again from the state before the span, which the forward pass kept.  The second form of h_t and 1 - q_t itself are for gates that are nearly open, where
+// 1 - q_t is far smaller than a rounding of q_t.
 //
 // One pass over the data.  A workgroup has a span of rows and 64 V channels, a wave a segment of the span's rows and V channels a lane, all of
 // it in registers.  The waves sum up their segments, the workgroup its span, and publishes that; the state before the span comes from
@@ -224,16 +225,33 @@ template <typename A> __device__ __forceinline__ void to_previous(const A &a, in
     sequence = max(sequence, 0);
 }
 
-// q for a forget gate f and bias b, which comes times log2(e).
-constexpr float LOG2E = 1.44269504f;
-__device__ __forceinline__ float share(float f, float b) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(fmaf(f, LOG2E, b))); }
+// The share q of a forget gate f and bias b, which comes times log2(e).  1 - q is formed from q as long as that leaves enough of it: a unit of q
+// is 8 units of 1 - q at 15/16, but 3 % of it at 1 - e^-13, and from e^-17 on nothing is left.  Of a gate that is open further than 15/16, 1 - q is kept in the place of
+// q, from the exponential, with a minus (also of zero).
+constexpr float LOG2E = 1.44269504f, OPEN = 0.9375f;
+__device__ __forceinline__ float gate(float f, float b) { return __builtin_amdgcn_exp2f(fmaf(f, LOG2E, b)); }
+__device__ __forceinline__ float share(float f, float b) { return __builtin_amdgcn_rcpf(1.0f + gate(f, b)); }
+__device__ __forceinline__ float kept(float q, float f, float b) { return q > OPEN ? -(gate(f, b) * q) : q; }
+// a for a gate that is open, else b.  (SOME: whether any of the wave's may be; the results are the same either way.)
+// By bits: a comparison for every row would take more scalar registers than there are.
+template <bool SOME> __device__ __forceinline__ float where_open(float q, float a, float b)
+{
+    if constexpr (SOME) asm("v_bfi_b32 %0, %1, %2, %0" : "+v"(b) : "v"(__float_as_int(q) >> 31), "v"(a));
+    return b;
+}
+// h + q (x - h), and where the gate is open x + (1 - q) (h - x): a part of the difference is added to what stays
+template <bool SOME> __device__ __forceinline__ float mixed(float q, float x, float h) { return fmaf(q, x - h, where_open<SOME>(q, x, h)); }
+// (1 - q) g
+template <bool SOME> __device__ __forceinline__ float left(float q, float g) { return fmaf(-q, g, where_open<SOME>(q, 0.0f, g)); }
 __device__ __forceinline__ float at(const float *p, int64_t i) { return p ? p[i] : 0.0f; }
 
-// f(special) with a constant 0 where there is none: most segments lie within one sequence, and a branch at every row costs them a tenth.
-template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, F &&f)
+// f(special, whether a gate is open) with constants: 0 special rows where there are none, as most segments lie within one sequence and a branch at every row costs them a
+// tenth, and no open gates where there are none: with them 131072 x 1024 bf16 takes 225 and 320 us, without 214 and 303.
+template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, bool open, F &&f)
 {
-    if (special == 0) f(std::integral_constant<uint64_t, 0>());
-    else f(special);
+    if (special != 0) f(special, std::true_type());
+    else if (open) f(std::integral_constant<uint64_t, 0>(), std::true_type());
+    else f(std::integral_constant<uint64_t, 0>(), std::false_type());
 }
 
 // What is the same in both directions: which span and channels a workgroup has, and its reads.
@@ -312,6 +330,24 @@ template <typename T, int V, int S> struct wave_tile {
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = seg.outside(i) ? 0.0f : at(a.d_final, (int64_t)sequence * a.width + ch + v);
     }
+    // the shares of the segment's gates; whether any of the wave's is open
+    static __device__ __forceinline__ bool shares(const pack (&f)[S], const float (&b)[V], float (&q)[S][V])
+    {
+        float most = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                q[i][v] = share(one(f[i], v), b[v]);
+                most = fmaxf(most, q[i][v]);
+            }
+        if (!__any(most > OPEN)) return false;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) q[i][v] = kept(q[i][v], one(f[i], v), b[v]);
+        return true;
+    }
     __device__ __forceinline__ void store(const bagel_rows<T> &m, int row, const float (&x)[V]) const { bagel_store<T, V>(m.row(row) + ch, x); }
 };
 
@@ -357,24 +393,23 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 8 : 4) void recurrence
     const segment<S> seg = segment_at<S>(a, w.t0, some);
     const uint64_t special = seg.special();
     w.clear_outside(seg, f, x);
-    float q[S][V], h[V];
+    float q[S][V], h[V], b[V];
     piece mine[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float b = at(a.bias, w.ch + v) * LOG2E;
+        b[v] = at(a.bias, w.ch + v) * LOG2E;
         mine[v] = {1.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v), b);
     }
+    const bool open = wt::shares(f, b, q);
     int sequence = seg.sequence;
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             if (special >> i & 1) w.enter(a, seg, i, sequence, mine);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                mine[v].H = fmaf(q[i][v], wt::one(x[i], v) - mine[v].H, mine[v].H);
-                mine[v].A = fmaf(-mine[v].A, q[i][v], mine[v].A);
+                mine[v].H = mixed<some()>(q[i][v], wt::one(x[i], v), mine[v].H);
+                mine[v].A = left<some()>(q[i][v], mine[v].A);
             }
         }
     });
@@ -409,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 8 : 4) void recurrence
 #pragma unroll
         for (int v = 0; v < V; ++v) a.carry[(int64_t)(w.t0 / SPAN) * a.width + w.ch + v] = h[v];
     sequence = seg.sequence;
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             if (special >> i & 1) {
@@ -417,7 +452,7 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 8 : 4) void recurrence
                 w.enter(a, seg, i, sequence, h);
             }
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = fmaf(q[i][v], wt::one(x[i], v) - h[v], h[v]);
+            for (int v = 0; v < V; ++v) h[v] = mixed<some()>(q[i][v], wt::one(x[i], v), h[v]);
             if ((special >> i & 1) && a.final_state && seg.last(i))
 #pragma unroll
                 for (int v = 0; v < V; ++v) a.final_state[(int64_t)sequence * a.width + w.ch + v] = h[v];
@@ -466,30 +501,28 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence
     for (int v = 0; v < V; ++v) {
         mine[v] = {1.0f, 0.0f};
         reach[v] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < S; ++i) q[i][v] = share(wt::one(f[i], v), b[v]);
     }
+    const bool open = wt::shares(f, b, q);
     int sequence = seg.sequence;
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             if (special >> i & 1) w.enter(a, seg, i, sequence, mine);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                mine[v].H = fmaf(q[i][v], wt::one(x[i], v) - mine[v].H, mine[v].H);
-                mine[v].A = fmaf(-mine[v].A, q[i][v], mine[v].A);
+                mine[v].H = mixed<some()>(q[i][v], wt::one(x[i], v), mine[v].H);
+                mine[v].A = left<some()>(q[i][v], mine[v].A);
             }
         }
     });
     const int last_sequence = sequence;      // of the segment's last row
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = S - 1; i >= 0; --i) {
             if (special >> i & 1) w.enter_back(a, seg, i, sequence, reach);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float g = wt::one(d[i], v) + reach[v];
-                reach[v] = fmaf(-q[i][v], g, g);
+                reach[v] = left<some()>(q[i][v], wt::one(d[i], v) + reach[v]);
             }
             if ((special >> i & 1) && seg.start(i)) to_previous(a, w.t0 + i, sequence);
         }
@@ -532,14 +565,14 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = through(pieces[k][w.lane][v], h[v]);
     sequence = seg.sequence;
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
             if (special >> i & 1) w.enter(a, seg, i, sequence, h);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 hx[i][v] = h[v] - wt::one(x[i], v);
-                h[v] = fmaf(-q[i][v], hx[i][v], h[v]);
+                h[v] = fmaf(-q[i][v], hx[i][v], where_open<some()>(q[i][v], wt::one(x[i], v), h[v]));
             }
         }
     });
@@ -548,7 +581,7 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence
         for (int v = 0; v < V; ++v) c[v] = through(back[k][w.lane][v], c[v]);
     const bool write_x = w.here && a.d_value.data, write_f = w.here && a.d_forget.data;
     sequence = last_sequence;
-    by_rows(special, [&](auto special) {
+    by_rows(special, open, [&](auto special, auto some) {
 #pragma unroll
         for (int i = S - 1; i >= 0; --i) {
             float dx[V], df[V];
@@ -558,10 +591,10 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float g = wt::one(d[i], v) + c[v];
-                dx[v] = q[i][v] * g;
-                c[v] = g - dx[v];
-                df[v] = hx[i][v] * fmaf(-q[i][v], dx[v], dx[v]);
+                const float part = some() ? fabsf(q[i][v]) : q[i][v], g = wt::one(d[i], v) + c[v], less = part * g, more = fmaf(-part, g, g);
+                dx[v] = where_open<some()>(q[i][v], more, less);
+                c[v] = where_open<some()>(q[i][v], less, more);
+                df[v] = hx[i][v] * fmaf(-part, less, less);
             }
             if (special >> i & 1) {
                 if (seg.outside(i))
@@ -621,9 +654,8 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int width, bage
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * width; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / width;
         const int ch = (int)(i - r * width);
-        const float q = share((float)forget.row(r)[ch], at(bias, ch) * LOG2E);
-        float h = state[i];
-        h = fmaf(q, (float)value.row(r)[ch] - h, h);
+        const float f = (float)forget.row(r)[ch], b = at(bias, ch) * LOG2E;
+        const float h = mixed<true>(kept(share(f, b), f, b), (float)value.row(r)[ch], state[i]);
         state[i] = h;
         if (hidden.data) hidden.row(r)[ch] = (T)h;
     }

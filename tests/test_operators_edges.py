@@ -1,0 +1,51 @@
+"""Edges of the operators of a policy with memory: gates that are nearly open or shut, large biases, infinities, draws of the moments in 8
+bits, arguments that have to be refused, and sizes at which a workgroup goes through several rows or blocks.
+
+Tolerances are those of test_operators.py where no other is derived."""
+import pytest
+import torch
+import test_operators as ops
+from paper_2202_13638_amd import binding
+
+gpu = pytest.mark.gpu
+ULP = 2.0 ** -23
+
+
+# ------------------------------------------------------------------------------------------------------ gated recurrence
+BIASES = [-30.0, -18.0, -14.0, -10.0, -5.0, 0.0, 5.0, 10.0]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("width", [64, 72, 260])
+def test_gradients_of_gates_that_are_nearly_open(width, dtype):
+    """A channel whose gate takes the value whole, 1 - q down to e^-32, has gradients of that size, and each is right by its own size: an optimiser that divides
+    by a gradient's own size sees nothing else.  The share of a gate carries (1.3 |z| + 3) units (see above), a gradient two of them; a state
+    that some hundred rows move is off by some twenty units.  Held to 4 |z| + 40 units of what is largest in the channel."""
+    t, at = ops.TYPES[dtype], [0, 140, 141, 400]
+    x, f, dh = (ops._normal((400, width), i, t, scale) for i, scale in ((1, 1.0), (2, 0.5), (3, 1.0)))
+    bias = torch.tensor([BIASES[c % len(BIASES)] for c in range(width)])
+    h0, dl = ops._normal((3, width), 5), ops._normal((3, width), 6)
+    want, terms = ops._recurrence_ref(x, f, at, bias, h0, dh, dl)
+    got = ops._run_recurrence(x.cuda(), f.cuda(), at, bias.cuda(), h0.cuda(), dh.cuda(), dl.cuda())
+    units = (4 * (f.double() + bias).abs().amax(0) + 40) * ULP
+    for k in ("hidden", "final", "d_value", "d_forget", "d_initial", "d_bias"):
+        g, w = got[k].double().cpu(), want[k]
+        bound = units * (terms if k == "d_bias" else w.abs().amax(0)) + 1.01 * ops.HALF_ULP[got[k].dtype] * w.abs()
+        off = (g - w).abs() / bound
+        assert bool((off <= 1).all()), f"{k}: {float(off.max()):.3g} times the bound, channel of bias {bias[int(off.amax(0).argmax()) if off.dim() > 1 else int(off.argmax())]}"
+
+
+@gpu
+def test_a_value_that_replaces_a_large_state():
+    """A state of 1e4 gives way to a value of a thousandth: what is left is the value and (1 - q) of the state, each to a rounding and to what the gate carries."""
+    width = 64
+    x, f = 1e-3 * (1 + ops._normal((1, width), 1).abs()), ops._normal((1, width), 2, scale=0.5)
+    bias, h0 = torch.full((width,), -18.0), 1e4 * (1 + ops._normal((1, width), 3).abs())
+    z = f.double() + bias
+    want = torch.sigmoid(-z) * x.double() + torch.sigmoid(z) * h0.double()
+    state, hidden = h0.cuda(), torch.empty(1, width, device="cuda")
+    binding.bagel_recurrence_step(x.cuda(), f.cuda(), state, bias=bias.cuda())
+    binding.bagel_recurrence(x.cuda(), f.cuda(), hidden, 1, bias=bias.cuda(), initial=h0.cuda())
+    for got in (state, hidden):
+        assert bool(((got.double().cpu() - want).abs() <= (4 * z.abs() + 40) * ULP * want).all())
