@@ -225,11 +225,11 @@ template <typename A> __device__ __forceinline__ void to_previous(const A &a, in
     sequence = max(sequence, 0);
 }
 
-// The share q of a forget gate f and bias b, which comes times log2(e).  1 - q is formed from q as long as that leaves enough of it: a unit of q
+// The share q of a forget gate f and bias b.  They are added first: they may be large and cancel, and a rounding of b log2(e) would stay.  1 - q is formed from q as long as that leaves enough of it: a unit of q
 // is 8 units of 1 - q at 15/16, but 3 % of it at 1 - e^-13, and from e^-17 on nothing is left.  Of a gate that is open further than 15/16, 1 - q is kept in the place of
 // q, from the exponential, with a minus (also of zero).
 constexpr float LOG2E = 1.44269504f, OPEN = 0.9375f;
-__device__ __forceinline__ float gate(float f, float b) { return __builtin_amdgcn_exp2f(fmaf(f, LOG2E, b)); }
+__device__ __forceinline__ float gate(float f, float b) { return __builtin_amdgcn_exp2f((f + b) * LOG2E); }
 __device__ __forceinline__ float share(float f, float b) { return __builtin_amdgcn_rcpf(1.0f + gate(f, b)); }
 __device__ __forceinline__ float kept(float q, float f, float b) { return q > OPEN ? -(gate(f, b) * q) : q; }
 // a for a gate that is open, else b.  (SOME: whether any of the wave's may be; the results are the same either way.)
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 8 : 4) void recurrence
     piece mine[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        b[v] = at(a.bias, w.ch + v) * LOG2E;
+        b[v] = at(a.bias, w.ch + v);
         mine[v] = {1.0f, 0.0f};
     }
     const bool open = wt::shares(f, b, q);
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(64 * WAVES, V == 1 && DEEP ? 6 : 4) void recurrence
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         h[v] = a.carry[(int64_t)w.span * a.width + w.ch + v];
-        b[v] = at(a.bias, w.ch + v) * LOG2E;
+        b[v] = at(a.bias, w.ch + v);
     }
     const segment<S> seg = segment_at<S>(a, w.t0, some);
     const uint64_t special = seg.special();
@@ -654,7 +654,7 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int width, bage
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * width; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / width;
         const int ch = (int)(i - r * width);
-        const float f = (float)forget.row(r)[ch], b = at(bias, ch) * LOG2E;
+        const float f = (float)forget.row(r)[ch], b = at(bias, ch);
         const float h = mixed<true>(kept(share(f, b), f, b), (float)value.row(r)[ch], state[i]);
         state[i] = h;
         if (hidden.data) hidden.row(r)[ch] = (T)h;

@@ -12,6 +12,27 @@ ULP = 2.0 ** -23
 
 
 # ------------------------------------------------------------------------------------------------------ gated recurrence
+@gpu
+@pytest.mark.parametrize("size", [0.0, 50.0, 200.0, 1000.0])
+def test_a_gate_of_a_large_bias_and_a_forget_gate_against_it(size):
+    """q depends on forget + bias alone, whose sum is exact here.  With z that sum: 2^-24 of z from its product with log2(e), and 2^-25 from
+    that constant, move the exponential by 1.1 |z| 2^-24; exponential, 1 + e, reciprocal, product and the new state round five times by a unit at
+    most.  Held to twice that."""
+    width, rows = 96, 40
+    z, bias = 3 * ops._normal((rows, width), 1), size * torch.where(torch.arange(width) % 2 == 0, 1.0, -1.0)
+    f = z - bias
+    z = f.double() + bias.double()
+    q = torch.sigmoid(-z)
+    state, hidden = torch.zeros(rows, width, device="cuda"), torch.empty(rows, width, device="cuda")
+    binding.bagel_recurrence_step(torch.ones(rows, width, device="cuda"), f.cuda(), state, hidden, bias=bias.cuda())
+    bound = (2 * z.abs() + 10) * ULP * q
+    assert bool(((state.double().cpu() - q).abs() <= bound).all())
+    r = ops._run_recurrence(torch.ones(rows, width, device="cuda"), f.cuda(), list(range(rows + 1)), bias.cuda(), None,
+                            torch.ones(rows, width, device="cuda"), None)
+    for got, want in ((r["hidden"], q), (r["final"], q), (r["d_value"], q), (r["d_forget"], -q * torch.sigmoid(z))):
+        assert bool(((got.double().cpu() - want).abs() <= 2 * (2 * z.abs() + 10) * ULP * want.abs()).all())
+
+
 BIASES = [-30.0, -18.0, -14.0, -10.0, -5.0, 0.0, 5.0, 10.0]
 
 
