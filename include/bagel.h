@@ -436,12 +436,22 @@ int bagel_recurrence_step(const bagel_gated_recurrence *args, void *hip_stream);
  * state_bits 8: m and v are float8 e4m3 codes[count] in blocks of BAGEL_ADAMW_BLOCK, with a float32 scale for each, m_scale and
  *   v_scale[ceil(count / BAGEL_ADAMW_BLOCK)], both zero at the start.  m = code * scale and sqrt(v) = code * scale, where scale = (largest magnitude
  *   of the block) / 448.  A value between two codes becomes one or the other by chance, so that its mean is kept: with beta2 = 0.999 a step
- *   moves v by far less than codes are apart, and rounding to nearest would lose every move.  The chance is 16 bits of a hash of
- *   the place in the tensor, `step` and `seed`: the library draws no random numbers, and equal calls give equal results.  A root
+ *   moves v by far less than codes are apart, and rounding to nearest would lose every move.  A root
  *   above zero never becomes code zero, which would make its next update unbounded.  Blocks whose largest magnitude is below 1e-30 are held as zero.
+ * draws: what the chance is made of, 16 bits of a hash for m and 16 for sqrt(v).  The library draws no random numbers: equal calls give equal results.
+ *   BAGEL_DRAWS_MIXED  of the place in the tensor, the tensor's number in the call, `step` and `seed`, independent of each other from place to place, tensor
+ *                      to tensor and update to update.  The seed may stay the same over all updates; calls that share an update (several groups of
+ *                      tensors) and runs that should differ take different ones.
+ *   BAGEL_DRAWS_GIVEN  for a caller that computes the draws itself, of the place, `step` and `seed` alone:
+ *                        x = place * 0x9E3779B9 + seed * 0xBB67AE85 + step * 0x9E3779B9;  x = (x ^ x >> 16) * 0x6A09E667;
+ *                        x = (x ^ x >> 15) * 0x3C6EF373;  x = x ^ x >> 16    (modulo 2^32; m takes the low half, sqrt(v) the high one).
+ *                      Tensors of a call share these.  With the same seed an update has the draws of the one before, one place on: every value of a block
+ *                      would go through the same ones, and their errors would not average out, so the seed has to be another one for every update.
  * lr >= 0, 0 <= beta < 1, eps > 0 (also as a float), lr weight_decay < 1.  Errors: EINVAL, EHIP.
  */
 #define BAGEL_ADAMW_BLOCK 256
+#define BAGEL_DRAWS_MIXED 0
+#define BAGEL_DRAWS_GIVEN 1
 
 typedef struct {
     float *param;
@@ -459,6 +469,7 @@ typedef struct {
     const float *grad_scale;
     int32_t grad_dtype, copy_dtype, state_bits;
     uint32_t seed;
+    int32_t draws;
 } bagel_adamw;
 
 int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_tensors, const bagel_adamw *options, void *hip_stream);

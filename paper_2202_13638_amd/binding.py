@@ -101,7 +101,7 @@ class _AdamWTensor(C.Structure):
 class _AdamW(C.Structure):
     _fields_ = [("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
                 ("grad_scale", C.c_void_p), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
-                ("seed", C.c_uint32)]
+                ("seed", C.c_uint32), ("draws", C.c_int32)]
 
 
 _lib = None
@@ -214,7 +214,7 @@ def bagel_sample_eval_static(dims: Dims, X, lengthscale, signal_var, omega, phas
 # makes the structures above as bytes.
 JOIN_MAX_WIDTH, RECURRENCE_SPAN, ADAMW_BLOCK = 16384, 128, 256
 _ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
-_JOIN_HEAD, _RECURRENCE_HEAD, _ADAMW_OPTIONS, _WORKSPACE = (struct.Struct(f) for f in ("qiiif", "qiii4xP", "qddddPiiiI", "Pq"))
+_JOIN_HEAD, _RECURRENCE_HEAD, _ADAMW_OPTIONS, _WORKSPACE = (struct.Struct(f) for f in ("qiiif", "qiii4xP", "qddddPiiiIi4x", "Pq"))
 assert (_JOIN_HEAD.size, _RECURRENCE_HEAD.size, _ADAMW_OPTIONS.size) == (_Join.branch.offset, _Recurrence.value.offset, C.sizeof(_AdamW))
 _NOTHING = bytes(256)
 _torch = _marshal = _raw_stream = None
@@ -376,12 +376,15 @@ def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, strea
 
 
 def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, copy=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
-                     weight_decay=0.01, grad_scale=None, seed=0, stream=None):
+                     weight_decay=0.01, grad_scale=None, seed=None, run=0, stream=None):
     """One update of a list of tensors (see include/bagel.h).
 
     params: contiguous float32 tensors; grads, m, v, copy (None: none): lists of tensors of the same shapes.  grads are all of one
     type, and so are the entries of copy.  m and v are float32, or float8_e4m3fn with m_scale and v_scale, lists of float32 tensors
-    with an entry for every ADAMW_BLOCK values.  weight_decay: a number, or one for every tensor."""
+    with an entry for every ADAMW_BLOCK values.  weight_decay: a number, or one for every tensor.
+
+    The draws that round moments in 8 bits are independent from place to place, tensor to tensor and update to update.  `run` tells runs apart, and
+    calls that share an update.  seed: for a caller that computes the draws itself (see BAGEL_DRAWS_GIVEN), another one for every update."""
     lib = _load()
     on, device = _stream(stream)
     n, table, grad_type, copy_type, bits = _marshal.adamw(device, params, grads, m, v, m_scale, v_scale, copy, weight_decay)
@@ -390,7 +393,8 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
         if not isinstance(grad_scale, _torch.Tensor) or grad_scale.numel() != 1 or grad_scale.dtype != _torch.float32 or grad_scale.get_device() != device:
             raise ValueError("grad_scale must hold one float32 value and be on the current GPU")
         scale = grad_scale.data_ptr()
-    options = _ADAMW_OPTIONS.pack(int(step), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, int(seed) & 0xFFFFFFFF)
+    options = _ADAMW_OPTIONS.pack(int(step), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, (run if seed is None else int(seed)) & 0xFFFFFFFF,
+                                  seed is not None)
     _done(lib, lib.bagel_adamw_step(table, n, options, on))
 
 

@@ -21,6 +21,7 @@ struct adamw_tensor {
     void *copy;
     int64_t count;
     float keep;                  // 1 - lr weight_decay
+    uint32_t key;                // of its draws
 };
 
 struct adamw_args {
@@ -28,7 +29,7 @@ struct adamw_args {
     uint32_t first[TENSORS];     // the first piece of each
     const float *grad_scale;
     int n, grad_dtype, copy_dtype;
-    uint32_t pieces, key;        // of all tensors
+    uint32_t pieces;             // of all tensors
     int each;                    // blocks of 256 that a wave takes of a piece: a piece is 4 each
     float beta1, rest1, beta2, rest2, rate, root, eps;       // rate = lr / (1 - beta1^step), root = 1 / sqrt(1 - beta2^step)
 };
@@ -101,14 +102,24 @@ template <bool WHOLE> __device__ __forceinline__ void store_codes(void *p, int64
             if (place<false>(i) < rest) q[place<false>(i)] = (uint8_t)(bytes >> 8 * i);
 }
 
-// 32 random bits for every place of a tensor: a product with an odd number near 2^32 / golden ratio spreads the places, two rounds of shift
-// and multiply mix high bits into low ones and back.
-__device__ __forceinline__ uint32_t chance(uint32_t place, uint32_t key)
+// Two rounds of shift and multiply mix high bits into low ones and back.
+__host__ __device__ __forceinline__ uint32_t mixed(uint32_t x)
 {
-    uint32_t x = place * 0x9E3779B9u + key;
     x = (x ^ (x >> 16)) * 0x6A09E667u;
     x = (x ^ (x >> 15)) * 0x3C6EF373u;
     return x ^ (x >> 16);
+}
+
+// 32 random bits for every place of a tensor, which a product with an odd number near 2^32 / golden ratio spreads.  Two keys give the same bits, moved on by
+// their difference over that number, so keys have to be far from each other by themselves.
+__device__ __forceinline__ uint32_t chance(uint32_t place, uint32_t key) { return mixed(place * 0x9E3779B9u + key); }
+
+// The key of a tensor's draws in one update.  Mixed in one after the other, seed, update and the tensor's number leave no two keys that are near
+// each other for a reason.  (A sum of multiples, which a caller that knows its draws gets, makes an update's draws those of the one before, one place on.)
+uint32_t key_of(const bagel_adamw &o, int tensor)
+{
+    if (o.draws == BAGEL_DRAWS_GIVEN) return o.seed * 0xBB67AE85u + (uint32_t)o.step * 0x9E3779B9u;
+    return mixed(mixed(mixed(mixed(o.seed + 0x3C6EF372u) ^ (uint32_t)o.step) + (uint32_t)(o.step >> 32)) ^ (uint32_t)tensor);
 }
 
 // The magnitude of a code (float8 e4m3) for y in [0, 448], up or down by a chance of 16 bits.  From 2^-6 on a code has 3 bits behind the
@@ -186,7 +197,7 @@ template <int BITS, bool WHOLE> __device__ __forceinline__ void update_block(con
     } else {
         uint32_t bits[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) bits[i] = chance((uint32_t)from + place<WHOLE>(i), a.key);
+        for (int i = 0; i < 4; ++i) bits[i] = chance((uint32_t)from + place<WHOLE>(i), w.key);
         const float sm = encode<false>(m, bits), sv = encode<true>(r, bits);
         store_codes<WHOLE>(w.m, from, rest, m);
         store_codes<WHOLE>(w.v, from, rest, r);
@@ -228,6 +239,7 @@ const char *check_adamw(const bagel_adamw_tensor *tensors, int32_t n, const bage
     if (!((float)o->eps > 0.0f) || !isfinite((float)o->eps)) return "eps must be positive";
     if (!bagel_type_ok(o->grad_dtype) || !bagel_type_ok(o->copy_dtype)) return "unknown dtype";
     if (o->state_bits != 32 && o->state_bits != 8) return "state_bits must be 32 or 8";
+    if (o->draws != BAGEL_DRAWS_MIXED && o->draws != BAGEL_DRAWS_GIVEN) return "unknown draws";
     for (int i = 0; i < n; ++i) {
         const bagel_adamw_tensor &t = tensors[i];
         if (t.count < 0 || t.count >= 1ll << 38) return "count must be >= 0 and below 2^38";
@@ -251,7 +263,6 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
     a.grad_scale = o->grad_scale;
     a.grad_dtype = o->grad_dtype;
     a.copy_dtype = o->copy_dtype;
-    a.key = o->seed * 0xBB67AE85u + (uint32_t)o->step * 0x9E3779B9u;
     a.beta1 = (float)o->beta1;
     a.rest1 = (float)(1.0 - o->beta1);
     a.beta2 = (float)o->beta2;
@@ -282,7 +293,7 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
         if (a.n == TENSORS || (a.n > 0 && a.pieces + pieces > 1u << 30)) {
             if ((e = launch()) != hipSuccess) break;
         }
-        a.tensor[a.n] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay)};
+        a.tensor[a.n] = {t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, t.copy, t.count, (float)(1.0 - o->lr * t.weight_decay), key_of(*o, i)};
         a.first[a.n++] = a.pieces;
         a.pieces += pieces;
     }

@@ -28,7 +28,7 @@ class MemoryPolicy:
 
     def __init__(self, d_in: int, d_out: int, width: int, blocks: int, dtype=torch.bfloat16, state_bits: int = 32, seed: int = 0):
         g = torch.Generator().manual_seed(seed)
-        self.width, self.blocks, self.dtype, self.updates = width, blocks, dtype, 0
+        self.width, self.blocks, self.dtype, self.seed, self.updates = width, blocks, dtype, seed, 0
 
         def matrix(rows, columns):
             return (torch.randn(rows, columns, generator=g) / columns ** 0.5).cuda()
@@ -97,11 +97,12 @@ class MemoryPolicy:
     def update(self, grads: Dict[str, torch.Tensor], lr: float = 1e-3, weight_decay: float = 0.01, grad_scale: Optional[torch.Tensor] = None):
         """One step of AdamW: the matrices with weight decay and their working copies, the vectors without."""
         self.updates += 1
-        for group, decay, copy in ((self.matrices, weight_decay, [self.work[k] for k in self.matrices]), (self.vectors, 0.0, None)):
+        groups = ((self.matrices, weight_decay, [self.work[k] for k in self.matrices]), (self.vectors, 0.0, None))
+        for i, (group, decay, copy) in enumerate(groups):
             moments = [self.moments[k] for k in group]
             binding.bagel_adamw_step(list(group.values()), [grads[k] for k in group], [s.m for s in moments], [s.v for s in moments], self.updates,
                                      m_scale=[s.m_scale for s in moments], v_scale=[s.v_scale for s in moments], copy=copy, lr=lr,
-                                     weight_decay=decay, grad_scale=grad_scale, seed=self.updates)
+                                     weight_decay=decay, grad_scale=grad_scale, run=len(groups) * self.seed + i)
 
     # ------------------------------------------------------------------------------------------------ one control period at a time
     def start(self, machines: int) -> List[torch.Tensor]:

@@ -70,3 +70,67 @@ def test_a_value_that_replaces_a_large_state():
     binding.bagel_recurrence(x.cuda(), f.cuda(), hidden, 1, bias=bias.cuda(), initial=h0.cuda())
     for got in (state, hidden):
         assert bool(((got.double().cpu() - want).abs() <= (4 * z.abs() + 40) * ULP * want).all())
+
+
+# ------------------------------------------------------------------------------------------------------------------ AdamW
+def _draws(step, n=1 << 14, tensors=2, **kw):
+    """For every place of some tensors of the same values whether its code was rounded up; the chance of that is (0.37 * 448 - 160) / 16 = 0.36."""
+    grads = [torch.full((n,), 0.37, device="cuda") for _ in range(tensors)]
+    for g in grads:
+        g[::256] = 1.0                                               # the largest of every block
+    p, m, v = ([torch.zeros(n, device="cuda").to(kind) for _ in range(tensors)] for kind in (torch.float32, torch.float8_e4m3fn, torch.float8_e4m3fn))
+    sm, sv = ([torch.zeros(n // 256, device="cuda") for _ in range(tensors)] for _ in range(2))
+    binding.bagel_adamw_step(p, grads, m, v, step, m_scale=sm, v_scale=sv, lr=0.0, weight_decay=0.0, **kw)
+    codes = torch.stack([c.float() for c in m])
+    here = torch.arange(n, device="cuda") % 256 != 0
+    assert set(codes[:, here].unique().tolist()) == {160.0, 176.0}
+    return (codes == 176).float(), here
+
+
+def _independent(a, b, here):
+    """Draws that have nothing to do with each other agree in 0.36^2 + 0.64^2 of all places, within five standard deviations."""
+    same = 0.36 ** 2 + 0.64 ** 2
+    return abs(float((a == b)[here].float().mean()) - same) < 5 * (same * (1 - same) / int(here.sum())) ** 0.5
+
+
+@gpu
+def test_draws_of_neighbours_updates_and_tensors_are_independent():
+    (a, here), (b, _), (again, _), (other, _) = _draws(41), _draws(42), _draws(41), _draws(41, run=1)
+    assert torch.equal(a, again)                                     # equal calls give equal results
+    for shift in (0, 1, 2, 17):                                      # the next update is not this one moved on
+        both = here & here.roll(-shift)
+        assert _independent(a.roll(-shift, 1)[0], b[0], both), shift
+        assert shift == 0 or _independent(a.roll(-shift, 1)[0], a[0], both), shift
+    assert _independent(a[0], a[1], here)                            # two tensors of one update
+    assert _independent(a[0], other[0], here)                        # and of two calls with other numbers
+
+
+@gpu
+def test_roots_of_a_long_run_scatter_from_place_to_place_only():
+    """sqrt(v) climbs from nothing over 4000 updates with gradients of 1 beside one of 3 in every block.  From place to place its codes scatter by 5 % (see
+    test_adamw_in_8_bits_keeps_means); where the draws are independent the mean of a block's 255 scatters by 0.05 / sqrt(255) = 0.3 %.  Held to 1 %."""
+    n = 1 << 13
+    m, v = (torch.zeros(n, device="cuda").to(torch.float8_e4m3fn) for _ in range(2))
+    sm, sv = (torch.zeros(n // 256, device="cuda") for _ in range(2))
+    p, g = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda")
+    g[::256] = 3.0
+    for t in range(1, 4001):
+        binding.bagel_adamw_step([p], [g], [m], [v], t, m_scale=[sm], v_scale=[sv], lr=0.0, weight_decay=0.0)
+    root = ops._values(v, sv).view(-1, 256)[:, 1:]
+    want = (1 - 0.999 ** 4000) ** 0.5
+    assert abs(float(root.mean()) / want - 1) < 0.01
+    assert float(root.mean(1).std()) / want < 0.01
+
+
+@gpu
+@pytest.mark.parametrize("step,seed", [(1, 0), (42, 7), (1 << 20, 0xFFFFFFFF)])
+def test_draws_of_a_given_number_are_those_that_are_documented(step, seed):
+    mask = 0xFFFFFFFF
+    got, here = _draws(step, seed=seed)
+    x = (torch.arange(got.shape[1]) * 0x9E3779B9 + seed * 0xBB67AE85 + step * 0x9E3779B9) & mask
+    x = ((x ^ (x >> 16)) * 0x6A09E667) & mask
+    x = ((x ^ (x >> 15)) * 0x3C6EF373) & mask
+    low = ((x ^ (x >> 16)) & 0xFFFF)[here.cpu()]
+    sure = ((low.double() / 65536 - 0.64).abs() > 1e-4)              # 0.37 * 448 itself is rounded
+    for tensor in got.cpu():
+        assert torch.equal((tensor[here.cpu()] == 1)[sure], (low >= 0.64 * 65536)[sure])
