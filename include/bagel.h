@@ -438,6 +438,8 @@ int bagel_recurrence_step(const bagel_gated_recurrence *args, void *hip_stream);
  *   of the block) / 448.  A value between two codes becomes one or the other by chance, so that its mean is kept: with beta2 = 0.999 a step
  *   moves v by far less than codes are apart, and rounding to nearest would lose every move.  A root
  *   above zero never becomes code zero, which would make its next update unbounded.  Blocks whose largest magnitude is below 1e-30 are held as zero.
+ *   A moment that is not finite (of a gradient that is not, or whose square is not) is held as NaN, and the scale is that of the others: as in
+ *   32 bits it stays in its place.
  * draws: what the chance is made of, 16 bits of a hash for m and 16 for sqrt(v).  The library draws no random numbers: equal calls give equal results.
  *   BAGEL_DRAWS_MIXED  of the place in the tensor, the tensor's number in the call, `step` and `seed`, independent of each other from place to place, tensor
  *                      to tensor and update to update.  The seed may stay the same over all updates; calls that share an update (several groups of

@@ -148,9 +148,8 @@ __device__ __forceinline__ float largest(const float (&v)[4])
 }
 
 // Codes of a block, and its scale in every lane.  ROOT: of roots, of which none above zero becomes zero.
-template <bool ROOT> __device__ __forceinline__ float encode(float (&v)[4], const uint32_t (&bits)[4])
+template <bool ROOT> __device__ __forceinline__ float encode_finite(float (&v)[4], const uint32_t (&bits)[4], float top)
 {
-    float top = largest(v);
     if (top < 1e-30f) top = 0.0f;
     const float scale = top > 0.0f ? 1.0f / top * LARGEST : 0.0f;
 #pragma unroll
@@ -159,6 +158,20 @@ template <bool ROOT> __device__ __forceinline__ float encode(float (&v)[4], cons
         v[i] = !ROOT ? copysignf(code, v[i]) : v[i] > 0.0f && top > 0.0f ? fmaxf(code, 1.0f / 512.0f) : code;
     }
     return top * (1.0f / LARGEST);
+}
+
+// The same where some are not finite: they are kept as NaN in their places.  A scale made of them would take the other 255 along.
+template <bool ROOT> __device__ __forceinline__ float encode(float (&v)[4], const uint32_t (&bits)[4])
+{
+    const float top = largest(v);
+    if (isfinite(top)) return encode_finite<ROOT>(v, bits, top);
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = isfinite(v[i]) ? v[i] : 0.0f;
+    const float scale = encode_finite<ROOT>(w, bits, largest(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = isfinite(v[i]) ? w[i] : __builtin_nanf("");
+    return scale;
 }
 
 template <int BITS, bool WHOLE> __device__ __forceinline__ void update_block(const adamw_args &a, const adamw_tensor &w, int64_t block, float gs)

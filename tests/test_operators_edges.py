@@ -134,3 +134,30 @@ def test_draws_of_a_given_number_are_those_that_are_documented(step, seed):
     sure = ((low.double() / 65536 - 0.64).abs() > 1e-4)              # 0.37 * 448 itself is rounded
     for tensor in got.cpu():
         assert torch.equal((tensor[here.cpu()] == 1)[sure], (low >= 0.64 * 65536)[sure])
+
+
+@gpu
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan"), 1e30])
+def test_an_infinity_takes_its_own_place_of_a_block_in_8_bits(bad):
+    """As in 32 bits: what is not finite is kept as that, and the other 255 of its block go on as if a small number stood there."""
+    n, at = 700, 300
+
+    def run(first):
+        p, g = ops._normal((n,), 1).cuda(), ops._normal((n,), 2).cuda()
+        m, v = (torch.zeros(n, device="cuda").to(torch.float8_e4m3fn) for _ in range(2))
+        sm, sv = (torch.zeros(3, device="cuda") for _ in range(2))
+        for t in range(1, 5):
+            g = ops._normal((n,), 2 + t).cuda()
+            g[at] = first if t == 2 else 1e-3
+            binding.bagel_adamw_step([p], [g], [m], [v], t, m_scale=[sm], v_scale=[sv], seed=t)
+        return p, m, v, sm, sv
+
+    want, got = run(1e-3), run(bad)
+    rest = torch.arange(n, device="cuda") != at
+    assert torch.equal(want[4], got[4]) and torch.equal(want[2].view(torch.uint8)[rest], got[2].view(torch.uint8)[rest])
+    assert torch.isnan(got[0][at])                                   # v is infinite, its step is no number
+    if abs(bad) == 1e30:
+        assert all(torch.isfinite(t.float()[rest]).all() for t in (got[0], got[1]))       # m is finite, and the largest of its block
+    else:
+        assert torch.equal(want[0][rest], got[0][rest]) and torch.equal(want[3], got[3])
+        assert torch.equal(want[1].view(torch.uint8)[rest], got[1].view(torch.uint8)[rest])
