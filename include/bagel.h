@@ -344,7 +344,8 @@ typedef struct {
  * the next block.  With R(z) = z / sqrt(mean(z^2) + eps) over a row,
  *   out    = resid + scale * act(gate) * (R(branch) * post_weight)
  *   normed = R(out) * pre_weight
- * gate: BAGEL_ACT_NONE (no gate is read, act = 1), or act(g) = g, 1 / (1 + exp(-g)), g / (1 + exp(-g)).  Vectors of `width`
+ * gate: BAGEL_ACT_NONE (no gate is read, act = 1), or act(g) = g, 1 / (1 + exp(-g)), g / (1 + exp(-g)); the last two and their
+ * derivatives are zero for a gate of minus infinity.  Vectors of `width`
  * that are NULL stand for ones.  `branch` may be left out (out = resid: the first block's norm), and so may `out` or `normed`.
  * `normed` is the norm of `out` before it is rounded.  `out` may be `resid` itself.
  *

@@ -72,6 +72,36 @@ def test_a_value_that_replaces_a_large_state():
         assert bool(((got.double().cpu() - want).abs() <= (4 * z.abs() + 40) * ULP * want).all())
 
 
+# ------------------------------------------------------------------------------------------------------------- block join
+@gpu
+@pytest.mark.parametrize("dtype", ops.TYPES)
+@pytest.mark.parametrize("width", [8, 64, 320, 777, 2600, 16384])
+def test_a_gate_that_is_shut_for_good(width, dtype):
+    """A gate of minus infinity takes its entry of the branch out: silu and logistic are 0 there, and so are their derivatives."""
+    t, rows = ops.TYPES[dtype], 5
+    for act in ("silu", "logistic"):
+        x = ops._join_inputs(rows, width, t, act)
+        shut = torch.rand(rows, width, generator=torch.Generator().manual_seed(9)) < 0.3
+        shut[3] = True                                              # a row of which nothing is left
+        far = torch.where(shut, torch.tensor(-1e4), x["gate"].float()).to(t)
+        x["gate"] = torch.where(shut, torch.tensor(float("-inf")), x["gate"].float()).to(t)
+        g = _cuda(x)
+        out, normed = torch.empty_like(g["resid"]), torch.empty_like(g["resid"])
+        rest = dict(act=act, **{k: g[k] for k in ("gate", "post_weight", "scale", "pre_weight")})
+        binding.bagel_block_join(g["branch"], g["resid"], out, normed, **rest)
+        assert torch.equal(out.cpu()[shut], x["resid"][shut])
+        # the reference has no infinite gates: at -1e4 its logistic function is exp(-1e4) = 0 in 64 bits too
+        want = ops._join_ref(x["branch"], x["resid"], far, act, x["post_weight"], x["scale"], x["pre_weight"], 1e-6)
+        ops._near(out, want[0], "out")
+        ops._near(normed, want[1], "normed")
+        got = ops._join_grad_case({**x, "gate": far}, g, out, ops._normal((rows, width), 7, t), ops._normal((rows, width), 8, t), act, 1e-6)
+        assert not got["d_gate"].cpu()[shut].any()
+
+
+def _cuda(d):
+    return {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in d.items()}
+
+
 # ------------------------------------------------------------------------------------------------------------------ AdamW
 def _draws(step, n=1 << 14, tensors=2, **kw):
     """For every place of some tensors of the same values whether its code was rounded up; the chance of that is (0.37 * 448 - 160) / 16 = 0.36."""
