@@ -140,14 +140,23 @@ struct list {
     list() = default;
     list(const list &) = delete;
     ~list() { Py_XDECREF(items); }
-    void of(PyObject *o, Py_ssize_t n, bool wanted)
+    // None is nothing at all, where nothing is wanted; whatever else is given has to be a sequence of n entries.
+    void of(PyObject *o, Py_ssize_t n, bool wanted, const char *name)
     {
         if (o != Py_None) {
             items = PySequence_Fast(o, "");
             PyErr_Clear();
         }
-        if (items ? PySequence_Fast_GET_SIZE(items) != n : wanted)
-            throw refused{"the lists of one update must have an entry for every tensor (moments in 8 bits need m_scale and v_scale)"};
+        if (items ? PySequence_Fast_GET_SIZE(items) != n : wanted || o != Py_None)
+            throw refused{std::string("the lists of one update must have an entry for every tensor, ") + name +
+                          " does not (moments in 8 bits need m_scale and v_scale)"};
+    }
+    // A list that has no place in this update: of the right length, and nothing in it.
+    void none(PyObject *o, Py_ssize_t n, const char *name)
+    {
+        of(o, n, false, name);
+        for (Py_ssize_t i = 0; items && i < n; ++i)
+            if ((*this)[i] != Py_None) throw refused{std::string(name) + " belongs to moments in 8 bits"};
     }
     PyObject *operator[](Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(items, i); }
 };
@@ -161,18 +170,21 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
         const Py_ssize_t n = PySequence_Size(args[1]);
         if (n < 0) return nullptr;
         list p, g, m, v, m_scale, v_scale, copy, decay;
-        p.of(args[1], n, true);
-        g.of(args[2], n, true);
-        m.of(args[3], n, true);
-        v.of(args[4], n, true);
+        p.of(args[1], n, true, "params");
+        g.of(args[2], n, true, "grads");
+        m.of(args[3], n, true, "m");
+        v.of(args[4], n, true, "v");
         const bool eight = n > 0 && tensor_of(m[0], "m").scalar_type() == at::kFloat8_e4m3fn;
         if (eight) {
-            m_scale.of(args[5], n, true);
-            v_scale.of(args[6], n, true);
+            m_scale.of(args[5], n, true, "m_scale");
+            v_scale.of(args[6], n, true, "v_scale");
+        } else {
+            m_scale.none(args[5], n, "m_scale");
+            v_scale.none(args[6], n, "v_scale");
         }
-        copy.of(args[7], n, false);
+        copy.of(args[7], n, false, "copy");
         const bool one_decay = PyFloat_Check(args[8]) || PyLong_Check(args[8]);
-        if (!one_decay) decay.of(args[8], n, true);
+        if (!one_decay) decay.of(args[8], n, true, "weight_decay");
         const double each_decay = one_decay ? PyFloat_AsDouble(args[8]) : 0.0;
         const at::ScalarType state = eight ? at::kFloat8_e4m3fn : at::kFloat;
         at::ScalarType grad_type = at::kFloat, copy_type = at::kFloat;

@@ -191,3 +191,28 @@ def test_an_infinity_takes_its_own_place_of_a_block_in_8_bits(bad):
     else:
         assert torch.equal(want[0][rest], got[0][rest]) and torch.equal(want[3], got[3])
         assert torch.equal(want[1].view(torch.uint8)[rest], got[1].view(torch.uint8)[rest])
+
+
+# --------------------------------------------------------------------------------------------- arguments, streams, errors
+def test_lists_of_an_update_are_lists():
+    """What is given and is no list of as many entries is refused, and so are scales beside moments in 32 bits: none is left out in silence."""
+    x = torch.zeros(4)
+    for bad in (5, True, object()):
+        with pytest.raises(ValueError, match="copy"):
+            binding.bagel_adamw_step([x], [x], [x], [x], 1, copy=bad)
+    with pytest.raises(ValueError, match="lists"):
+        binding.bagel_adamw_step([x], [x], [x], [x], 1, copy=[x, x])
+    for name in ("m_scale", "v_scale"):
+        for bad in ([x], 5, [x, x]):
+            with pytest.raises(ValueError, match=name):
+                binding.bagel_adamw_step([x], [x], [x], [x], 1, **{name: bad})
+
+
+@gpu
+def test_lists_of_an_update_are_lists_on_the_gpu():
+    x = [torch.zeros(4, device="cuda") for _ in range(5)]
+    with pytest.raises(ValueError, match="copy"):
+        binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, copy=5)
+    with pytest.raises(ValueError, match="m_scale"):
+        binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, m_scale=[x[4]], v_scale=[x[4]])
+    binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, m_scale=[None], v_scale=[None])       # nothing is there
