@@ -308,7 +308,8 @@ int bagel_profile_enable(bagel_ctx *ctx, int every);
 int bagel_profile_read(bagel_ctx *ctx, double *kernel_ms, int *launches);
 
 /* Message of the last error on this context ("" if none); valid until the next call on it.
- * With ctx == NULL: message of the last failed call without a context on this thread (bagel_create among them). */
+ * With ctx == NULL: message of the last failed call without a context on this thread (bagel_create among them); empty after a
+ * bagel_create or bagel_sample_eval_static that succeeded. */
 const char *bagel_last_error(const bagel_ctx *ctx);
 
 /*

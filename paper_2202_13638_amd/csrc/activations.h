@@ -8,7 +8,6 @@
 
 // Sets the message of bagel_last_error(NULL) on this thread and returns `code` (bagel_api.hip).
 int bagel_refuse(int code, const char *format, ...) __attribute__((format(printf, 2, 3)));
-void bagel_no_error();
 
 inline int bagel_type_bytes(int dtype) { return dtype == BAGEL_FLOAT32 ? 4 : 2; }
 inline bool bagel_type_ok(int dtype) { return dtype == BAGEL_FLOAT32 || dtype == BAGEL_BFLOAT16 || dtype == BAGEL_FLOAT16; }

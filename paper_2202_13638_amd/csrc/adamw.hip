@@ -312,6 +312,5 @@ extern "C" int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_ten
     }
     if (e == hipSuccess && a.n > 0) e = launch();
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_adamw_step: %s", hipGetErrorString(e));
-    bagel_no_error();
     return BAGEL_OK;
 }

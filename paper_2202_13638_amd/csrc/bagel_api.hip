@@ -34,8 +34,6 @@ int bagel_refuse(int code, const char *format, ...)
     return code;
 }
 
-void bagel_no_error() { g_create_err[0] = 0; }
-
 static const char *check_dims(const bagel_dims *d)
 {
     if (d->d_s < 1 || d->d_s > BAGEL_MAX_STATE) return "d_s must be in 1..8";

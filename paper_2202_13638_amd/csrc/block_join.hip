@@ -611,7 +611,6 @@ extern "C" int bagel_block_join(const bagel_join *j, void *hip_stream)
         const hipError_t e = bagel_by_type(j->dtype, [&](auto t) { return launch_join<typename decltype(t)::type>(*j, (hipStream_t)hip_stream); });
         if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_block_join: %s", hipGetErrorString(e));
     }
-    bagel_no_error();
     return BAGEL_OK;
 }
 
@@ -620,6 +619,5 @@ extern "C" int bagel_block_join_grad(const bagel_join *j, void *hip_stream)
     if (const char *msg = check_join(j, true)) return bagel_refuse(BAGEL_EINVAL, "bagel_block_join_grad: %s", msg);
     const hipError_t e = bagel_by_type(j->dtype, [&](auto t) { return launch_join_grad<typename decltype(t)::type>(*j, (hipStream_t)hip_stream); });
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_block_join_grad: %s", hipGetErrorString(e));
-    bagel_no_error();
     return BAGEL_OK;
 }

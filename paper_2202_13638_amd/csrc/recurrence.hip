@@ -792,7 +792,6 @@ extern "C" int bagel_recurrence(const bagel_gated_recurrence *r, void *hip_strea
     if (const char *msg = check_recurrence(r, false)) return bagel_refuse(BAGEL_EINVAL, "bagel_recurrence: %s", msg);
     const hipError_t e = bagel_by_type(r->dtype, [&](auto t) { return launch_forward<typename decltype(t)::type>(*r, (hipStream_t)hip_stream); });
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_recurrence: %s", hipGetErrorString(e));
-    bagel_no_error();
     return BAGEL_OK;
 }
 
@@ -801,7 +800,6 @@ extern "C" int bagel_recurrence_grad(const bagel_gated_recurrence *r, void *hip_
     if (const char *msg = check_recurrence(r, true)) return bagel_refuse(BAGEL_EINVAL, "bagel_recurrence_grad: %s", msg);
     const hipError_t e = bagel_by_type(r->dtype, [&](auto t) { return launch_grad<typename decltype(t)::type>(*r, (hipStream_t)hip_stream); });
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_recurrence_grad: %s", hipGetErrorString(e));
-    bagel_no_error();
     return BAGEL_OK;
 }
 
@@ -816,6 +814,5 @@ extern "C" int bagel_recurrence_step(const bagel_gated_recurrence *r, void *hip_
         const hipError_t e = bagel_by_type(r->dtype, [&](auto t) { return launch_step<typename decltype(t)::type>(*r, (hipStream_t)hip_stream); });
         if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_recurrence_step: %s", hipGetErrorString(e));
     }
-    bagel_no_error();
     return BAGEL_OK;
 }

@@ -2,6 +2,7 @@
 bits, arguments that have to be refused, and sizes at which a workgroup goes through several rows or blocks.
 
 Tolerances are those of test_operators.py where no other is derived."""
+import ctypes as C
 import pytest
 import torch
 import test_operators as ops
@@ -216,3 +217,15 @@ def test_lists_of_an_update_are_lists_on_the_gpu():
     with pytest.raises(ValueError, match="m_scale"):
         binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, m_scale=[x[4]], v_scale=[x[4]])
     binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, m_scale=[None], v_scale=[None])       # nothing is there
+
+
+def test_the_message_of_a_failed_call_stays():
+    lib = binding.load()
+    ctx = C.c_void_p()
+    assert lib.bagel_create(C.byref(ctx), None, None) == binding.EINVAL
+    message = lib.bagel_last_error(None)
+    assert message.startswith(b"bagel_create:")
+    o = binding._AdamW()
+    o.step, o.lr, o.eps, o.state_bits = 1, 1e-3, 1e-8, 32
+    assert lib.bagel_adamw_step(None, 0, C.byref(o), None) == binding.OK          # no tensors: nothing to do
+    assert lib.bagel_last_error(None) == message
