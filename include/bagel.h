@@ -327,7 +327,7 @@ const char *bagel_last_error(const bagel_ctx *ctx);
  * Activations are matrices of `rows` x `width` in one of three types, with rows a `stride` apart (in elements, at least the width
  * where there are several rows) and the entries of a row next to each other; any start and any stride is allowed, those that are multiples
  * of 16 bytes are faster.  Parameters, states that pass from step to step and their gradients are contiguous float32.  All
- * arithmetic is in float32; a result in 16 bits is rounded once, to nearest.  Matrices of one call may not overlap where one of them is
+ * arithmetic is in float32; a result in 16 bits is rounded once, to nearest.  Arrays of one call may not overlap where one of them is
  * written, but for the pairs that are named.  NaN and infinities are not screened; they stay within the row (join) or the sequence (recurrence)
  * that they come in, except in the gradients of the parameters, which are sums over all.
  */
@@ -388,7 +388,8 @@ int bagel_block_join_grad(const bagel_join *args, void *hip_stream);
  * sequences of equal length, `sequences` divides `rows`.  (Offsets that break these rules give wrong numbers, but no access
  * outside of the arrays.)
  *   initial[sequences][width]  h before the first step, NULL: zero
- *   final_state[sequences][width] or NULL: h after the last step; of an empty sequence, its initial state
+ *   final_state[sequences][width] or NULL: h after the last step; of an empty sequence, its initial state.  Not in the place of `initial`, nor d_initial in
+ *   that of d_final: the ones are read while the others are written (EINVAL)
  *   carry[bagel_recurrence_carry_rows(rows)][width] or NULL: what bagel_recurrence_grad needs of the forward pass, h before the
  *   rows 0, BAGEL_RECURRENCE_SPAN, 2 BAGEL_RECURRENCE_SPAN, ... (where a sequence begins there, anything finite)
  *

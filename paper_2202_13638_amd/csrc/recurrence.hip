@@ -758,6 +758,13 @@ const char *check_matrices(const bagel_gated_recurrence *r, int64_t rows, bool g
     return nullptr;
 }
 
+// States of all sequences that are read and such that are written: waves read the ones while others write the others.
+bool states_overlap(const bagel_gated_recurrence *r, const float *read, const float *written)
+{
+    const uintptr_t a = (uintptr_t)read, b = (uintptr_t)written, bytes = (uintptr_t)r->sequences * r->width * sizeof(float);
+    return read && written && (a < b ? b - a : a - b) < bytes;
+}
+
 const char *check_recurrence(const bagel_gated_recurrence *r, bool grad)
 {
     if (const char *msg = check_sizes(r)) return msg;
@@ -772,6 +779,8 @@ const char *check_recurrence(const bagel_gated_recurrence *r, bool grad)
         if (grad && !r->carry) return "the carry of the forward pass is needed";
         if (!r->workspace) return "a workspace is needed";
     }
+    if (!grad && states_overlap(r, r->initial, r->final_state)) return "initial and final_state overlap";
+    if (grad && states_overlap(r, r->d_final, r->d_initial)) return "d_final and d_initial overlap";
     if (r->workspace_bytes < bagel_recurrence_workspace(r->rows, r->width)) return "the workspace is too small";
     if ((uintptr_t)r->workspace & 15) return "the workspace must start at a multiple of 16 bytes";
     return check_matrices(r, r->rows, grad);

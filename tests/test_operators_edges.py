@@ -73,6 +73,15 @@ def test_a_value_that_replaces_a_large_state():
         assert bool(((got.double().cpu() - want).abs() <= (4 * z.abs() + 40) * ULP * want).all())
 
 
+def test_states_that_are_read_and_written_may_not_overlap():
+    """Waves read the states before a sequence while others write those behind it."""
+    for change in (dict(initial=0x20000, final=0x20000), dict(initial=0x20000, final=0x20000 + 4 * 63),
+                   dict(initial=0x20000 + 4 * 63, final=0x20000)):
+        ops._refused("bagel_recurrence", ops._recurrence_struct(rows=6, sequences=2, **change), "overlap")
+    for change in (dict(d_final=0x20000, d_initial=0x20000), dict(d_final=0x20000, d_initial=0x20000 + 4 * 63)):
+        ops._refused("bagel_recurrence_grad", ops._recurrence_struct(rows=6, sequences=2, **change), "overlap")
+
+
 # ------------------------------------------------------------------------------------------------------------- block join
 @gpu
 @pytest.mark.parametrize("dtype", ops.TYPES)
