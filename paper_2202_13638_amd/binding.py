@@ -217,6 +217,8 @@ _ACTS = {"none": 0, "identity": 1, "logistic": 2, "silu": 3}
 _JOIN_HEAD, _RECURRENCE_HEAD, _ADAMW_OPTIONS, _WORKSPACE = (struct.Struct(f) for f in ("qiiif", "qiii4xP", "qddddPiiiIi4x", "Pq"))
 assert (_JOIN_HEAD.size, _RECURRENCE_HEAD.size, _ADAMW_OPTIONS.size) == (_Join.branch.offset, _Recurrence.value.offset, C.sizeof(_AdamW))
 _NOTHING = bytes(256)
+_JOIN_FIELDS, _RECURRENCE_FIELDS = ("rows", "width", "dtype", "act", "eps"), ("rows", "width", "dtype", "offsets", "offsets")
+_ADAMW_FIELDS = ("step", "lr", "beta1", "beta2", "eps", "grad_scale", "grad_dtype", "copy_dtype", "state_bits", "seed", "draws")
 _torch = _marshal = _raw_stream = None
 
 
@@ -229,6 +231,26 @@ def _load():
         # the handle of the current stream, in 0.1 us where torch.cuda.current_stream() takes 2.7
         _raw_stream = getattr(_torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: _torch.cuda.current_stream(device).cuda_stream)
     return _lib or load()
+
+
+def _pack(form, fields, *values):
+    """The bytes of some fields; a ValueError that names the one that does not fit."""
+    try:
+        return form.pack(*values)
+    except (struct.error, OverflowError, TypeError):
+        for code, name, value in zip((c for c in form.format if c in "qifdPI"), fields, values):
+            try:
+                struct.pack(code, value)
+            except (struct.error, OverflowError, TypeError):
+                raise ValueError(f"{name} must be a {'number' if code in 'fd' else 'whole number'} that fits its field, not {value!r}") from None
+        raise
+
+
+def _whole(value, name):
+    try:
+        return int(value)
+    except (TypeError, ValueError, OverflowError):
+        raise ValueError(f"{name} must be a whole number, not {value!r}") from None
 
 
 def _stream(stream):
@@ -244,7 +266,7 @@ def _stream(stream):
 def _workspace(workspace, need, device, stream):
     """The caller's work space, or one from torch's allocator on the call's stream (`stream` as the caller gave it)."""
     if workspace is None:
-        if need == 0:
+        if need <= 0:                                                 # none, or sizes that the library refuses
             return None, bytes(16)
         if stream is None:
             workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
@@ -284,7 +306,7 @@ def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="no
     on, device = _stream(stream)
     like, name = (resid, "resid") if resid is not None else (branch, "branch")
     rows, width, code = _marshal.first(like, name, device)
-    args = (_JOIN_HEAD.pack(rows, width, code, kind, eps) + _marshal.matrices(like, _FORWARD, (branch, gate, resid, out, normed)) +
+    args = (_pack(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) + _marshal.matrices(like, _FORWARD, (branch, gate, resid, out, normed)) +
             _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) + _NOTHING)
     _done(lib, lib.bagel_block_join(args, on))
 
@@ -299,7 +321,7 @@ def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, 
     rows, width, code = _marshal.first(out, "out", device)
     sums = d_post_weight is not None or d_scale is not None or d_pre_weight is not None
     workspace, space = _workspace(workspace, lib.bagel_block_join_workspace(rows, width) if sums else 0, device, stream)
-    args = (_JOIN_HEAD.pack(rows, width, code, kind, eps) + _marshal.matrices(out, _FORWARD, (branch, gate, None, out, None)) +
+    args = (_pack(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) + _marshal.matrices(out, _FORWARD, (branch, gate, None, out, None)) +
             _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) +
             _marshal.matrices(out, _BACKWARD, (d_out, d_normed, d_branch, d_gate, d_resid)) +
             _marshal.vectors(device, (width,), _D_VECTORS, (d_post_weight, d_scale, d_pre_weight)) + space)
@@ -319,7 +341,7 @@ def bagel_recurrence_workspace(rows: int, width: int) -> int:
 def _sequences(offsets, device):
     """(number of sequences, pointer of their offsets): an int32 tensor on the GPU, or the number of sequences of equal length."""
     if not isinstance(offsets, _torch.Tensor):
-        return int(offsets), 0
+        return _whole(offsets, "offsets"), 0
     if offsets.dtype != _torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
         raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
     return offsets.numel() - 1, offsets.data_ptr()
@@ -338,7 +360,7 @@ def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None,
     rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
     workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = (_RECURRENCE_HEAD.pack(rows, width, code, n, at) +
+    args = (_pack(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), _needed(hidden, "hidden"))) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, final)) +
             _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (carry,)) + bytes(8 + 3 * 16 + 3 * 8) + space)
@@ -353,7 +375,7 @@ def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, c
     rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
     workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = (_RECURRENCE_HEAD.pack(rows, width, code, n, at) +
+    args = (_pack(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), None)) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, None)) +
             _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (_needed(carry, "carry"),)) + bytes(8) +
@@ -368,7 +390,7 @@ def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, strea
     lib = _load()
     on, device = _stream(stream)
     rows, width, code = _marshal.first(value, "value", device)
-    args = (_RECURRENCE_HEAD.pack(0, width, code, rows, 0) +
+    args = (_pack(_RECURRENCE_HEAD, ("", "width", "dtype", "rows", ""), 0, width, code, rows, 0) +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), hidden)) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + bytes(3 * 8) +
             _marshal.vectors(device, (rows, width), ("state",), (_needed(state, "state"),)) + _NOTHING)
@@ -393,8 +415,8 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
         if not isinstance(grad_scale, _torch.Tensor) or grad_scale.numel() != 1 or grad_scale.dtype != _torch.float32 or grad_scale.get_device() != device:
             raise ValueError("grad_scale must hold one float32 value and be on the current GPU")
         scale = grad_scale.data_ptr()
-    options = _ADAMW_OPTIONS.pack(int(step), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, (run if seed is None else int(seed)) & 0xFFFFFFFF,
-                                  seed is not None)
+    draws, given = (_whole(run, "run"), 0) if seed is None else (_whole(seed, "seed"), 1)
+    options = _pack(_ADAMW_OPTIONS, _ADAMW_FIELDS, _whole(step, "step"), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, draws & 0xFFFFFFFF, given)
     _done(lib, lib.bagel_adamw_step(table, n, options, on))
 
 

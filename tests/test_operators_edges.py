@@ -228,6 +228,28 @@ def test_lists_of_an_update_are_lists_on_the_gpu():
     binding.bagel_adamw_step([x[0]], [x[1]], [x[2]], [x[3]], 1, m_scale=[None], v_scale=[None])       # nothing is there
 
 
+@gpu
+def test_numbers_that_do_not_fit_are_refused():
+    x = torch.zeros(4, 8, device="cuda")
+    for offsets in (2 ** 31, 2 ** 40, 2 ** 70, -2 ** 40):
+        with pytest.raises(ValueError, match="offsets"):
+            binding.bagel_recurrence(x, x, torch.empty_like(x), offsets)
+    with pytest.raises(ValueError, match="eps"):
+        binding.bagel_block_join(x, x, torch.empty_like(x), eps="small")
+    with pytest.raises(binding.BagelError, match="eps"):             # infinite in 32 bits
+        binding.bagel_block_join(x, x, torch.empty_like(x), eps=1e60)
+    for kw in (dict(step=2 ** 70), dict(step="one"), dict(lr="fast"), dict(beta1=None), dict(seed=object()), dict(run="a")):
+        with pytest.raises(ValueError, match=next(iter(kw))):
+            binding.bagel_adamw_step(*[[torch.zeros(4, device="cuda")] for _ in range(4)], **{"step": 1, **kw})
+    # sizes beyond the library's, where a work space is to be made first: the library's own refusal
+    wide, vector = torch.zeros(1, 16400, device="cuda"), torch.zeros(16400, device="cuda")
+    with pytest.raises(binding.BagelError, match="width"):
+        binding.bagel_block_join_grad(wide, wide, wide, d_scale=vector)
+    wide = torch.zeros(1, 1 << 20, device="cuda")
+    with pytest.raises(binding.BagelError, match="width"):
+        binding.bagel_recurrence(wide, wide, torch.empty_like(wide), 1)
+
+
 def test_the_message_of_a_failed_call_stays():
     lib = binding.load()
     ctx = C.c_void_p()
