@@ -2,13 +2,21 @@
 bits, arguments that have to be refused, and sizes at which a workgroup goes through several rows or blocks.
 
 Tolerances are those of test_operators.py where no other is derived."""
+import concurrent.futures
 import ctypes as C
+import os
+import shutil
+import subprocess
+import sys
+
 import pytest
 import torch
+
 import test_operators as ops
 from paper_2202_13638_amd import binding
 
 gpu = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ULP = 2.0 ** -23
 
 
@@ -112,6 +120,78 @@ def _cuda(d):
     return {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in d.items()}
 
 
+def _close(got, want, name, terms=None):
+    """_near of test_operators.py, where the tensors are."""
+    w = want.double()
+    bound = ops.HALF_ULP[got.dtype] * w.abs() * 1.01 + ops.WORK * (w.abs().max() if terms is None else terms)
+    if got.dtype == torch.float16:
+        bound = bound + 2.0 ** -25
+    off = (got.double() - w).abs()
+    assert bool((off <= bound).all()), f"{name}: off by {float(off.max()):.3g}, at most {float((off - bound).max()):.3g} too much"
+
+
+# a width of every tile, in 32 bits; in 16 twice these (less one) fill the same tiles
+TILES = [3, 101, 253, 511, 777, 1021, 1277, 1301, 1533, 2045, 2056, 3001, 4093, 5001, 8192, 12001]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ops.TYPES)
+@pytest.mark.parametrize("width", TILES)
+def test_join_of_more_rows_than_there_are_places(width, dtype):
+    """Every tile with several rows to a workgroup: forward there are at most 4096 workgroups, back 512 or 1024, of one row or of four."""
+    t = ops.TYPES[dtype]
+    width = width if dtype == "f32" or width > 8192 else 2 * width - (width % 8 != 0)
+    packs = -(-width * t.itemsize // 16)
+    forward, back = (20011, 5003) if packs <= 128 else (4211, 1301)
+    act = ["silu", "logistic", "identity", "none"][(width + len(dtype)) % 4]
+    g = torch.Generator(device="cuda").manual_seed(width)
+
+    def normal(*shape, scale=1.0, mean=0.0, to=torch.float32):
+        return (torch.randn(shape, generator=g, device="cuda") * scale + mean).to(to)
+
+    x = dict(branch=normal(forward, width, scale=0.7, to=t), resid=normal(forward, width, scale=2.0, to=t),
+             gate=normal(forward, width, scale=1.5, to=t) if act != "none" else None, post_weight=normal(width, scale=0.2, mean=1.0),
+             scale=normal(width, scale=0.2, mean=0.3), pre_weight=normal(width, scale=0.2, mean=1.0))
+    vectors = {k: x[k] for k in ("post_weight", "scale", "pre_weight")}
+    out, normed = (torch.full((forward, width), float("nan"), dtype=t, device="cuda") for _ in range(2))
+    binding.bagel_block_join(x["branch"], x["resid"], out, normed, gate=x["gate"], act=act, eps=1e-5, **vectors)
+    w, c, u = (v.double() for v in vectors.values())
+
+    def norm(z):
+        return torch.rsqrt(z.square().mean(1, keepdim=True) + 1e-5)
+
+    z = x["branch"].double()
+    a, _ = ops._act(x["gate"].double() if act != "none" else None, act)
+    want = x["resid"].double() + c * w * z * norm(z) * (1.0 if a is None else a)
+    _close(out, want, "out")
+    _close(normed, want * norm(want) * u, "normed")
+    del normed, want, z, a
+    # back, by the formulas at the stored `out`; d_resid takes the place of d_out
+    x = {k: v[:back] if v is not None and v.dim() == 2 else v for k, v in x.items()}
+    out = out[:back]
+    d_out, d_normed = normal(back, width, to=t), normal(back, width, to=t)
+    o, z, dy, ro = out.double(), x["branch"].double(), d_normed.double(), norm(out.double())
+    a, da = ops._act(x["gate"].double() if act != "none" else None, act)
+    a, da = (torch.ones_like(z), torch.zeros_like(z)) if a is None else (a, da)
+    n_out, rz = o * ro, norm(z)
+    n = z * rz
+    d = ro * (dy * u - n_out * (dy * u * n_out).mean(1, keepdim=True))
+    dx = d_out.double() + d
+    k = dx * c * w * a
+    parts = d_out.double().abs() + d.abs() + 2 * (dy * u * ro).abs()
+    want = {"d_resid": dx, "d_branch": rz * (k - n * (k * n).mean(1, keepdim=True)), "d_post_weight": (dx * c * a * n).sum(0), "d_scale": (dx * w * a * n).sum(0),
+            "d_pre_weight": (dy * n_out).sum(0)}
+    terms = {"d_resid": parts.max(), "d_branch": 2 * (parts * c * w * a * rz).abs().max(), "d_post_weight": (parts * c * a * n).abs().sum(0),
+             "d_scale": (parts * w * a * n).abs().sum(0), "d_pre_weight": (dy * n_out).abs().sum(0)}
+    if act != "none":
+        want["d_gate"], terms["d_gate"] = dx * c * w * n * da, (parts * c * w * n * da).abs().max()
+    got = {k: torch.full(v.shape, float("nan"), dtype=t if v.dim() == 2 else torch.float32, device="cuda") for k, v in want.items()}
+    got["d_resid"] = d_out
+    binding.bagel_block_join_grad(x["branch"], out, d_out, d_normed, gate=x["gate"], act=act, eps=1e-5, **vectors, **got)
+    for k, v in want.items():
+        _close(got[k], v, k, terms[k])
+
+
 # ------------------------------------------------------------------------------------------------------------------ AdamW
 def _draws(step, n=1 << 14, tensors=2, **kw):
     """For every place of some tensors of the same values whether its code was rounded up; the chance of that is (0.37 * 448 - 160) / 16 = 0.36."""
@@ -203,6 +283,13 @@ def test_an_infinity_takes_its_own_place_of_a_block_in_8_bits(bad):
         assert torch.equal(want[1].view(torch.uint8)[rest], got[1].view(torch.uint8)[rest])
 
 
+@gpu
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_adamw_in_8_bits_of_four_blocks_a_wave(grad):
+    """From 16384 blocks on a wave takes four of them one after the other; the last block of the last is not whole."""
+    ops.test_adamw_in_8_bits((4_300_007,), grad)
+
+
 # --------------------------------------------------------------------------------------------- arguments, streams, errors
 def test_lists_of_an_update_are_lists():
     """What is given and is no list of as many entries is refused, and so are scales beside moments in 32 bits: none is left out in silence."""
@@ -260,3 +347,68 @@ def test_the_message_of_a_failed_call_stays():
     o.step, o.lr, o.eps, o.state_bits = 1, 1e-3, 1e-8, 32
     assert lib.bagel_adamw_step(None, 0, C.byref(o), None) == binding.OK          # no tensors: nothing to do
     assert lib.bagel_last_error(None) == message
+
+
+@gpu
+def test_work_spaces_on_another_stream():
+    """Without one of the caller's, a call on another stream makes its work space there."""
+    rows, width = 3000, 264
+    x, f, dh = (ops._normal((rows, width), i, torch.bfloat16).cuda() for i in (1, 2, 3))
+    j = _cuda(ops._join_inputs(rows, width, torch.bfloat16, "silu"))
+    rest = dict(act="silu", **{k: j[k] for k in ("gate", "post_weight", "scale", "pre_weight")})
+
+    def calls(stream):
+        r = [torch.zeros_like(x) for _ in range(4)]
+        vectors = {k: torch.zeros(width, device="cuda") for k in ("d_post_weight", "d_scale", "d_pre_weight")}
+        d_bias, carry = torch.zeros(width, device="cuda"), torch.zeros(binding.bagel_recurrence_carry_rows(rows), width, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(3):
+            binding.bagel_recurrence(x, f, r[0], 1, carry=carry, stream=stream)
+            binding.bagel_recurrence_grad(x, f, dh, r[1], r[2], 1, carry, d_bias=d_bias, stream=stream)
+            binding.bagel_block_join_grad(j["branch"], j["resid"], x, dh, d_branch=r[3], stream=stream, **vectors, **rest)
+        torch.cuda.synchronize()
+        return [*r, d_bias, *vectors.values()]
+
+    assert all(torch.equal(a, b) for a, b in zip(calls(None), calls(torch.cuda.Stream())))
+
+
+def test_first_calls_from_several_threads():
+    """The library is looked up by whoever comes first; nobody sees half of it."""
+    code = ("import threading, torch\nfrom paper_2202_13638_amd import binding\nx, got = torch.zeros(2, 2), []\nstart = threading.Barrier(8)\n"
+            "def call():\n    start.wait()\n    try:\n        binding.bagel_block_join(x, x, x)\n    except Exception as e:\n        got.append(type(e).__name__)\n"
+            "t = [threading.Thread(target=call) for _ in range(8)]\n[i.start() for i in t]\n[i.join() for i in t]\nprint(got)\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith(str(["ValueError"] * 8)), r.stdout + r.stderr
+
+
+@pytest.mark.slow
+def test_host_side_of_the_operators_under_sanitizers(tmp_path):
+    """AddressSanitizer and UndefinedBehaviorSanitizer on host code; device code as the library has it.  No GPU is involved."""
+    if shutil.which("hipcc") is None:
+        pytest.skip("hipcc not found")
+    from paper_2202_13638_amd import build
+    build.build()
+    units = ["adamw.hip", "bagel_api.hip", "block_join.hip", "recurrence.hip"]
+    san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+           "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
+    sources = [os.path.join(build.CSRC, u) for u in units] + [os.path.join(ROOT, "tests", "sanitize", "operators_driver.cpp")]
+
+    def compiled(source):
+        obj = str(tmp_path / (os.path.basename(source) + ".o"))
+        r = subprocess.run(["hipcc", *build.FLAGS, "-g", "-x", "hip", *san, "-c", source, "-o", obj], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr
+        return obj
+
+    with concurrent.futures.ThreadPoolExecutor(len(sources)) as pool:
+        objs = list(pool.map(compiled, sources))
+    objs += [os.path.join(build.BUILD, s.replace(".hip", ".o")) for s in build.SOURCES if s not in units]
+    exe = str(tmp_path / "operators_san")
+    r = subprocess.run(["hipcc", "--offload-arch=gfx950", "-fno-gpu-sanitize", "-fsanitize=address", "-fsanitize=undefined", "-o", exe, *objs],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    # the HIP runtime keeps allocations of its own to the end
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:halt_on_error=1", UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0 and "operators sanitizer driver: ok" in out, out
+    assert "ERROR: AddressSanitizer" not in out and "runtime error" not in out, out
