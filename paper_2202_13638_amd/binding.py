@@ -218,7 +218,7 @@ _JOIN_HEAD, _RECURRENCE_HEAD, _ADAMW_OPTIONS, _WORKSPACE = (struct.Struct(f) for
 assert (_JOIN_HEAD.size, _RECURRENCE_HEAD.size, _ADAMW_OPTIONS.size) == (_Join.branch.offset, _Recurrence.value.offset, C.sizeof(_AdamW))
 _NOTHING = bytes(256)
 _JOIN_FIELDS, _RECURRENCE_FIELDS = ("rows", "width", "dtype", "act", "eps"), ("rows", "width", "dtype", "offsets", "offsets")
-_ADAMW_FIELDS = ("step", "lr", "beta1", "beta2", "eps", "grad_scale", "grad_dtype", "copy_dtype", "state_bits", "seed", "draws")
+_STEP_FIELDS, _ADAMW_FIELDS = ("", "width", "dtype", "rows"), ("step", "lr", "beta1", "beta2", "eps", "grad_scale", "grads", "copy", "m")
 _torch = _marshal = _raw_stream = None
 
 
@@ -233,24 +233,17 @@ def _load():
     return _lib or load()
 
 
-def _pack(form, fields, *values):
-    """The bytes of some fields; a ValueError that names the one that does not fit."""
-    try:
-        return form.pack(*values)
-    except (struct.error, OverflowError, TypeError):
-        for code, name, value in zip((c for c in form.format if c in "qifdPI"), fields, values):
-            try:
-                struct.pack(code, value)
-            except (struct.error, OverflowError, TypeError):
-                raise ValueError(f"{name} must be a {'number' if code in 'fd' else 'whole number'} that fits its field, not {value!r}") from None
-        raise
+_UNFIT = (struct.error, OverflowError, TypeError, ValueError)
 
 
-def _whole(value, name):
-    try:
-        return int(value)
-    except (TypeError, ValueError, OverflowError):
-        raise ValueError(f"{name} must be a whole number, not {value!r}") from None
+def _unfit(form, fields, *values):
+    """What is wrong with values that could not be packed: a ValueError that names the first of them that does not fit its field."""
+    for code, name, value in zip((c for c in form.format if c in "qifdPI"), fields, values):
+        try:
+            struct.pack(code, value if code in "fd" else int(value) & 0xFFFFFFFF if code == "I" else int(value))
+        except _UNFIT:
+            return ValueError(f"{name} must be a {'number' if code in 'fd' else 'whole number'} that fits its field, not {value!r}")
+    return ValueError("an argument does not fit its field")
 
 
 def _stream(stream):
@@ -306,7 +299,11 @@ def bagel_block_join(branch, resid, out=None, normed=None, *, gate=None, act="no
     on, device = _stream(stream)
     like, name = (resid, "resid") if resid is not None else (branch, "branch")
     rows, width, code = _marshal.first(like, name, device)
-    args = (_pack(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) + _marshal.matrices(like, _FORWARD, (branch, gate, resid, out, normed)) +
+    try:
+        head = _JOIN_HEAD.pack(rows, width, code, kind, eps)
+    except _UNFIT:
+        raise _unfit(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) from None
+    args = (head + _marshal.matrices(like, _FORWARD, (branch, gate, resid, out, normed)) +
             _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) + _NOTHING)
     _done(lib, lib.bagel_block_join(args, on))
 
@@ -321,7 +318,11 @@ def bagel_block_join_grad(branch, out, d_out=None, d_normed=None, *, gate=None, 
     rows, width, code = _marshal.first(out, "out", device)
     sums = d_post_weight is not None or d_scale is not None or d_pre_weight is not None
     workspace, space = _workspace(workspace, lib.bagel_block_join_workspace(rows, width) if sums else 0, device, stream)
-    args = (_pack(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) + _marshal.matrices(out, _FORWARD, (branch, gate, None, out, None)) +
+    try:
+        head = _JOIN_HEAD.pack(rows, width, code, kind, eps)
+    except _UNFIT:
+        raise _unfit(_JOIN_HEAD, _JOIN_FIELDS, rows, width, code, kind, eps) from None
+    args = (head + _marshal.matrices(out, _FORWARD, (branch, gate, None, out, None)) +
             _marshal.vectors(device, (width,), _VECTORS, (post_weight, scale, pre_weight)) +
             _marshal.matrices(out, _BACKWARD, (d_out, d_normed, d_branch, d_gate, d_resid)) +
             _marshal.vectors(device, (width,), _D_VECTORS, (d_post_weight, d_scale, d_pre_weight)) + space)
@@ -341,7 +342,10 @@ def bagel_recurrence_workspace(rows: int, width: int) -> int:
 def _sequences(offsets, device):
     """(number of sequences, pointer of their offsets): an int32 tensor on the GPU, or the number of sequences of equal length."""
     if not isinstance(offsets, _torch.Tensor):
-        return _whole(offsets, "offsets"), 0
+        try:
+            return int(offsets), 0
+        except _UNFIT:
+            raise ValueError(f"offsets must be an int32 tensor or the number of sequences, not {offsets!r}") from None
     if offsets.dtype != _torch.int32 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.get_device() != device:
         raise ValueError(f"offsets must be a contiguous int32 tensor of one dimension on cuda:{device}, or the number of sequences")
     return offsets.numel() - 1, offsets.data_ptr()
@@ -360,7 +364,11 @@ def bagel_recurrence(value, forget, hidden, offsets, *, bias=None, initial=None,
     rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
     workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = (_pack(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) +
+    try:
+        head = _RECURRENCE_HEAD.pack(rows, width, code, n, at)
+    except _UNFIT:
+        raise _unfit(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) from None
+    args = (head +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), _needed(hidden, "hidden"))) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, final)) +
             _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (carry,)) + bytes(8 + 3 * 16 + 3 * 8) + space)
@@ -375,7 +383,11 @@ def bagel_recurrence_grad(value, forget, d_hidden, d_value, d_forget, offsets, c
     rows, width, code = _marshal.first(value, "value", device)
     n, at = _sequences(offsets, device)
     workspace, space = _workspace(workspace, lib.bagel_recurrence_workspace(rows, width), device, stream)
-    args = (_pack(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) +
+    try:
+        head = _RECURRENCE_HEAD.pack(rows, width, code, n, at)
+    except _UNFIT:
+        raise _unfit(_RECURRENCE_HEAD, _RECURRENCE_FIELDS, rows, width, code, n, at) from None
+    args = (head +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), None)) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + _marshal.vectors(device, (n, width), ("initial", "final"), (initial, None)) +
             _marshal.vectors(device, (lib.bagel_recurrence_carry_rows(rows), width), ("carry",), (_needed(carry, "carry"),)) + bytes(8) +
@@ -390,7 +402,11 @@ def bagel_recurrence_step(value, forget, state, hidden=None, *, bias=None, strea
     lib = _load()
     on, device = _stream(stream)
     rows, width, code = _marshal.first(value, "value", device)
-    args = (_pack(_RECURRENCE_HEAD, ("", "width", "dtype", "rows", ""), 0, width, code, rows, 0) +
+    try:
+        head = _RECURRENCE_HEAD.pack(0, width, code, rows, 0)
+    except _UNFIT:
+        raise _unfit(_RECURRENCE_HEAD, _STEP_FIELDS, 0, width, code, rows, 0) from None
+    args = (head +
             _marshal.matrices(value, ("value", "forget", "hidden"), (value, _needed(forget, "forget"), hidden)) +
             _marshal.vectors(device, (width,), ("bias",), (bias,)) + bytes(3 * 8) +
             _marshal.vectors(device, (rows, width), ("state",), (_needed(state, "state"),)) + _NOTHING)
@@ -415,8 +431,12 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
         if not isinstance(grad_scale, _torch.Tensor) or grad_scale.numel() != 1 or grad_scale.dtype != _torch.float32 or grad_scale.get_device() != device:
             raise ValueError("grad_scale must hold one float32 value and be on the current GPU")
         scale = grad_scale.data_ptr()
-    draws, given = (_whole(run, "run"), 0) if seed is None else (_whole(seed, "seed"), 1)
-    options = _pack(_ADAMW_OPTIONS, _ADAMW_FIELDS, _whole(step, "step"), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, draws & 0xFFFFFFFF, given)
+    draws, given = (run, 0) if seed is None else (seed, 1)
+    try:
+        options = _ADAMW_OPTIONS.pack(int(step), lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, int(draws) & 0xFFFFFFFF, given)
+    except _UNFIT:
+        fields = _ADAMW_FIELDS + ("run" if seed is None else "seed",)
+        raise _unfit(_ADAMW_OPTIONS, fields, step, lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, draws) from None
     _done(lib, lib.bagel_adamw_step(table, n, options, on))
 
 

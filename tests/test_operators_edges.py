@@ -318,7 +318,7 @@ def test_lists_of_an_update_are_lists_on_the_gpu():
 @gpu
 def test_numbers_that_do_not_fit_are_refused():
     x = torch.zeros(4, 8, device="cuda")
-    for offsets in (2 ** 31, 2 ** 40, 2 ** 70, -2 ** 40):
+    for offsets in (2 ** 31, 2 ** 40, 2 ** 70, -2 ** 40, "two", None):
         with pytest.raises(ValueError, match="offsets"):
             binding.bagel_recurrence(x, x, torch.empty_like(x), offsets)
     with pytest.raises(ValueError, match="eps"):
