@@ -165,6 +165,9 @@ def load():
         L.bagel_adamw_step.argtypes = [vp, C.c_int32, vp, vp]
         L.bagel_last_error.restype = C.c_char_p
         L.bagel_last_error.argtypes = [vp]
+        # The message is thread-local.  Until a thread has touched it, glibc looks up the thread-local data of every library the long way, the
+        # HIP runtime's too: 0.27 us of a launch.
+        L.bagel_last_error(None)
         _lib = L
     return _lib
 
