@@ -245,13 +245,15 @@ template <bool SOME> __device__ __forceinline__ float mixed(float q, float x, fl
 template <bool SOME> __device__ __forceinline__ float left(float q, float g) { return fmaf(-q, g, where_open<SOME>(q, 0.0f, g)); }
 __device__ __forceinline__ float at(const float *p, int64_t i) { return p ? p[i] : 0.0f; }
 
-// f(special, whether a gate is open) with constants: 0 special rows where there are none, as most segments lie within one sequence and a branch at every row costs them a
-// tenth, and no open gates where there are none: with them 131072 x 1024 bf16 takes 225 and 320 us, without 214 and 303.
+// f(special, whether a gate is open) with constants: 0 special rows where there are none, as most segments lie within one sequence and a branch at every row costs
+// them a tenth, and no open gates where there are none (131072 x 1024 bf16: 209 and 297 us, and 220 and 309 where many gates are open).
 template <typename F> __device__ __forceinline__ void by_rows(uint64_t special, bool open, F &&f)
 {
-    if (special != 0) f(special, std::true_type());
-    else if (open) f(std::integral_constant<uint64_t, 0>(), std::true_type());
-    else f(std::integral_constant<uint64_t, 0>(), std::false_type());
+    const std::integral_constant<uint64_t, 0> none;
+    if (special != 0 && open) f(special, std::true_type());
+    else if (special != 0) f(special, std::false_type());
+    else if (open) f(none, std::true_type());
+    else f(none, std::false_type());
 }
 
 // What is the same in both directions: which span and channels a workgroup has, and its reads.
