@@ -223,7 +223,7 @@ template <int BITS, bool WHOLE> __device__ __forceinline__ void update_block(con
 
 // A wave takes a block of 256 at a time, four entries a lane: the block's largest magnitude is a matter of one wave.  Every byte is read and written once, and
 // memory bounds it: 64 tensors, 33.6 million values, 32 bits, gradients and copy in bf16: 179 us, 5.3 TB/s; 404 million values in 8 bits: 1280 us, 5.1
-// TB/s.  Six small tensors take 4.1 us, latency.
+// TB/s.  Six small tensors take 3.9 us, latency.
 template <int BITS> __global__ __launch_bounds__(256) void adamw_kernel(adamw_args a)
 {
     const float gs = a.grad_scale ? a.grad_scale[0] : 1.0f;

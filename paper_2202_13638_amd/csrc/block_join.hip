@@ -26,8 +26,8 @@ template <typename T> struct join_args {
                                  // without w) and of d_normed out ro (d_pre_weight)
 };
 
-// act(g) and its derivative.  For an infinite g the logistic function is 0 or 1 exactly and its derivative 0.  silu of minus infinity and its derivative are 0, their limits: a
-// gate that is shut for good takes its entry of the branch out.  (silu of plus infinity is infinite, and so is the row of `out`.)  The reciprocal is the
+// act(g) and its derivative.  For an infinite g the logistic function is 0 or 1 exactly and its derivative 0.  silu of minus infinity and its derivative
+// are 0, their limits: a gate that is shut for good takes its entry of the branch out.  (silu of plus infinity is infinite, and `out` with it.)  The reciprocal is the
 // hardware's, off by one unit in the last place at most: a division takes ten instructions an entry, and in 16 bits these kernels are near the rate of the
 // arithmetic (65536 x 4096 back: 844 us with it, 807 without; 20000 x 2500 forward: 131 and 113).
 __device__ __forceinline__ float act(int kind, float g, float &slope)
@@ -338,7 +338,8 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads), ON_SIMD) void 
 }
 
 // Rows that registers do not hold (sixteen waves leave 128 to a lane): three passes over a row, the second and third out of the cache, and the sums
-// of a workgroup in its part of the work space.  8192 x 16384 f32 997 us, 4.3 TB/s of what has to be moved.
+// of a workgroup in its part of the work space, read and written for every row.  8192 x 16384 f32 2200 us, 2.0 TB/s of what has to be moved (1600 us without
+// the gradients of the vectors), in bf16 2870 and 1880 us: far from the bound, which is 842 and 421 us.
 template <typename T, int V, bool GATED> __global__ __launch_bounds__(1024) void join_grad_wide_kernel(join_args<T> a)
 {
     __shared__ float shared[2][16][4];
@@ -526,7 +527,8 @@ template <typename T, int V> int launch_wide(const join_args<T> &a, hipStream_t 
 // 16384 x 3001: 216, 202).  Forward two packs on four waves and one on eight are alike.
 //   Up to 1024, two packs on eight waves (16384 x 8192: 257 / 441, one on sixteen 335 / 645; 16384 x 4096 in f32 258 / 409, 246 / 417), which back up
 // to 768 go by what is not there (16384 x 4200: 297, 340; 16384 x 6000: 344, 383; 16384 x 8192: 446, 433).
-//   Above, what sixteen waves can hold, and for the way back of wider rows three passes over a row.
+//   Above, what sixteen waves can hold (back only in f32, where a gated tile spills 33 registers: 8192 x 4200 354 us, 3.1 TB/s, 8192 x 8192 500 us, 4.3
+// TB/s), and for the way back of wider rows three passes over a row.
 template <typename T> int launch_rows(const join_args<T> &a, bool grad, hipStream_t stream)
 {
     constexpr int V = 16 / sizeof(T);

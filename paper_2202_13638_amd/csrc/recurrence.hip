@@ -12,10 +12,10 @@
 // it in registers.  The waves sum up their segments, the workgroup its span, and publishes that; the state before the span comes from
 // what the spans before it published, and the rows are gone through once more, in registers, from there.
 //   A published sum is one word of 64 bits a channel, A and H: it is whole as soon as it is there, and nothing else has to be ordered with it.
-//   Memory is the bound that there has to be: 3 and 5 entries moved for a dozen operations each.  131072 x 1024 in f32 is there (302 us forward and 489 back, 5.3 and
-// 5.5 TB/s).  In 16 bits a workgroup moves half as much for the same waits, and a workgroup's life is what bounds it (131072 x 1024 in bf16 212 us and
-// 303 us, 3.8 and 4.4 TB/s; of its 12.3 us forward 3.6 us go by until its rows are there, 2 in its sums, 4.2 in publishing and looking
-// back; without looking back the two took 189 and 275 us).  q, x and the gradient stay in registers in the meantime, which is why two workgroups and no
+//   Memory is the bound that there has to be: 3 and 5 entries moved for a dozen operations each.  131072 x 1024 in f32 is there (304 us forward and 492 back, 5.3 and
+// 5.4 TB/s).  In 16 bits a workgroup moves half as much for the same waits, and a workgroup's life is what bounds it (131072 x 1024 in bf16 209 us and
+// 297 us, 3.8 and 4.5 TB/s; of some 12 us forward 3.6 us go by until its rows are there, 2 in its sums, 4.2 in publishing and looking
+// back; without looking back the two took 21 and 28 us less).  q, x and the gradient stay in registers in the meantime, which is why two workgroups and no
 // more share a compute unit.
 //   Spans are handed out by a counter in the order in which they depend on each other.  So a workgroup waits only for spans handed out before
 //   its own, to workgroups that run already and publish their sums before they wait for anything: every wait ends.
@@ -225,9 +225,9 @@ template <typename A> __device__ __forceinline__ void to_previous(const A &a, in
     sequence = max(sequence, 0);
 }
 
-// The share q of a forget gate f and bias b.  They are added first: they may be large and cancel, and a rounding of b log2(e) would stay.  1 - q is formed from q as long as that leaves enough of it: a unit of q
-// is 8 units of 1 - q at 15/16, but 3 % of it at 1 - e^-13, and from e^-17 on nothing is left.  Of a gate that is open further than 15/16, 1 - q is kept in the place of
-// q, from the exponential, with a minus (also of zero).
+// The share q of a forget gate f and bias b.  They are added first: they may be large and cancel, and a rounding of b log2(e) would stay.
+// 1 - q is formed from q as long as that leaves enough of it: a unit of q is 8 units of 1 - q at 15/16, but 3 % of it at 1 - e^-13, and from 1 - e^-17 on
+// nothing is left.  Of a gate that is open further than 15/16, 1 - q is kept in the place of q, from the exponential, with a minus (also of zero).
 constexpr float LOG2E = 1.44269504f, OPEN = 0.9375f;
 __device__ __forceinline__ float gate(float f, float b) { return __builtin_amdgcn_exp2f((f + b) * LOG2E); }
 __device__ __forceinline__ float share(float f, float b) { return __builtin_amdgcn_rcpf(1.0f + gate(f, b)); }
@@ -648,7 +648,8 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float *sums, int spans
     d_bias[ch] = v;
 }
 
-// A row of each of many sequences, a thread to an entry: 2.9 us for 256 x 512 in bf16, all of it latency.
+// A row of each of many sequences, a thread to an entry: 2.7 us for 256 x 512 in bf16, all of it latency; 32768 x 4096 347 us in bf16 and f16, 479 us in f32, 131072 x
+// 777 bf16 268 us, 5.3 to 5.6 TB/s, which is the rate of a copy: memory bounds it, and wider loads would have nothing to win.
 template <typename T>
 __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int width, bagel_rows<T> value, bagel_rows<T> forget, bagel_rows<T> hidden,
                                                    const float *bias, float *state)
