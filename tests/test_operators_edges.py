@@ -67,6 +67,23 @@ def test_gradients_of_gates_that_are_nearly_open(width, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_channels_beside_an_open_gate_have_the_same_bits(dtype):
+    """Waves without an open gate go through other loops than waves with one."""
+    t, width, at = ops.TYPES[dtype], 200, [0, 300, 300, 900, 1500]
+    x, f, dh = (ops._normal((at[-1], width), i, t, 0.5).cuda() for i in (1, 2, 3))
+    bias, h0, dl = ops._normal((width,), 4, mean=6.0, scale=0.2).cuda(), ops._normal((4, width), 5).cuda(), ops._normal((4, width), 6).cuda()
+    a = ops._run_recurrence(x, f, at, bias, h0, dh, dl)
+    open_ones = torch.tensor([5, 131, 199], device="cuda")
+    bias[open_ones] = -9.0
+    b = ops._run_recurrence(x, f, at, bias, h0, dh, dl)
+    rest = torch.ones(width, dtype=torch.bool, device="cuda")
+    rest[open_ones] = False
+    for k in a:
+        assert torch.equal(a[k][..., rest], b[k][..., rest]), k
+
+
+@gpu
 def test_a_value_that_replaces_a_large_state():
     """A state of 1e4 gives way to a value of a thousandth: what is left is the value and (1 - q) of the state, each to a rounding and to what the gate carries."""
     width = 64
