@@ -479,6 +479,116 @@ typedef struct {
 
 int bagel_adamw_step(const bagel_adamw_tensor *tensors, int32_t n_tensors, const bagel_adamw *options, void *hip_stream);
 
+/*
+ * Layer norm of every row, or of each of `groups` equal parts of a row on its own (the heads of a block; `groups` divides the width): over a part of n entries
+ *   y = (x - m) / sqrt(v + eps) * weight + bias,   m = sum(x) / n,   v = sum((x - m)^2) / n
+ * weight[width] and bias[width] that are NULL stand for ones and zeros.  `out` may be `x` itself.
+ *
+ * bagel_layer_norm_grad: from x, weight and d_out (the gradient for out), d_x, d_weight[width] and d_bias[width], any of which may be left out.
+ * `out`, `bias` are not read.  d_x may be d_out or x itself.  d_weight and d_bias are sums over all rows in an order that depends on the sizes alone.
+ * rows >= 0, 1 <= width <= BAGEL_NORM_MAX_WIDTH, eps > 0.  Errors: EINVAL, EHIP.
+ */
+#define BAGEL_NORM_MAX_WIDTH 16384
+
+typedef struct {
+    int64_t rows;
+    int32_t width, dtype, groups;
+    float eps;
+    bagel_matrix x, out;
+    const float *weight, *bias;
+    /* gradients (not looked at by bagel_layer_norm) */
+    bagel_matrix d_out, d_x;
+    float *d_weight, *d_bias;
+    void *workspace;         /* needed for d_weight and d_bias */
+    int64_t workspace_bytes;
+} bagel_norm;
+
+int64_t bagel_layer_norm_workspace(int64_t rows, int32_t width, int32_t groups);
+int bagel_layer_norm(const bagel_norm *args, void *hip_stream);
+int bagel_layer_norm_grad(const bagel_norm *args, void *hip_stream);
+
+/*
+ * Linear attention with a decay for every head, over `sequences` sequences packed one after the other in the rows (offsets as in bagel_recurrence: int32 on the
+ * device, or NULL for sequences of equal length).  A head of queries belongs to a memory, `states` of which are shared by `heads` heads of queries in equal
+ * parts: head h reads memory h / (heads / states).  Along a sequence, for every memory and its heads,
+ *   S_t = decay S_{t-1} + key_t value_t^T,   out_t = scale S_t^T query_t,   decay = exp(log_decay)
+ *   query[rows][heads][key_width], key[rows][states][key_width], value[rows][states][value_width], out[rows][heads][value_width]: the entries of a
+ *     head are next to each other, rows and heads any distances apart (in elements, >= 0; heads and rows of a result may not overlap); any start is
+ *     allowed, distances and starts of 16 bytes are faster
+ *   log_decay[states], at most 0 (minus infinity: nothing is remembered; a constant of the head, it has no gradient)
+ *   initial[sequences][states][key_width][value_width]  S before the first row, NULL: zero
+ *   final_state of the same shape or NULL: S after the last row; of an empty sequence, its initial state.  Not in the place of `initial`, nor d_initial
+ *     in that of d_final (EINVAL)
+ * Rows behind the last sequence: what they hold is not used, and their results are zero.  Products take their operands in the type of the activations, which
+ * for sums within a chunk of rows means one rounding of what is multiplied; the memories, their sums and decays are in float32.
+ * (Offsets that break their rules give wrong numbers, but no access outside of the arrays.)
+ *
+ * bagel_linear_attention_grad: from the same inputs, d_out (the gradient for out) and d_final (for final_state, NULL: zero): d_query, d_key, d_value of the shapes of
+ * query, key and value, and d_initial, any of which may be left out.  Gradients of a shared memory's key and value are sums over its heads.  Nothing of the
+ * forward pass is needed.
+ *
+ * bagel_linear_attention_step: one row of each of `sequences` sequences (rows = sequences; offsets, initial and final_state are not looked at);
+ * state[sequences][states][key_width][value_width] is updated in place.
+ * rows >= 0; heads, states >= 1, states divides heads, heads <= 4096; 1 <= key_width, value_width <= BAGEL_ATTENTION_MAX_WIDTH; rows and sequences below
+ * 2^28, and their sum times states below 2^31.  Work space as of bagel_linear_attention_workspace (the step needs none).  Errors: EINVAL, EHIP.
+ */
+#define BAGEL_ATTENTION_MAX_WIDTH 128
+
+typedef struct {
+    void *data;              /* device pointer, or NULL for what is left out */
+    int64_t stride, head;    /* elements from one row to the next, and from one head to the next */
+} bagel_heads;
+
+typedef struct {
+    int64_t rows;
+    int32_t key_width, value_width, heads, states, dtype, sequences;
+    float scale;
+    const int32_t *offsets;
+    const float *log_decay;
+    bagel_heads query, key, value, out;
+    const float *initial;
+    float *final_state;
+    float *state;                            /* bagel_linear_attention_step only */
+    /* gradients (looked at by bagel_linear_attention_grad only) */
+    bagel_heads d_out, d_query, d_key, d_value;
+    const float *d_final;
+    float *d_initial;
+    void *workspace;                         /* bagel_linear_attention and bagel_linear_attention_grad */
+    int64_t workspace_bytes;
+} bagel_attention;
+
+int64_t bagel_linear_attention_workspace(const bagel_attention *args, int32_t grad);    /* sizes alone are looked at; grad: whether for the gradient */
+int bagel_linear_attention(const bagel_attention *args, void *hip_stream);
+int bagel_linear_attention_grad(const bagel_attention *args, void *hip_stream);
+int bagel_linear_attention_step(const bagel_attention *args, void *hip_stream);
+
+/*
+ * The norm of the gradients of many tensors together, and their clipping:
+ *   norm[0] = |grad_scale[0]| sqrt(sum of g^2 over all tensors),   factor[0] = grad_scale[0] min(1, max_norm / (norm + eps)),   out = g * factor
+ * grad_scale is a device scalar, NULL: one.  factor is what bagel_adamw_step takes as its grad_scale, and no gradient needs to be written then: out may be
+ * NULL, for some tensors or all.  out may be the gradient itself.  Where the norm is not finite, factor is NaN (bagel_adamw_step then changes nothing) and
+ * out is left as it was.  Squares and sums are in float64: a norm is finite wherever float32 holds it.  The sum has an order that depends on the counts alone.
+ * The tensors are an array on the host, read before the call returns; any number, of any count >= 0, at any alignment of their type.
+ * Work space: bagel_clip_norm_workspace(n_tensors) bytes.  max_norm >= 0 (infinity: no clipping), eps > 0.  Errors: EINVAL, EHIP.
+ */
+typedef struct {
+    const void *grad;
+    void *out;
+    int64_t count;
+} bagel_clip_tensor;
+
+typedef struct {
+    int32_t dtype;
+    float max_norm, eps;
+    const float *grad_scale;
+    float *norm, *factor;
+    void *workspace;
+    int64_t workspace_bytes;
+} bagel_clip;
+
+int64_t bagel_clip_norm_workspace(int32_t n_tensors);
+int bagel_clip_norm(const bagel_clip_tensor *tensors, int32_t n_tensors, const bagel_clip *options, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,7 +26,10 @@ EXPORTS = ["bagel_num_params", "bagel_create", "bagel_destroy", "bagel_workspace
            "bagel_profile_enable", "bagel_profile_read", "bagel_sample_eval_static",
            "bagel_block_join", "bagel_block_join_grad", "bagel_block_join_workspace",
            "bagel_recurrence", "bagel_recurrence_grad", "bagel_recurrence_step", "bagel_recurrence_workspace",
-           "bagel_recurrence_carry_rows", "bagel_adamw_step"]
+           "bagel_recurrence_carry_rows", "bagel_adamw_step",
+           "bagel_layer_norm", "bagel_layer_norm_grad", "bagel_layer_norm_workspace",
+           "bagel_linear_attention", "bagel_linear_attention_grad", "bagel_linear_attention_step", "bagel_linear_attention_workspace",
+           "bagel_clip_norm", "bagel_clip_norm_workspace"]
 
 
 class BagelError(RuntimeError):
@@ -104,6 +107,33 @@ class _AdamW(C.Structure):
                 ("seed", C.c_uint32), ("draws", C.c_int32)]
 
 
+class _Norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("groups", C.c_int32), ("eps", C.c_float),
+                *_matrices("x", "out"), ("weight", C.c_void_p), ("bias", C.c_void_p), *_matrices("d_out", "d_x"),
+                ("d_weight", C.c_void_p), ("d_bias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+def _heads(*names):
+    return [f for n in names for f in ((n, C.c_void_p), (n + "_stride", C.c_int64), (n + "_head", C.c_int64))]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("key_width", C.c_int32), ("value_width", C.c_int32), ("heads", C.c_int32), ("states", C.c_int32),
+                ("dtype", C.c_int32), ("sequences", C.c_int32), ("scale", C.c_float), ("offsets", C.c_void_p), ("log_decay", C.c_void_p),
+                *_heads("query", "key", "value", "out"), ("initial", C.c_void_p), ("final", C.c_void_p), ("state", C.c_void_p),
+                *_heads("d_out", "d_query", "d_key", "d_value"), ("d_final", C.c_void_p), ("d_initial", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class _ClipTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64)]
+
+
+class _Clip(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("max_norm", C.c_float), ("eps", C.c_float), ("grad_scale", C.c_void_p), ("norm", C.c_void_p),
+                ("factor", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 _lib = None
 
 
@@ -163,6 +193,14 @@ def load():
             getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [vp, vp]
         L.bagel_adamw_step.restype = C.c_int
         L.bagel_adamw_step.argtypes = [vp, C.c_int32, vp, vp]
+        L.bagel_layer_norm_workspace.restype = L.bagel_linear_attention_workspace.restype = L.bagel_clip_norm_workspace.restype = C.c_int64
+        L.bagel_layer_norm_workspace.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+        L.bagel_linear_attention_workspace.argtypes = [vp, C.c_int32]
+        L.bagel_clip_norm_workspace.argtypes = [C.c_int32]
+        for name in ("bagel_layer_norm", "bagel_layer_norm_grad", "bagel_linear_attention", "bagel_linear_attention_grad", "bagel_linear_attention_step"):
+            getattr(L, name).restype, getattr(L, name).argtypes = C.c_int, [vp, vp]
+        L.bagel_clip_norm.restype = C.c_int
+        L.bagel_clip_norm.argtypes = [vp, C.c_int32, vp, vp]
         L.bagel_last_error.restype = C.c_char_p
         L.bagel_last_error.argtypes = [vp]
         # The message is thread-local.  Until a thread has touched it, glibc looks up the thread-local data of every library the long way, the
@@ -441,6 +479,135 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
         fields = _ADAMW_FIELDS + ("run" if seed is None else "seed",)
         raise _unfit(_ADAMW_OPTIONS, fields, step, lr, beta1, beta2, eps, scale, grad_type, copy_type, bits, draws) from None
     _done(lib, lib.bagel_adamw_step(table, n, options, on))
+
+
+NORM_MAX_WIDTH, ATTENTION_MAX_WIDTH = 16384, 128
+_NORM_HEAD, _ATTENTION_HEAD, _CLIP_OPTIONS = (struct.Struct(f) for f in ("qiiif", "qiiiiiifPP", "iffPPP"))
+assert (_NORM_HEAD.size, _ATTENTION_HEAD.size, _CLIP_OPTIONS.size) == (_Norm.x.offset, _Attention.query.offset, _Clip.workspace.offset)
+_NORM_FIELDS, _CLIP_FIELDS = ("rows", "width", "dtype", "groups", "eps"), ("grads", "max_norm", "eps", "grad_scale", "norm", "factor")
+_ATTENTION_FIELDS = ("rows", "key's width", "value's width", "heads", "heads of key", "dtype", "offsets", "scale", "offsets", "log_decay")
+
+
+def bagel_layer_norm_workspace(rows: int, width: int, groups: int = 1) -> int:
+    """Bytes of work space of bagel_layer_norm_grad."""
+    return int(load().bagel_layer_norm_workspace(rows, width, groups))
+
+
+def bagel_layer_norm(x, out, *, weight=None, bias=None, groups=1, eps=1e-5, stream=None):
+    """out = (x - mean) / sqrt(variance + eps) * weight + bias over rows, or over each of `groups` equal parts of a row (see include/bagel.h)."""
+    lib = _load()
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(x, "x", device)
+    try:
+        head = _NORM_HEAD.pack(rows, width, code, groups, eps)
+    except _UNFIT:
+        raise _unfit(_NORM_HEAD, _NORM_FIELDS, rows, width, code, groups, eps) from None
+    args = (head + _marshal.matrices(x, ("x", "out"), (x, _needed(out, "out"))) +
+            _marshal.vectors(device, (width,), ("weight", "bias"), (weight, bias)) + _NOTHING)
+    _done(lib, lib.bagel_layer_norm(args, on))
+
+
+def bagel_layer_norm_grad(x, d_out, d_x=None, *, weight=None, groups=1, eps=1e-5, d_weight=None, d_bias=None, workspace=None, stream=None):
+    """The gradient of bagel_layer_norm (see include/bagel.h)."""
+    lib = _load()
+    on, device = _stream(stream)
+    rows, width, code = _marshal.first(x, "x", device)
+    try:
+        head = _NORM_HEAD.pack(rows, width, code, groups, eps)
+    except _UNFIT:
+        raise _unfit(_NORM_HEAD, _NORM_FIELDS, rows, width, code, groups, eps) from None
+    sums = d_weight is not None or d_bias is not None
+    workspace, space = _workspace(workspace, lib.bagel_layer_norm_workspace(rows, width, groups) if sums else 0, device, stream)
+    args = (head + _marshal.matrices(x, ("x", "out"), (x, None)) + _marshal.vectors(device, (width,), ("weight", "bias"), (weight, None)) +
+            _marshal.matrices(x, ("d_out", "d_x"), (_needed(d_out, "d_out"), d_x)) +
+            _marshal.vectors(device, (width,), ("d_weight", "d_bias"), (d_weight, d_bias)) + space)
+    _done(lib, lib.bagel_layer_norm_grad(args, on))
+
+
+_ONE_ROW_EACH = object()         # in the place of offsets: as many sequences as rows
+
+
+def _attention(device, query, key, value, out, offsets, log_decay, scale):
+    """What the calls of linear attention have in common: (rows, heads, states, key width, value width, type, sequences, first bytes)."""
+    rows, heads, key_width, code = _marshal.first_heads(query, "query", device)
+    states, value_width = _marshal.first_heads(key, "key", device)[1], _marshal.first_heads(value, "value", device)[2]
+    n, at = (rows, 0) if offsets is _ONE_ROW_EACH else _sequences(offsets, device)
+    decay = _marshal.vectors(device, (states,), ("log_decay",), (_needed(log_decay, "log_decay"),))
+    try:
+        head = _ATTENTION_HEAD.pack(rows, key_width, value_width, heads, states, code, n, scale, at, 0)
+    except _UNFIT:
+        raise _unfit(_ATTENTION_HEAD, _ATTENTION_FIELDS, rows, key_width, value_width, heads, states, code, n, scale, at, 0) from None
+    head = head[:-8] + decay + _marshal.heads(device, code, rows, ("query", "key", "value", "out"),
+                                              (heads, key_width, states, key_width, states, value_width, heads, value_width), (query, key, value, out))
+    return rows, heads, states, key_width, value_width, code, n, head
+
+
+def bagel_linear_attention_workspace(rows: int, sequences: int, heads: int, states: int, key_width: int, value_width: int, grad: bool = False) -> int:
+    """Bytes of work space of bagel_linear_attention, or (grad) of bagel_linear_attention_grad."""
+    sizes = _Attention()
+    sizes.rows, sizes.sequences, sizes.heads, sizes.states, sizes.key_width, sizes.value_width = rows, sequences, heads, states, key_width, value_width
+    return int(load().bagel_linear_attention_workspace(C.byref(sizes), int(grad)))
+
+
+def bagel_linear_attention(query, key, value, out, offsets, log_decay, *, scale=1.0, initial=None, final=None, workspace=None, stream=None):
+    """S_t = decay S_{t-1} + key_t value_t^T, out_t = scale S_t^T query_t along packed sequences, decay = exp(log_decay) (see include/bagel.h).
+
+    query[rows, heads, key width], key[rows, states, key width], value[rows, states, value width], out[rows, heads, value width],
+    log_decay[states], initial and final [sequences, states, key width, value width]."""
+    lib = _load()
+    on, device = _stream(stream)
+    rows, heads, states, dk, dv, code, n, head = _attention(device, query, key, value, _needed(out, "out"), offsets, log_decay, scale)
+    workspace, space = _workspace(workspace, lib.bagel_linear_attention_workspace(head, 0), device, stream)
+    args = head + _marshal.vectors(device, (n, states, dk, dv), ("initial", "final"), (initial, final)) + bytes(8 + 4 * 24 + 16) + space
+    _done(lib, lib.bagel_linear_attention(args, on))
+
+
+def bagel_linear_attention_grad(query, key, value, d_out, d_query, d_key, d_value, offsets, log_decay, *, scale=1.0, initial=None, d_final=None,
+                                d_initial=None, workspace=None, stream=None):
+    """The gradient of bagel_linear_attention (see include/bagel.h); results that are None are left out."""
+    lib = _load()
+    on, device = _stream(stream)
+    rows, heads, states, dk, dv, code, n, head = _attention(device, query, key, value, None, offsets, log_decay, scale)
+    workspace, space = _workspace(workspace, lib.bagel_linear_attention_workspace(head, 1), device, stream)
+    args = (head + _marshal.vectors(device, (n, states, dk, dv), ("initial", "final"), (initial, None)) + bytes(8) +
+            _marshal.heads(device, code, rows, ("d_out", "d_query", "d_key", "d_value"), (heads, dv, heads, dk, states, dk, states, dv),
+                           (_needed(d_out, "d_out"), d_query, d_key, d_value)) +
+            _marshal.vectors(device, (n, states, dk, dv), ("d_final", "d_initial"), (d_final, d_initial)) + space)
+    _done(lib, lib.bagel_linear_attention_grad(args, on))
+
+
+def bagel_linear_attention_step(query, key, value, state, out, log_decay, *, scale=1.0, stream=None):
+    """One row of as many sequences as there are rows, the float32 state[rows, states, key width, value width] updated in place (see include/bagel.h)."""
+    lib = _load()
+    on, device = _stream(stream)
+    rows, heads, states, dk, dv, code, n, head = _attention(device, query, key, value, _needed(out, "out"), _ONE_ROW_EACH, log_decay, scale)
+    args = head + bytes(16) + _marshal.vectors(device, (n, states, dk, dv), ("state",), (_needed(state, "state"),)) + _NOTHING
+    _done(lib, lib.bagel_linear_attention_step(args, on))
+
+
+def bagel_clip_norm(grads, max_norm, norm, factor, *, grad_scale=None, out=None, eps=1e-6, workspace=None, stream=None):
+    """norm = |grad_scale| sqrt(sum of squares of all gradients), factor = grad_scale min(1, max_norm / (norm + eps)), out = gradients * factor
+    (see include/bagel.h).
+
+    grads: a list of contiguous tensors of one type; norm, factor and grad_scale (None: one): float32 tensors of one value.  out: None, or a list with
+    a tensor or None for every gradient, which may be the gradient itself.  `factor` is a grad_scale for bagel_adamw_step."""
+    lib = _load()
+    on, device = _stream(stream)
+    n, table, code = _marshal.clip(device, grads, out)
+    places = []
+    for name, t in (("grad_scale", grad_scale), ("norm", norm), ("factor", factor)):
+        if t is None and name == "grad_scale":
+            places.append(0)
+            continue
+        if not isinstance(t, _torch.Tensor) or t.numel() != 1 or t.dtype != _torch.float32 or t.get_device() != device:
+            raise ValueError(f"{name} must hold one float32 value and be on the current GPU")
+        places.append(t.data_ptr())
+    workspace, space = _workspace(workspace, lib.bagel_clip_norm_workspace(n), device, stream)
+    try:
+        options = _CLIP_OPTIONS.pack(code, max_norm, eps, *places)
+    except _UNFIT:
+        raise _unfit(_CLIP_OPTIONS, _CLIP_FIELDS, code, max_norm, eps, *places) from None
+    _done(lib, lib.bagel_clip_norm(table, n, options + space, on))
 
 
 class Bagel:

@@ -1,0 +1,348 @@
+// Linear attention with a decay for every head (include/bagel.h), its gradient and its single step.
+//
+// With l the decay of a memory, over the rows t of a sequence,
+//   S_t = l S_{t-1} + k_t v_t^T,   o_t = c S_t^T q_t
+// and backwards, with R_t the gradient of S_t,
+//   R_t = c q_t do_t^T + l R_{t+1},   dq_t = c S_t do_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dS_0 = l R_1
+// So every gradient is a linear attention of its own: dq that of do, v, k with the memory S^T; dv that of k, q, do and dk that of v, do, q from the
+// last row to the first, with the memories R and R^T.
+#include "activations.h"
+
+namespace {
+
+template <typename T> struct heads_of {
+    T *data;
+    int64_t stride, head;
+    __device__ __forceinline__ T *at(int64_t row, int h) const { return data + row * stride + h * head; }
+};
+template <typename T> heads_of<T> heads_from(const bagel_heads &h) { return {(T *)h.data, h.stride, h.head}; }
+
+// One linear attention: out = memory^T a, memory += b c^T.  a and out have `qs` heads to a memory, b and c `ks`, of which one or both are 1.
+template <typename T> struct pass_args {
+    int64_t rows;
+    int sequences, each, states, qs, ks, wb, wc;     // wb: width of a and b, wc: of c and out
+    float scale;                                     // of the results
+    float scale_b;                                   // of b
+    const int32_t *offsets;
+    const float *log_decay;
+    heads_of<T> a, b, c, out;
+    const float *first;                              // memories before the first row (gone through), null: zero
+    float *last;                                     // and behind the last, null: not wanted
+    int64_t step_b, step_c;                          // of their entries: [sequences][states] times wb, wc in either order
+};
+
+// Rows begin to end - 1 of sequence i; offsets that break the rules lead nowhere else.
+template <typename A> __device__ __forceinline__ void sequence_rows(const A &a, int i, int64_t &begin, int64_t &end)
+{
+    if (!a.offsets) {
+        begin = (int64_t)i * a.each;
+        end = begin + a.each;
+        return;
+    }
+    begin = min(max((int64_t)a.offsets[i], (int64_t)0), a.rows);
+    end = min(max((int64_t)a.offsets[i + 1], begin), a.rows);
+}
+
+// The plain form: a workgroup to a memory, row after row, an entry of its columns in each of 128 threads for half of its rows.
+template <typename T, bool BACK> __global__ __launch_bounds__(256) void rows_kernel(pass_args<T> p)
+{
+    constexpr int MOST = BAGEL_ATTENTION_MAX_WIDTH;
+    __shared__ float sa[MOST], sb[MOST], sc[MOST], part[MOST];
+    const int state = blockIdx.x % p.states, seq = blockIdx.x / p.states, col = threadIdx.x & 127, half = threadIdx.x >> 7;
+    int64_t begin, end;
+    sequence_rows(p, seq, begin, end);
+    const float log_decay = p.log_decay[state], decay = expf(log_decay);
+    float S[MOST / 2];
+    const int64_t memory = ((int64_t)seq * p.states + state) * p.wb * p.wc;
+#pragma unroll
+    for (int j = 0; j < MOST / 2; ++j) {
+        const int r = half * (MOST / 2) + j;
+        S[j] = p.first && r < p.wb && col < p.wc ? p.first[memory + r * p.step_b + col * p.step_c] : 0.0f;
+    }
+    const int t = threadIdx.x;
+    for (int64_t n = 0; n < end - begin; ++n) {
+        const int64_t row = BACK ? end - 1 - n : begin + n;
+        if (!BACK)
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
+        for (int g = 0; g < p.ks; ++g) {
+            __syncthreads();
+            if (t < MOST) sb[t] = t < p.wb ? (float)p.b.at(row, state * p.ks + g)[t] * p.scale_b : 0.0f;
+            else sc[t - MOST] = t - MOST < p.wc ? (float)p.c.at(row, state * p.ks + g)[t - MOST] : 0.0f;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] = fmaf(sb[half * (MOST / 2) + j], sc[col], S[j]);
+        }
+        for (int g = 0; g < p.qs && p.out.data; ++g) {
+            __syncthreads();
+            if (t < MOST) sa[t] = t < p.wb ? (float)p.a.at(row, state * p.qs + g)[t] : 0.0f;
+            __syncthreads();
+            float o = 0.0f;
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) o = fmaf(sa[half * (MOST / 2) + j], S[j], o);
+            if (half) part[col] = o;
+            __syncthreads();
+            if (!half && col < p.wc) p.out.at(row, state * p.qs + g)[col] = (T)((o + part[col]) * p.scale);
+        }
+        if (BACK)
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
+    }
+    if (!p.last) return;
+#pragma unroll
+    for (int j = 0; j < MOST / 2; ++j) {
+        const int r = half * (MOST / 2) + j;
+        if (r < p.wb && col < p.wc) p.last[memory + r * p.step_b + col * p.step_c] = S[j];
+    }
+}
+
+// Zeros in the rows behind the last sequence.
+template <typename T> __global__ __launch_bounds__(256) void behind_kernel(int64_t rows, int sequences, const int32_t *offsets, int heads, int width, heads_of<T> out)
+{
+    const int64_t end = min(max((int64_t)offsets[sequences], (int64_t)0), rows), n = (rows - end) * heads * width;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / (heads * width);
+        const int j = (int)(i - r * heads * width);
+        out.at(end + r, j / width)[j % width] = (T)0.0f;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, heads_of<T> q,
+                                                   heads_of<T> k, heads_of<T> v, heads_of<T> out, float *state)
+{
+    __shared__ float sk[BAGEL_ATTENTION_MAX_WIDTH], sv[BAGEL_ATTENTION_MAX_WIDTH], sq[BAGEL_ATTENTION_MAX_WIDTH], part[256];
+    for (int64_t i = blockIdx.x; i < rows * states; i += gridDim.x) {
+        const int64_t row = i / states;
+        const int s = (int)(i - row * states), t = threadIdx.x, col = t & 127, half = t >> 7;
+        const float decay = expf(log_decay[s]);
+        float *S = state + i * wk * wv;
+        __syncthreads();
+        if (t < wk) sk[t] = (float)k.at(row, s)[t];
+        if (t < wv) sv[t] = (float)v.at(row, s)[t];
+        __syncthreads();
+        if (col < wv)
+            for (int r = half; r < wk; r += 2) S[r * wv + col] = fmaf(sk[r], sv[col], S[r * wv + col] * decay);
+        for (int g = 0; g < each; ++g) {
+            __syncthreads();
+            if (t < wk) sq[t] = (float)q.at(row, s * each + g)[t];
+            __syncthreads();
+            float o = 0.0f;
+            if (col < wv)
+                for (int r = half; r < wk; r += 2) o = fmaf(sq[r], S[r * wv + col], o);
+            part[t] = o;
+            __syncthreads();
+            if (half == 0 && col < wv) out.at(row, s * each + g)[col] = (T)((part[col] + part[col + 128]) * scale);
+        }
+    }
+}
+
+template <typename T> pass_args<T> args_of(const bagel_attention &b)
+{
+    pass_args<T> p{};
+    p.rows = b.rows;
+    p.sequences = b.sequences;
+    p.each = b.sequences > 0 ? (int)(b.rows / b.sequences) : 0;
+    p.states = b.states;
+    p.offsets = b.offsets;
+    p.log_decay = b.log_decay;
+    p.scale = p.scale_b = 1.0f;
+    return p;
+}
+
+// The passes of a call.  S is [key][value]; `turned`: the memory of the pass is its transpose.
+template <typename T> hipError_t launch_pass(pass_args<T> &p, bool back, const bagel_attention &b, bool turned, hipStream_t stream)
+{
+    p.step_b = turned ? 1 : b.value_width;
+    p.step_c = turned ? b.value_width : 1;
+    const unsigned groups = (unsigned)((int64_t)p.sequences * p.states);
+    if (groups > 0 && back) rows_kernel<T, true><<<groups, 256, 0, stream>>>(p);
+    if (groups > 0 && !back) rows_kernel<T, false><<<groups, 256, 0, stream>>>(p);
+    if (p.offsets && p.out.data && p.rows > 0) {
+        const int64_t n = (p.rows * p.states * p.qs * p.wc + 255) / 256;
+        behind_kernel<T><<<(unsigned)(n < 1024 ? n : 1024), 256, 0, stream>>>(p.rows, p.sequences, p.offsets, p.states * p.qs, p.wc, p.out);
+    }
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_attention(const bagel_attention &b, hipStream_t stream)
+{
+    pass_args<T> p = args_of<T>(b);
+    p.qs = b.heads / b.states;
+    p.ks = 1;
+    p.wb = b.key_width;
+    p.wc = b.value_width;
+    p.scale = b.scale;
+    p.a = heads_from<T>(b.query);
+    p.b = heads_from<T>(b.key);
+    p.c = heads_from<T>(b.value);
+    p.out = heads_from<T>(b.out);
+    p.first = b.initial;
+    p.last = b.final_state;
+    return launch_pass(p, false, b, false, stream);
+}
+
+template <typename T> hipError_t launch_attention_grad(const bagel_attention &b, hipStream_t stream)
+{
+    const int each = b.heads / b.states;
+    pass_args<T> p = args_of<T>(b);
+    const heads_of<T> q = heads_from<T>(b.query), k = heads_from<T>(b.key), v = heads_from<T>(b.value), d = heads_from<T>(b.d_out);
+    hipError_t e = hipSuccess;
+    if (b.d_query.data) {
+        p.qs = each;
+        p.ks = 1;
+        p.wb = b.value_width;
+        p.wc = b.key_width;
+        p.scale = b.scale;
+        p.a = d;
+        p.b = v;
+        p.c = k;
+        p.out = heads_from<T>(b.d_query);
+        p.first = b.initial;
+        if ((e = launch_pass(p, false, b, true, stream)) != hipSuccess) return e;
+    }
+    p = args_of<T>(b);
+    p.qs = 1;
+    p.ks = each;
+    if (b.d_value.data || b.d_initial) {
+        p.wb = b.key_width;
+        p.wc = b.value_width;
+        p.scale_b = b.scale;
+        p.a = k;
+        p.b = q;
+        p.c = d;
+        p.out = heads_from<T>(b.d_value);
+        p.first = b.d_final;
+        p.last = b.d_initial;
+        if ((e = launch_pass(p, true, b, false, stream)) != hipSuccess) return e;
+    }
+    if (b.d_key.data) {
+        p.wb = b.value_width;
+        p.wc = b.key_width;
+        p.scale_b = b.scale;
+        p.a = v;
+        p.b = d;
+        p.c = q;
+        p.out = heads_from<T>(b.d_key);
+        p.first = b.d_final;
+        p.last = nullptr;
+        e = launch_pass(p, true, b, true, stream);
+    }
+    return e;
+}
+
+template <typename T> hipError_t launch_step(const bagel_attention &b, hipStream_t stream)
+{
+    const int64_t groups = b.rows * b.states;
+    step_kernel<T><<<(unsigned)(groups < 1 << 20 ? groups : 1 << 20), 256, 0, stream>>>(
+        b.rows, b.states, b.heads / b.states, b.key_width, b.value_width, b.scale, b.log_decay, heads_from<T>(b.query), heads_from<T>(b.key),
+        heads_from<T>(b.value), heads_from<T>(b.out), b.state);
+    return hipGetLastError();
+}
+
+const char *check_sizes(const bagel_attention *b)
+{
+    if (!b) return "null argument";
+    if (b->rows < 0 || b->rows >= 1 << 28) return "rows must be >= 0 and below 2^28";
+    if (b->sequences < 0 || b->sequences >= 1 << 28) return "sequences must be >= 0 and below 2^28";
+    if (b->states < 1 || b->heads < 1 || b->heads > 4096 || b->heads % b->states != 0) return "heads must be in 1..4096, and states divide them";
+    if (b->key_width < 1 || b->key_width > BAGEL_ATTENTION_MAX_WIDTH || b->value_width < 1 || b->value_width > BAGEL_ATTENTION_MAX_WIDTH)
+        return "key_width and value_width must be in 1..128";
+    if ((b->rows + b->sequences) * b->states >= 1ll << 31) return "rows and sequences together, times states, must be below 2^31";
+    return nullptr;
+}
+
+// Whether heads can be addressed; those of a result may not overlap.
+const char *check_heads(const bagel_heads &h, int64_t rows, int heads, int width, int dtype, bool written)
+{
+    if (!h.data) return nullptr;
+    if ((uintptr_t)h.data & (bagel_type_bytes(dtype) - 1)) return "heads do not start at a multiple of their type";
+    if (h.stride < 0 || h.head < 0 || h.stride >= 1ll << 40 || h.head >= 1ll << 40) return "a stride of heads or rows must be >= 0 and below 2^40";
+    if (!written) return nullptr;
+    const bool side_by_side = (heads <= 1 || h.head >= width) && (rows <= 1 || h.stride >= (heads - 1) * h.head + width);
+    const bool one_after_the_other = (rows <= 1 || h.stride >= width) && (heads <= 1 || h.head >= (rows - 1) * h.stride + width);
+    return side_by_side || one_after_the_other ? nullptr : "rows or heads of a result overlap: a stride is too small";
+}
+
+bool memories_overlap(const bagel_attention *b, const float *read, const float *written)
+{
+    const uintptr_t x = (uintptr_t)read, y = (uintptr_t)written, bytes = (uintptr_t)b->sequences * b->states * b->key_width * b->value_width * sizeof(float);
+    return read && written && (x < y ? y - x : x - y) < bytes;
+}
+
+const char *check_inputs(const bagel_attention *b)
+{
+    if (!bagel_type_ok(b->dtype)) return "unknown dtype";
+    if (!isfinite(b->scale)) return "scale must be finite";
+    if (!b->log_decay) return "log_decay is needed";
+    if (b->rows > 0 && (!b->query.data || !b->key.data || !b->value.data)) return "query, key and value are needed";
+    if (const char *msg = check_heads(b->query, b->rows, b->heads, b->key_width, b->dtype, false)) return msg;
+    if (const char *msg = check_heads(b->key, b->rows, b->states, b->key_width, b->dtype, false)) return msg;
+    return check_heads(b->value, b->rows, b->states, b->value_width, b->dtype, false);
+}
+
+const char *check_attention(const bagel_attention *b, bool grad)
+{
+    if (const char *msg = check_sizes(b)) return msg;
+    if (const char *msg = check_inputs(b)) return msg;
+    if (b->rows > 0) {
+        if (b->sequences < 1) return "rows without a sequence";
+        if (!b->offsets && b->rows % b->sequences != 0) return "without offsets, sequences must divide rows";
+        if (!grad && !b->out.data) return "out is needed";
+        if (grad && !b->d_out.data) return "d_out is needed";
+    }
+    if (!grad) {
+        if (const char *msg = check_heads(b->out, b->rows, b->heads, b->value_width, b->dtype, true)) return msg;
+        if (memories_overlap(b, b->initial, b->final_state)) return "initial and final_state overlap";
+    } else {
+        if (const char *msg = check_heads(b->d_out, b->rows, b->heads, b->value_width, b->dtype, false)) return msg;
+        if (const char *msg = check_heads(b->d_query, b->rows, b->heads, b->key_width, b->dtype, true)) return msg;
+        if (const char *msg = check_heads(b->d_key, b->rows, b->states, b->key_width, b->dtype, true)) return msg;
+        if (const char *msg = check_heads(b->d_value, b->rows, b->states, b->value_width, b->dtype, true)) return msg;
+        if (memories_overlap(b, b->d_final, b->d_initial)) return "d_final and d_initial overlap";
+    }
+    const int64_t need = bagel_linear_attention_workspace(b, grad);
+    if (need > 0 && !b->workspace) return "a workspace is needed";
+    if (b->workspace_bytes < need) return "the workspace is too small";
+    if ((uintptr_t)b->workspace & 15) return "the workspace must start at a multiple of 16 bytes";
+    return nullptr;
+}
+
+}  // namespace
+
+extern "C" int64_t bagel_linear_attention_workspace(const bagel_attention *b, int32_t grad)
+{
+    if (check_sizes(b)) return BAGEL_EINVAL;
+    return 0;
+}
+
+extern "C" int bagel_linear_attention(const bagel_attention *b, void *hip_stream)
+{
+    if (const char *msg = check_attention(b, false)) return bagel_refuse(BAGEL_EINVAL, "bagel_linear_attention: %s", msg);
+    const hipError_t e = bagel_by_type(b->dtype, [&](auto t) { return launch_attention<typename decltype(t)::type>(*b, (hipStream_t)hip_stream); });
+    if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_linear_attention: %s", hipGetErrorString(e));
+    return BAGEL_OK;
+}
+
+extern "C" int bagel_linear_attention_grad(const bagel_attention *b, void *hip_stream)
+{
+    if (const char *msg = check_attention(b, true)) return bagel_refuse(BAGEL_EINVAL, "bagel_linear_attention_grad: %s", msg);
+    const hipError_t e = bagel_by_type(b->dtype, [&](auto t) { return launch_attention_grad<typename decltype(t)::type>(*b, (hipStream_t)hip_stream); });
+    if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_linear_attention_grad: %s", hipGetErrorString(e));
+    return BAGEL_OK;
+}
+
+extern "C" int bagel_linear_attention_step(const bagel_attention *b, void *hip_stream)
+{
+    const char *msg = check_sizes(b);
+    if (!msg && b->sequences != b->rows) msg = "a step has as many rows as sequences";
+    if (!msg) msg = check_inputs(b);
+    if (!msg && b->rows > 0 && (!b->out.data || !b->state)) msg = "out and state are needed";
+    if (!msg) msg = check_heads(b->out, b->rows, b->heads, b->value_width, b->dtype, true);
+    if (msg) return bagel_refuse(BAGEL_EINVAL, "bagel_linear_attention_step: %s", msg);
+    if (b->rows > 0) {
+        const hipError_t e = bagel_by_type(b->dtype, [&](auto t) { return launch_step<typename decltype(t)::type>(*b, (hipStream_t)hip_stream); });
+        if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_linear_attention_step: %s", hipGetErrorString(e));
+    }
+    return BAGEL_OK;
+}

@@ -135,6 +135,51 @@ PyObject *vectors(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// heads(device, type code, rows, names, (heads, width, heads, width, ...), tensors) -> a bagel_heads for each, of shape [rows, heads, width]; None: left out
+PyObject *heads(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 6 || !PyTuple_Check(args[3]) || !PyTuple_Check(args[4]) || !PyTuple_Check(args[5]) || PyTuple_GET_SIZE(args[3]) != PyTuple_GET_SIZE(args[5]) ||
+            PyTuple_GET_SIZE(args[4]) != 2 * PyTuple_GET_SIZE(args[5]))
+            throw refused{"heads(device, type code, rows, names, sizes, tensors)"};
+        const int64_t device = PyLong_AsLongLong(args[0]), code = PyLong_AsLongLong(args[1]), rows = PyLong_AsLongLong(args[2]);
+        const at::ScalarType type = code == BAGEL_FLOAT32 ? at::kFloat : code == BAGEL_BFLOAT16 ? at::kBFloat16 : at::kHalf;
+        std::vector<int64_t> out;
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(args[5]); ++i) {
+            PyObject *o = PyTuple_GET_ITEM(args[5], i);
+            if (o == Py_None) {
+                out.insert(out.end(), {0, 0, 0});
+                continue;
+            }
+            const char *name = name_of(args[3], i);
+            const at::Tensor &t = tensor_of(o, name);
+            const int64_t shape[3] = {rows, PyLong_AsLongLong(PyTuple_GET_ITEM(args[4], 2 * i)), PyLong_AsLongLong(PyTuple_GET_ITEM(args[4], 2 * i + 1))};
+            if (t.scalar_type() != type || t.sizes() != at::IntArrayRef(shape, 3) || !on(t, device))
+                refuse(name, t, "a " + type_name(type) + " tensor of shape " + shown(at::IntArrayRef(shape, 3)) + " on cuda:" + std::to_string(device));
+            if (t.stride(2) != 1 && shape[2] > 1 && rows > 0) throw refused{std::string(name) + ": the entries of a head must be next to each other"};
+            const int64_t head = shape[1] > 1 ? t.stride(1) : shape[2];
+            out.insert(out.end(), {(int64_t)(intptr_t)t.data_ptr(), rows > 1 ? t.stride(0) : head * shape[1], head});
+        }
+        return bytes_of(out);
+    });
+}
+
+// first_heads(tensor, name, device) -> (rows, heads, width, type code) of a tensor of heads
+PyObject *first_heads(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 3) throw refused{"first_heads(tensor, name, device)"};
+        const char *name = PyUnicode_AsUTF8(args[1]);
+        const int64_t device = PyLong_AsLongLong(args[2]);
+        if (!THPVariable_Check(args[0]) || type_code(THPVariable_Unpack(args[0]).scalar_type()) < 0)
+            throw refused{std::string(name) + " must be a float32, bfloat16 or float16 tensor"};
+        const at::Tensor &t = THPVariable_Unpack(args[0]);
+        if (!on(t, device)) throw refused{std::string(name) + " must be on the current GPU"};
+        if (t.dim() != 3) throw refused{std::string(name) + " must have three dimensions, rows, heads and width, not " + std::to_string(t.dim())};
+        return Py_BuildValue("LLLi", (long long)t.size(0), (long long)t.size(1), (long long)t.size(2), type_code(t.scalar_type()));
+    });
+}
+
 struct list {
     PyObject *items = nullptr;               // a list or tuple, or null
     list() = default;
@@ -150,6 +195,14 @@ struct list {
         if (items ? PySequence_Fast_GET_SIZE(items) != n : wanted || o != Py_None)
             throw refused{std::string("the lists of one update must have an entry for every tensor, ") + name +
                           " does not (moments in 8 bits need m_scale and v_scale)"};
+    }
+    // A list of one entry for every gradient, or None.
+    void beside(PyObject *o, Py_ssize_t n, const char *name)
+    {
+        if (o == Py_None) return;
+        items = PySequence_Fast(o, "");
+        PyErr_Clear();
+        if (!items || PySequence_Fast_GET_SIZE(items) != n) throw refused{std::string(name) + " must be a list with an entry for every gradient"};
     }
     // A list that has no place in this update: of the right length, and nothing in it.
     void none(PyObject *o, Py_ssize_t n, const char *name)
@@ -242,9 +295,57 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     });
 }
 
+// clip(device, grads, out) -> (n, bagel_clip_tensor for each, type code)
+PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
+{
+    return guarded([&]() -> PyObject * {
+        if (n_args != 3) throw refused{"clip(device, grads, out)"};
+        const int64_t device = PyLong_AsLongLong(args[0]);
+        const Py_ssize_t n = THPVariable_Check(args[1]) ? -1 : PySequence_Size(args[1]);
+        if (n < 0) {
+            PyErr_Clear();
+            throw refused{"grads must be a list of tensors"};
+        }
+        list g, out;
+        g.beside(args[1], n, "grads");
+        out.beside(args[2], n, "out");
+        at::ScalarType type = at::kFloat;
+        if (n > 0) type = tensor_of(g[0], "grads").scalar_type();
+        if (type_code(type) < 0) throw refused{"grads must be float32, bfloat16 or float16 tensors"};
+        PyObject *table = PyBytes_FromStringAndSize(nullptr, n * (Py_ssize_t)sizeof(bagel_clip_tensor));
+        if (!table) return nullptr;
+        try {
+            bagel_clip_tensor *to = (bagel_clip_tensor *)PyBytes_AS_STRING(table);
+            for (Py_ssize_t i = 0; i < n; ++i) {
+                const at::Tensor &grad = tensor_of(g[i], "grads");
+                const auto held = [&](PyObject *o, const char *name) {
+                    const at::Tensor &t = tensor_of(o, name);
+                    if (t.scalar_type() != type || t.sizes() != grad.sizes() || !t.is_contiguous() || !on(t, device))
+                        refuse(("tensor " + std::to_string(i) + " of the gradients: " + name).c_str(), t,
+                               "a contiguous " + type_name(type) + " tensor of shape " + shown(grad.sizes()) + " on cuda:" + std::to_string(device));
+                    return t.data_ptr();
+                };
+                bagel_clip_tensor x;
+                std::memset(&x, 0, sizeof(x));
+                x.grad = held(g[i], "grads");
+                x.out = out.items && out[i] != Py_None ? held(out[i], "out") : nullptr;
+                x.count = grad.numel();
+                to[i] = x;
+            }
+        } catch (...) {
+            Py_DECREF(table);
+            throw;
+        }
+        return Py_BuildValue("nNi", n, table, type_code(type));
+    });
+}
+
 PyMethodDef METHODS[] = {{"first", (PyCFunction)(void *)first, METH_FASTCALL, nullptr},
                          {"matrices", (PyCFunction)(void *)matrices, METH_FASTCALL, nullptr},
                          {"vectors", (PyCFunction)(void *)vectors, METH_FASTCALL, nullptr},
+                         {"first_heads", (PyCFunction)(void *)first_heads, METH_FASTCALL, nullptr},
+                         {"heads", (PyCFunction)(void *)heads, METH_FASTCALL, nullptr},
+                         {"clip", (PyCFunction)(void *)clip, METH_FASTCALL, nullptr},
                          {"adamw", (PyCFunction)(void *)adamw, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef MODULE = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of binding.py.", -1, METHODS, nullptr, nullptr, nullptr, nullptr};
