@@ -6,110 +6,13 @@
 //   R_t = c q_t do_t^T + l R_{t+1},   dq_t = c S_t do_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dS_0 = l R_1
 // So every gradient is a linear attention of its own: dq that of do, v, k with the memory S^T; dv that of k, q, do and dk that of v, do, q from the
 // last row to the first, with the memories R and R^T.
-#include "activations.h"
+#include "linear_attention.h"
 
 namespace {
 
-template <typename T> struct heads_of {
-    T *data;
-    int64_t stride, head;
-    __device__ __forceinline__ T *at(int64_t row, int h) const { return data + row * stride + h * head; }
-};
-template <typename T> heads_of<T> heads_from(const bagel_heads &h) { return {(T *)h.data, h.stride, h.head}; }
-
-// One linear attention: out = memory^T a, memory += b c^T.  a and out have `qs` heads to a memory, b and c `ks`, of which one or both are 1.
-template <typename T> struct pass_args {
-    int64_t rows;
-    int sequences, each, states, qs, ks, wb, wc;     // wb: width of a and b, wc: of c and out
-    float scale;                                     // of the results
-    float scale_b;                                   // of b
-    const int32_t *offsets;
-    const float *log_decay;
-    heads_of<T> a, b, c, out;
-    const float *first;                              // memories before the first row (gone through), null: zero
-    float *last;                                     // and behind the last, null: not wanted
-    int64_t step_b, step_c;                          // of their entries: [sequences][states] times wb, wc in either order
-};
-
-// Rows begin to end - 1 of sequence i; offsets that break the rules lead nowhere else.
-template <typename A> __device__ __forceinline__ void sequence_rows(const A &a, int i, int64_t &begin, int64_t &end)
-{
-    if (!a.offsets) {
-        begin = (int64_t)i * a.each;
-        end = begin + a.each;
-        return;
-    }
-    begin = min(max((int64_t)a.offsets[i], (int64_t)0), a.rows);
-    end = min(max((int64_t)a.offsets[i + 1], begin), a.rows);
-}
-
-// The plain form: a workgroup to a memory, row after row, an entry of its columns in each of 128 threads for half of its rows.
-template <typename T, bool BACK> __global__ __launch_bounds__(256) void rows_kernel(pass_args<T> p)
-{
-    constexpr int MOST = BAGEL_ATTENTION_MAX_WIDTH;
-    __shared__ float sa[MOST], sb[MOST], sc[MOST], part[MOST];
-    const int state = blockIdx.x % p.states, seq = blockIdx.x / p.states, col = threadIdx.x & 127, half = threadIdx.x >> 7;
-    int64_t begin, end;
-    sequence_rows(p, seq, begin, end);
-    const float log_decay = p.log_decay[state], decay = expf(log_decay);
-    float S[MOST / 2];
-    const int64_t memory = ((int64_t)seq * p.states + state) * p.wb * p.wc;
-#pragma unroll
-    for (int j = 0; j < MOST / 2; ++j) {
-        const int r = half * (MOST / 2) + j;
-        S[j] = p.first && r < p.wb && col < p.wc ? p.first[memory + r * p.step_b + col * p.step_c] : 0.0f;
-    }
-    const int t = threadIdx.x;
-    for (int64_t n = 0; n < end - begin; ++n) {
-        const int64_t row = BACK ? end - 1 - n : begin + n;
-        if (!BACK)
-#pragma unroll
-            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
-        for (int g = 0; g < p.ks; ++g) {
-            __syncthreads();
-            if (t < MOST) sb[t] = t < p.wb ? (float)p.b.at(row, state * p.ks + g)[t] * p.scale_b : 0.0f;
-            else sc[t - MOST] = t - MOST < p.wc ? (float)p.c.at(row, state * p.ks + g)[t - MOST] : 0.0f;
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < MOST / 2; ++j) S[j] = fmaf(sb[half * (MOST / 2) + j], sc[col], S[j]);
-        }
-        for (int g = 0; g < p.qs && p.out.data; ++g) {
-            __syncthreads();
-            if (t < MOST) sa[t] = t < p.wb ? (float)p.a.at(row, state * p.qs + g)[t] : 0.0f;
-            __syncthreads();
-            float o = 0.0f;
-#pragma unroll
-            for (int j = 0; j < MOST / 2; ++j) o = fmaf(sa[half * (MOST / 2) + j], S[j], o);
-            if (half) part[col] = o;
-            __syncthreads();
-            if (!half && col < p.wc) p.out.at(row, state * p.qs + g)[col] = (T)((o + part[col]) * p.scale);
-        }
-        if (BACK)
-#pragma unroll
-            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
-    }
-    if (!p.last) return;
-#pragma unroll
-    for (int j = 0; j < MOST / 2; ++j) {
-        const int r = half * (MOST / 2) + j;
-        if (r < p.wb && col < p.wc) p.last[memory + r * p.step_b + col * p.step_c] = S[j];
-    }
-}
-
-// Zeros in the rows behind the last sequence.
-template <typename T> __global__ __launch_bounds__(256) void behind_kernel(int64_t rows, int sequences, const int32_t *offsets, int heads, int width, heads_of<T> out)
-{
-    const int64_t end = min(max((int64_t)offsets[sequences], (int64_t)0), rows), n = (rows - end) * heads * width;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / (heads * width);
-        const int j = (int)(i - r * heads * width);
-        out.at(end + r, j / width)[j % width] = (T)0.0f;
-    }
-}
-
 template <typename T>
-__global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, heads_of<T> q,
-                                                   heads_of<T> k, heads_of<T> v, heads_of<T> out, float *state)
+__global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, bagel_heads_of<T> q,
+                                                   bagel_heads_of<T> k, bagel_heads_of<T> v, bagel_heads_of<T> out, float *state)
 {
     __shared__ float sk[BAGEL_ATTENTION_MAX_WIDTH], sv[BAGEL_ATTENTION_MAX_WIDTH], sq[BAGEL_ATTENTION_MAX_WIDTH], part[256];
     for (int64_t i = blockIdx.x; i < rows * states; i += gridDim.x) {
@@ -137,9 +40,37 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
     }
 }
 
-template <typename T> pass_args<T> args_of(const bagel_attention &b)
+// Rows of a segment: enough segments for the card, but no shorter than is worth a memory that is written and read.
+int64_t segment_rows(const bagel_attention &b)
 {
-    pass_args<T> p{};
+    constexpr int64_t LEAST = 256, WANTED = 768;
+    const int64_t rows = b.rows * b.states / WANTED, chunk = BAGEL_ATTENTION_CHUNK;
+    return rows < LEAST ? LEAST : (rows + chunk - 1) / chunk * chunk;
+}
+
+// Numbers of segments, and whether a sequence may have more than one.
+struct segments {
+    int64_t rows, slots;
+    bool several;
+};
+segments segments_of(const bagel_attention &b)
+{
+    segments s = {segment_rows(b), 0, false};
+    const int64_t longest = b.sequences == 0 ? 0 : b.offsets ? b.rows : b.rows / b.sequences;
+    s.several = longest > s.rows;
+    if (!s.several) s.rows = longest > 0 ? (longest + BAGEL_ATTENTION_CHUNK - 1) / BAGEL_ATTENTION_CHUNK * BAGEL_ATTENTION_CHUNK : BAGEL_ATTENTION_CHUNK;
+    s.slots = b.offsets ? b.rows / s.rows + b.sequences : b.sequences * (longest > 0 ? (longest + s.rows - 1) / s.rows : 1);
+    return s;
+}
+int64_t memories_bytes(const bagel_attention &b, const segments &s)
+{
+    return s.several ? s.slots * b.states * b.key_width * b.value_width * (int64_t)sizeof(float) : 0;
+}
+
+template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
+{
+    const segments s = segments_of(b);
+    bagel_attention_pass<T> p{};
     p.rows = b.rows;
     p.sequences = b.sequences;
     p.each = b.sequences > 0 ? (int)(b.rows / b.sequences) : 0;
@@ -147,36 +78,33 @@ template <typename T> pass_args<T> args_of(const bagel_attention &b)
     p.offsets = b.offsets;
     p.log_decay = b.log_decay;
     p.scale = p.scale_b = 1.0f;
+    p.segment = s.rows;
+    p.slots = s.slots;
+    p.memories = s.several ? (float *)b.workspace : nullptr;
     return p;
 }
 
-// The passes of a call.  S is [key][value]; `turned`: the memory of the pass is its transpose.
-template <typename T> hipError_t launch_pass(pass_args<T> &p, bool back, const bagel_attention &b, bool turned, hipStream_t stream)
+// S is [key][value]; `turned`: the memory of the pass is its transpose.
+template <typename T> hipError_t launch_pass(bagel_attention_pass<T> &p, bool back, const bagel_attention &b, bool turned, hipStream_t stream)
 {
+    p.back = back;
     p.step_b = turned ? 1 : b.value_width;
     p.step_c = turned ? b.value_width : 1;
-    const unsigned groups = (unsigned)((int64_t)p.sequences * p.states);
-    if (groups > 0 && back) rows_kernel<T, true><<<groups, 256, 0, stream>>>(p);
-    if (groups > 0 && !back) rows_kernel<T, false><<<groups, 256, 0, stream>>>(p);
-    if (p.offsets && p.out.data && p.rows > 0) {
-        const int64_t n = (p.rows * p.states * p.qs * p.wc + 255) / 256;
-        behind_kernel<T><<<(unsigned)(n < 1024 ? n : 1024), 256, 0, stream>>>(p.rows, p.sequences, p.offsets, p.states * p.qs, p.wc, p.out);
-    }
-    return hipGetLastError();
+    return bagel_launch_attention_pass(p, stream);
 }
 
 template <typename T> hipError_t launch_attention(const bagel_attention &b, hipStream_t stream)
 {
-    pass_args<T> p = args_of<T>(b);
+    bagel_attention_pass<T> p = args_of<T>(b);
     p.qs = b.heads / b.states;
     p.ks = 1;
     p.wb = b.key_width;
     p.wc = b.value_width;
     p.scale = b.scale;
-    p.a = heads_from<T>(b.query);
-    p.b = heads_from<T>(b.key);
-    p.c = heads_from<T>(b.value);
-    p.out = heads_from<T>(b.out);
+    p.a = bagel_heads_from<T>(b.query);
+    p.b = bagel_heads_from<T>(b.key);
+    p.c = bagel_heads_from<T>(b.value);
+    p.out = bagel_heads_from<T>(b.out);
     p.first = b.initial;
     p.last = b.final_state;
     return launch_pass(p, false, b, false, stream);
@@ -185,8 +113,8 @@ template <typename T> hipError_t launch_attention(const bagel_attention &b, hipS
 template <typename T> hipError_t launch_attention_grad(const bagel_attention &b, hipStream_t stream)
 {
     const int each = b.heads / b.states;
-    pass_args<T> p = args_of<T>(b);
-    const heads_of<T> q = heads_from<T>(b.query), k = heads_from<T>(b.key), v = heads_from<T>(b.value), d = heads_from<T>(b.d_out);
+    bagel_attention_pass<T> p = args_of<T>(b);
+    const bagel_heads_of<T> q = bagel_heads_from<T>(b.query), k = bagel_heads_from<T>(b.key), v = bagel_heads_from<T>(b.value), d = bagel_heads_from<T>(b.d_out);
     hipError_t e = hipSuccess;
     if (b.d_query.data) {
         p.qs = each;
@@ -197,7 +125,7 @@ template <typename T> hipError_t launch_attention_grad(const bagel_attention &b,
         p.a = d;
         p.b = v;
         p.c = k;
-        p.out = heads_from<T>(b.d_query);
+        p.out = bagel_heads_from<T>(b.d_query);
         p.first = b.initial;
         if ((e = launch_pass(p, false, b, true, stream)) != hipSuccess) return e;
     }
@@ -211,7 +139,7 @@ template <typename T> hipError_t launch_attention_grad(const bagel_attention &b,
         p.a = k;
         p.b = q;
         p.c = d;
-        p.out = heads_from<T>(b.d_value);
+        p.out = bagel_heads_from<T>(b.d_value);
         p.first = b.d_final;
         p.last = b.d_initial;
         if ((e = launch_pass(p, true, b, false, stream)) != hipSuccess) return e;
@@ -223,7 +151,7 @@ template <typename T> hipError_t launch_attention_grad(const bagel_attention &b,
         p.a = v;
         p.b = d;
         p.c = q;
-        p.out = heads_from<T>(b.d_key);
+        p.out = bagel_heads_from<T>(b.d_key);
         p.first = b.d_final;
         p.last = nullptr;
         e = launch_pass(p, true, b, true, stream);
@@ -235,8 +163,8 @@ template <typename T> hipError_t launch_step(const bagel_attention &b, hipStream
 {
     const int64_t groups = b.rows * b.states;
     step_kernel<T><<<(unsigned)(groups < 1 << 20 ? groups : 1 << 20), 256, 0, stream>>>(
-        b.rows, b.states, b.heads / b.states, b.key_width, b.value_width, b.scale, b.log_decay, heads_from<T>(b.query), heads_from<T>(b.key),
-        heads_from<T>(b.value), heads_from<T>(b.out), b.state);
+        b.rows, b.states, b.heads / b.states, b.key_width, b.value_width, b.scale, b.log_decay, bagel_heads_from<T>(b.query), bagel_heads_from<T>(b.key),
+        bagel_heads_from<T>(b.value), bagel_heads_from<T>(b.out), b.state);
     return hipGetLastError();
 }
 
@@ -313,7 +241,12 @@ const char *check_attention(const bagel_attention *b, bool grad)
 extern "C" int64_t bagel_linear_attention_workspace(const bagel_attention *b, int32_t grad)
 {
     if (check_sizes(b)) return BAGEL_EINVAL;
-    return 0;
+    bagel_attention with = *b, without = *b;         // (whether there are offsets may not be known yet)
+    if (!with.offsets) with.offsets = reinterpret_cast<const int32_t *>(1);
+    without.offsets = nullptr;
+    (void)grad;                                      // one pass after the other has it
+    const int64_t x = memories_bytes(with, segments_of(with)), y = memories_bytes(without, segments_of(without));
+    return x > y ? x : y;
 }
 
 extern "C" int bagel_linear_attention(const bagel_attention *b, void *hip_stream)
