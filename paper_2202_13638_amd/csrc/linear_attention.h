@@ -33,4 +33,16 @@ template <typename T> struct bagel_attention_pass {
     float *memories;                                 // [slots][states][wb][wc]: behind every segment; null: one segment to a sequence
 };
 
+// Zeros in the results' rows behind the last sequence, by workgroup number `group` of `groups`.
+template <typename T> __device__ __forceinline__ void bagel_clear_behind(const bagel_attention_pass<T> &p, int64_t group, int64_t groups)
+{
+    const int64_t end = min(max((int64_t)p.offsets[p.sequences], (int64_t)0), p.rows), each = (int64_t)p.states * p.qs * p.wc, n = (p.rows - end) * each;
+    for (int64_t i = group * blockDim.x + threadIdx.x; i < n; i += groups * blockDim.x) {
+        const int64_t r = i / each;
+        const int j = (int)(i - r * each);
+        p.out.at(end + r, j / p.wc)[j % p.wc] = (T)0.0f;
+    }
+}
+
+// (wb and wc are 16 bytes at least)
 template <typename T> hipError_t bagel_launch_attention_pass(const bagel_attention_pass<T> &p, hipStream_t stream);

@@ -10,6 +10,63 @@
 
 namespace {
 
+// A pass row after row: a workgroup to a memory, an entry of its columns in each of 128 threads for half of its rows.
+template <typename T> __global__ __launch_bounds__(256) void rows_kernel(bagel_attention_pass<T> p)
+{
+    constexpr int MOST = BAGEL_ATTENTION_MAX_WIDTH;
+    __shared__ float sa[MOST], sb[MOST], sc[MOST], part[MOST];
+    const int64_t work = (int64_t)p.sequences * p.states;
+    if ((int64_t)blockIdx.x >= work) return bagel_clear_behind(p, blockIdx.x - work, gridDim.x - work);
+    const int state = blockIdx.x % p.states, sequence = blockIdx.x / p.states, t = threadIdx.x, column = t & 127, half = t >> 7;
+    int64_t begin = (int64_t)sequence * p.each, end = begin + p.each;
+    if (p.offsets) {
+        begin = min(max((int64_t)p.offsets[sequence], (int64_t)0), p.rows);
+        end = min(max((int64_t)p.offsets[sequence + 1], begin), p.rows);
+    }
+    const float decay = expf(p.log_decay[state]);
+    float S[MOST / 2];
+    const int64_t memory = ((int64_t)sequence * p.states + state) * p.wb * p.wc;
+#pragma unroll
+    for (int j = 0; j < MOST / 2; ++j) {
+        const int r = half * (MOST / 2) + j;
+        S[j] = p.first && r < p.wb && column < p.wc ? p.first[memory + r * p.step_b + column * p.step_c] : 0.0f;
+    }
+    for (int64_t n = 0; n < end - begin; ++n) {
+        const int64_t row = p.back ? end - 1 - n : begin + n;
+        if (!p.back)
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
+        for (int g = 0; g < p.ks; ++g) {
+            __syncthreads();
+            if (t < MOST) sb[t] = t < p.wb ? (float)p.b.at(row, state * p.ks + g)[t] * p.scale_b : 0.0f;
+            else sc[t - MOST] = t - MOST < p.wc ? (float)p.c.at(row, state * p.ks + g)[t - MOST] : 0.0f;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] = fmaf(sb[half * (MOST / 2) + j], sc[column], S[j]);
+        }
+        for (int g = 0; g < p.qs && p.out.data; ++g) {
+            __syncthreads();
+            if (t < MOST) sa[t] = t < p.wb ? (float)p.a.at(row, state * p.qs + g)[t] : 0.0f;
+            __syncthreads();
+            float o = 0.0f;
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) o = fmaf(sa[half * (MOST / 2) + j], S[j], o);
+            if (half) part[column] = o;
+            __syncthreads();
+            if (!half && column < p.wc) p.out.at(row, state * p.qs + g)[column] = (T)((o + part[column]) * p.scale);
+        }
+        if (p.back)
+#pragma unroll
+            for (int j = 0; j < MOST / 2; ++j) S[j] *= decay;
+    }
+    if (!p.last) return;
+#pragma unroll
+    for (int j = 0; j < MOST / 2; ++j) {
+        const int r = half * (MOST / 2) + j;
+        if (r < p.wb && column < p.wc) p.last[memory + r * p.step_b + column * p.step_c] = S[j];
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, bagel_heads_of<T> q,
                                                    bagel_heads_of<T> k, bagel_heads_of<T> v, bagel_heads_of<T> out, float *state)
@@ -40,11 +97,13 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
     }
 }
 
-// Rows of a segment: enough segments for the card, but no shorter than is worth a memory that is written and read.
+// Rows of a segment: enough segments for the card, but no shorter than is worth a memory that is written and read.  Where there are sequences enough, they are
+// left whole, and only one that is far longer than the others is shared out.
 int64_t segment_rows(const bagel_attention &b)
 {
-    constexpr int64_t LEAST = 256, WANTED = 768;
-    const int64_t rows = b.rows * b.states / WANTED, chunk = BAGEL_ATTENTION_CHUNK;
+    constexpr int64_t LEAST = 256, WANTED = 768, chunk = BAGEL_ATTENTION_CHUNK;
+    int64_t rows = b.rows * b.states / WANTED;
+    if (b.sequences > 0 && (int64_t)b.sequences * b.states >= 512) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
     return rows < LEAST ? LEAST : (rows + chunk - 1) / chunk * chunk;
 }
 
@@ -84,13 +143,17 @@ template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
     return p;
 }
 
-// S is [key][value]; `turned`: the memory of the pass is its transpose.
+// S is [key][value]; `turned`: the memory of the pass is its transpose.  The matrix kernels load packs of 16 bytes; heads that are shorter than that go row by row.
 template <typename T> hipError_t launch_pass(bagel_attention_pass<T> &p, bool back, const bagel_attention &b, bool turned, hipStream_t stream)
 {
     p.back = back;
     p.step_b = turned ? 1 : b.value_width;
     p.step_c = turned ? b.value_width : 1;
-    return bagel_launch_attention_pass(p, stream);
+    constexpr int PACK = 16 / sizeof(T);
+    if (p.wb >= PACK && p.wc >= PACK) return bagel_launch_attention_pass(p, stream);
+    const int64_t work = (int64_t)p.sequences * p.states, clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
+    if (work + clear > 0) rows_kernel<T><<<(unsigned)(work + clear), 256, 0, stream>>>(p);
+    return hipGetLastError();
 }
 
 template <typename T> hipError_t launch_attention(const bagel_attention &b, hipStream_t stream)
