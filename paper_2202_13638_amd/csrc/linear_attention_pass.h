@@ -119,17 +119,11 @@ template <typename T, int W, int THREADS> struct incoming {
     using in = packs_of<T, W, THREADS>;
     static constexpr int V = in::V;
     typename in::pack x[in::count];
-    int64_t first, on;           // entries from the first of the 64 rows to the thread's first pack, and from pack to pack
-    __device__ __forceinline__ void start(const bagel_heads_of<T> &h, int step, int width)
+    __device__ __forceinline__ void load(const T *from, int64_t stride, int width)
     {
-        first = (int64_t)(step * in::row(0)) * h.stride + min(in::column(), width - V);
-        on = (int64_t)(step * in::apart) * h.stride;
-    }
-    __device__ __forceinline__ void load(const T *from)
-    {
-        from += first;
+        from += in::row(0) * stride + min(in::column(), width - V);
 #pragma unroll
-        for (int k = 0; k < in::count; ++k) x[k] = reinterpret_cast<const bagel_loose_pack<T, V> *>(from + k * on)->x;
+        for (int k = 0; k < in::count; ++k) x[k] = reinterpret_cast<const bagel_loose_pack<T, V> *>(from + k * (in::apart * stride))->x;
     }
     __device__ __forceinline__ void load_few(const T *from, int n, int64_t stride, int width)
     {
@@ -288,14 +282,19 @@ __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention
     __shared__ tile<T, WC> sc;
     __shared__ tile<T, SUMS ? 16 : WB> sa;
     __shared__ tile<T, SUMS ? 16 : CHUNK> sp;
-    __shared__ tile<T, SUMS ? 16 : WC> so;           // results, on their way to memory while the next step's tiles come
+    // Results go through shared memory, and from there while the next step's tiles come, so that rows are written in packs; in 32 bits a lane has a pack
+    constexpr bool THROUGH = !SUMS && sizeof(T) == 2;
+    __shared__ tile<T, THROUGH ? WC : 16> so;
     __shared__ int sp_exponent[4][2];
     __shared__ floats weight_out[CHUNK / 4];         // powers of l from the rows to the memory behind the chunk
     __shared__ floats weight_p[SUMS ? 1 : 3][2][64]; // and between rows of a piece of P (a lane's eight entries), that begins 0, 16 and 32 rows before
     const int64_t segments = p.slots * p.states;
     if ((int64_t)blockIdx.x >= segments) return bagel_clear_behind(p, blockIdx.x - segments, gridDim.x - segments);
-    const int64_t slot = blockIdx.x / p.states;
-    const int state = blockIdx.x % p.states;
+    // Workgroups go to the eight dies in turn.  Each die takes segments that follow each other, so that the heads of the same rows, which lie side by side in
+    // memory, are read by one.
+    const int64_t die = blockIdx.x % 8, work = die * (segments / 8) + min(die, segments % 8) + blockIdx.x / 8;
+    const int64_t slot = work / p.states;
+    const int state = (int)(work - slot * p.states);
     const place at = place_of(p, slot);
     if (!at.there || (SUMS && at.last)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, j16 = lane & 15;
@@ -342,42 +341,50 @@ __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention
         if constexpr (!SUMS) clear(sa, p.wb);
     }
     const int heads = HEADS == MANY_B ? p.ks : HEADS == MANY_A && !SUMS ? p.qs : 1;
-    incoming<T, SUMS ? 64 : WB, THREADS> na;
-    incoming<T, WB, THREADS> nb;
-    incoming<T, WC, THREADS> nc;
-    if constexpr (!SUMS) na.start(p.a, step, p.wb);
-    nb.start(p.b, step, p.wb);
-    nc.start(p.c, step, p.wc);
     const auto head_a = [&](int h) { return HEADS == MANY_A ? state * heads + h : state; };
     const auto head_b = [&](int h) { return HEADS == MANY_B ? state * heads + h : state; };
-    // The tiles of a step, on their way: of head h, the rows from `base` on
-    const auto ask = [&](int64_t base, int h) {
-        if constexpr (!SUMS)
-            if (HEADS != MANY_B || h == 0) na.load(p.a.at(base, head_a(h)));
-        if (HEADS == MANY_B || h == 0) {
-            nb.load(p.b.at(base, head_b(h)));
-            nc.load(p.c.at(base, head_b(h)));
+    // The tiles of a step, on their way: two steps' at a time, as one alone would leave too little of the memory's rate in use
+    struct tiles {
+        incoming<T, SUMS ? 64 : WB, THREADS> a;
+        incoming<T, WB, THREADS> b;
+        incoming<T, WC, THREADS> c;
+    } coming[2];
+    const auto ask = [&](tiles &to, int64_t base, int h) {
+        // (those of every step come last: what is waited for is counted from there, whether there were others or not)
+        const auto ask_a = [&] {
+            if constexpr (!SUMS) to.a.load(p.a.at(base, head_a(h)), step * p.a.stride, p.wb);
+        };
+        const auto ask_b = [&] {
+            to.b.load(p.b.at(base, head_b(h)), step * p.b.stride, p.wb);
+            to.c.load(p.c.at(base, head_b(h)), step * p.c.stride, p.wc);
+        };
+        if constexpr (HEADS == MANY_B) {
+            if (h == 0) ask_a();
+            ask_b();
+        } else {
+            if (h == 0) ask_b();
+            ask_a();
         }
     };
-    const auto ask_few = [&](int h, int n) {
+    const auto ask_few = [&](tiles &to, int h, int n) {
         if constexpr (!SUMS)
-            if (HEADS != MANY_B || h == 0) na.load_few(p.a.at(at.base, head_a(h)), n, step * p.a.stride, p.wb);
+            if (HEADS != MANY_B || h == 0) to.a.load_few(p.a.at(at.base, head_a(h)), n, step * p.a.stride, p.wb);
         if (HEADS == MANY_B || h == 0) {
-            nb.load_few(p.b.at(at.base, head_b(h)), n, step * p.b.stride, p.wb);
-            nc.load_few(p.c.at(at.base, head_b(h)), n, step * p.c.stride, p.wc);
+            to.b.load_few(p.b.at(at.base, head_b(h)), n, step * p.b.stride, p.wb);
+            to.c.load_few(p.c.at(at.base, head_b(h)), n, step * p.c.stride, p.wc);
         }
     };
     floats O[HEADS == MANY_B ? 4 : 1];
     // One step: head h of the chunk at `base`, of which n rows are there, whose tiles were asked for.  `next` asks for the next one's; `before` takes away what
     // the step before left in `so`.
-    const auto go = [&](int h, const int n, auto &&before, auto &&next) {
+    const auto go = [&](const tiles &come, int h, const int n, T *out, auto &&before, auto &&next) {
         __syncthreads();
         before();
         if constexpr (!SUMS)
-            if (HEADS != MANY_B || h == 0) na.put(sa, pack_b, n, p.wb);
+            if (HEADS != MANY_B || h == 0) come.a.put(sa, pack_b, n, p.wb);
         if (HEADS == MANY_B || h == 0) {
-            nb.put(sb, pack_b, n, p.wb);
-            nc.put(sc, pack_c, n, p.wc);
+            come.b.put(sb, pack_b, n, p.wb);
+            come.c.put(sc, pack_c, n, p.wc);
         }
         if (n != CHUNK) weigh_out(n);
         __syncthreads();
@@ -532,47 +539,80 @@ __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention
                 bagel_pack<T, 4> x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = (T)(o[j] * p.scale);
-                so.entries(entries_o, it, wave) = x;
+                if constexpr (THROUGH) {
+                    so.entries(entries_o, it, wave) = x;
+                } else {
+                    const int first = 16 * wave + 4 * g;
+                    if (16 * it + j16 >= n || first >= p.wc) continue;
+                    T *to = out + (16 * it + j16) * (step * p.out.stride) + first;
+                    if (first + 4 <= p.wc) reinterpret_cast<bagel_loose_pack<T, 4> *>(to)->x = x;
+                    else
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (first + j < p.wc) to[j] = x[j];
+                }
             }
         }
     };
-    int64_t base = at.base, left = at.rows;
-    const int rest = (int)(left % CHUNK);
-    if (left >= CHUNK) ask(base, 0);
+    const int64_t chunks = at.rows / CHUNK;
+    const int rest = (int)(at.rows % CHUNK);
+    // The steps of whole chunks are asked for, and those of the rows that are left, as the 64 rows up to the last one; behind these the same again, which nobody
+    // reads: a branch around the loads would make every wait one for all of them.
+    int64_t ask_chunk = 0;
+    int ask_head = 0;
+    const auto ask_next = [&](tiles &to) {
+        ask(to, at.base + step * min(ask_chunk * CHUNK, at.rows - CHUNK), ask_head);
+        if (HEADS == ONE || ++ask_head == heads) {
+            ask_head = 0;
+            ++ask_chunk;
+        }
+    };
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt) asm volatile("" : "+v"(S[bt]));      // the memory is there before anything else is asked for, so that no wait in the loop is one for it
     T *ready = nullptr;                              // where the whole rows in `so` go
     const auto before = [&] {
-        if constexpr (!SUMS)
+        if constexpr (THROUGH)
             if (ready) write_rows<T, WC, THREADS>(so, pack_c, ready, step * p.out.stride, CHUNK, p.wc);
     };
-    for (; left >= CHUNK; left -= CHUNK, base += step * CHUNK) {
-        // the next chunk, or the 64 rows up to the last one
-        const int64_t next = base + step * min(left - CHUNK, (int64_t)CHUNK);
-        const auto step_of = [&](int h) {
-            go(h, CHUNK, before, [&] {
-                if (HEADS != ONE && h + 1 < heads) ask(base, h + 1);
-                else if (left > CHUNK) ask(next, 0);
-            });
-            if (!SUMS && p.out.data) ready = HEADS == MANY_B && h < heads - 1 ? nullptr : p.out.at(base, head_a(h));
-        };
-        if constexpr (HEADS == ONE) step_of(0);
-        else
-            for (int h = 0; h < heads; ++h) step_of(h);
+    int64_t chunk = 0;
+    int h = 0;
+    const auto whole_step = [&](const tiles &come, tiles &then) {
+        T *out = !SUMS && p.out.data ? p.out.at(at.base + step * (chunk * CHUNK), head_a(h)) : nullptr;
+        go(come, h, CHUNK, out, before, [&] { ask_next(then); });
+        ready = HEADS == MANY_B && h < heads - 1 ? nullptr : out;
+        if (HEADS == ONE || ++h == heads) {
+            h = 0;
+            ++chunk;
+        }
+    };
+    // Two steps to a round, after one on its own where they are odd in number; what is left is then on its way in the first place.
+    if ((chunks * heads) & 1) {
+        tiles alone;
+        ask_next(alone);
+        ask_next(coming[0]);
+        whole_step(alone, coming[1]);
+    } else if (chunks > 0) {
+        ask_next(coming[0]);
+        ask_next(coming[1]);
     }
-    if (rest > 0) {                                  // the rows that are left, of which nothing is on its way where there are no others
-        for (int h = 0; h < heads; ++h) {
-            if (h > 0 || at.rows < CHUNK) {
-                if (at.rows < CHUNK) ask_few(h, rest);
-                else ask(at.base + step * (at.rows - CHUNK), h);
-            }
-            go(h, rest, before, [] {});
-            if constexpr (!SUMS) {
+    while (chunk < chunks) {
+        whole_step(coming[0], coming[0]);
+        whole_step(coming[1], coming[1]);
+    }
+    if (rest > 0) {                                  // the rows that are left: further heads, or all of them where there are no others, are not on their way yet
+        T *out = nullptr;
+        for (h = 0; h < heads; ++h) {
+            if (chunks == 0) ask_few(coming[0], h, rest);
+            else if (h > 0) ask(coming[0], at.base + step * (at.rows - CHUNK), h);
+            if (!SUMS && p.out.data) out = p.out.at(at.base + step * (chunks * CHUNK), head_a(h));
+            go(coming[0], h, rest, out, before, [] {});
+            ready = nullptr;
+            if constexpr (THROUGH) {
                 __syncthreads();
-                if (p.out.data && (HEADS != MANY_B || h == heads - 1))
-                    write_rows<T, WC, THREADS>(so, pack_c, p.out.at(base, head_a(h)), step * p.out.stride, rest, p.wc);
-                ready = nullptr;
+                if (out && (HEADS != MANY_B || h == heads - 1)) write_rows<T, WC, THREADS>(so, pack_c, out, step * p.out.stride, rest, p.wc);
             }
         }
-    } else if constexpr (!SUMS) {
+    } else if constexpr (THROUGH) {
         __syncthreads();
         before();
     }
@@ -592,7 +632,7 @@ template <typename T> __global__ __launch_bounds__(256) void memories_kernel(bag
 {
     const int size = p.wb * p.wc;
     for (int64_t work = blockIdx.x; work < (int64_t)p.sequences * p.states * blocks; work += gridDim.x) {
-        const int i = (int)(work % blocks) * 256 + threadIdx.x, state = (int)(work / blocks % p.states), sequence = (int)(work / blocks / p.states);
+        const int state = (int)(work / blocks % p.states), sequence = (int)(work / blocks / p.states);
         int64_t length = p.each, slot;
         if (!p.offsets) {
             slot = (int64_t)sequence * max((length + p.segment - 1) / p.segment, (int64_t)1);
@@ -602,32 +642,35 @@ template <typename T> __global__ __launch_bounds__(256) void memories_kernel(bag
             slot = begin / p.segment + sequence;
         }
         const int64_t segments = (length + p.segment - 1) / p.segment, each = (int64_t)p.states * size;
-        if (i >= size || segments < 3) continue;     // (of two, the first one's is whole)
+        if (segments < 3) continue;                  // (of two, the first one's is whole)
         const float keep = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
-        float *m = p.memories + (slot * p.states + state) * size + i;
-        float s = m[0];
-        constexpr int AHEAD = 8;
-        for (int64_t k = 1; k < segments - 1; k += AHEAD) {
-            float add[AHEAD];
+        for (int i = (int)(work % blocks) * 256 + threadIdx.x; i < size; i += blocks * 256) {
+            float *m = p.memories + (slot * p.states + state) * size + i;
+            float s = m[0];
+            constexpr int AHEAD = 16;
+            for (int64_t k = 1; k < segments - 1; k += AHEAD) {
+                float add[AHEAD];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) add[j] = k + j < segments - 1 ? m[(k + j) * each] : 0.0f;
+                for (int j = 0; j < AHEAD; ++j) add[j] = k + j < segments - 1 ? m[(k + j) * each] : 0.0f;
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j)
-                if (k + j < segments - 1) m[(k + j) * each] = s = fmaf(keep, s, add[j]);
+                for (int j = 0; j < AHEAD; ++j)
+                    if (k + j < segments - 1) m[(k + j) * each] = s = fmaf(keep, s, add[j]);
+            }
         }
     }
 }
 
 template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS> hipError_t launch_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
 {
-    constexpr int THREADS = 4 * WC, ON_SIMD = sizeof(T) == 2 && WB == 64 ? WC == 64 ? 3 : 4 : 2;
+    constexpr int THREADS = 4 * WC, ON_SIMD = sizeof(T) == 4 && WB == 128 && WC == 64 ? 1 : 2;
     constexpr heads_kind SUMS_HEADS = HEADS == MANY_A ? ONE : HEADS;
     const int64_t work = p.slots * p.states;
     if (p.memories) {
         chunks_kernel<T, WB, WC, WHOLE, true, SUMS_HEADS, ON_SIMD><<<(unsigned)work, THREADS, 0, stream>>>(p);
-        const int blocks = (p.wb * p.wc + 255) / 256;
-        const int64_t all = (int64_t)p.sequences * p.states * blocks;
-        memories_kernel<T><<<(unsigned)(all < 1 << 20 ? all : 1 << 20), 256, 0, stream>>>(p, blocks);
+        // some workgroups to a memory where there are few of them
+        const int64_t all = (int64_t)p.sequences * p.states, most = (p.wb * p.wc + 255) / 256, wanted = 1024 / all;
+        const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+        memories_kernel<T><<<(unsigned)(all * blocks < 1 << 16 ? all * blocks : 1 << 16), 256, 0, stream>>>(p, blocks);
     }
     const int64_t clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
     if (work + clear > 0) chunks_kernel<T, WB, WC, WHOLE, false, HEADS, ON_SIMD><<<(unsigned)(work + clear), THREADS, 0, stream>>>(p);
