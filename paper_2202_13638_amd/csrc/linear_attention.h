@@ -15,8 +15,10 @@ constexpr int BAGEL_ATTENTION_CHUNK = 64;            // rows that are gone throu
 
 // One linear attention: memory = decay memory + scale_b b c^T, out = scale memory^T a.  a and out have `qs` heads to a memory, b and c `ks`, of which
 // one or both are 1.  `back`: from a sequence's last row to its first, and the memory is multiplied by its decay behind a row, not before.
-// A sequence is gone through in segments of `segment` rows (of the last fewer), each by another workgroup.  Segment s of sequence i is number
-// offsets[i] / segment + i + s: that leaves room for all segments of the sequences before, whatever their lengths.
+//
+// A sequence is gone through in segments of `segment` rows (of the last fewer), each by another workgroup, which begins with the memory behind the segment
+// before.  The first segments of all sequences have the numbers 0 to sequences - 1.  Segment s >= 1 of sequence i is number
+// sequences + offsets[i] / segment + s - 1: that leaves room for those of the sequences before, whatever their lengths.
 template <typename T> struct bagel_attention_pass {
     int64_t rows;
     int sequences, each, states, qs, ks, wb, wc;     // each: rows of a sequence where there are no offsets; wb: width of a and b, wc: of c and out
@@ -27,11 +29,23 @@ template <typename T> struct bagel_attention_pass {
     bagel_heads_of<T> a, b, c, out;
     const float *first;                              // memories before the first row (gone through), null: zero
     float *last;                                     // and behind the last, null: not wanted
-    int64_t step_b, step_c;                          // of their entries: [sequences][states] times wb, wc in either order
+    int64_t step_b, step_c;                          // of a memory's entries, wb times wc in either order; [sequences][states] of them
     int64_t segment;                                 // a multiple of the chunk
-    int64_t slots;                                   // numbers of segments; 1 for each sequence where `segment` holds any of them
-    float *memories;                                 // [slots][states][wb][wc]: behind every segment; null: one segment to a sequence
+    int64_t further;                                 // numbers of segments that are not the first of their sequence
+    float *memories;                                 // [sequences + further][states][..]: behind every segment but the last; null: one segment to a sequence
 };
+
+// The memories behind all segments but the last of their sequences, of one pass or two (with as many sequences, rows, states and segments).
+template <typename T> hipError_t bagel_launch_attention_memories(const bagel_attention_pass<T> *p, int n, hipStream_t stream);
+
+// The gradients of keys and values in one pass: `p` is that of the values (memory R, a = key, b = query, c = gradient of the results), `q` that of the
+// keys (R transposed, a = value, b = gradient of the results, c = query).  Only where bagel_attention_keys_fit.
+template <typename T> hipError_t bagel_launch_attention_keys(const bagel_attention_pass<T> &p, const bagel_attention_pass<T> &q, hipStream_t stream);
+// (Two memories of wide heads and the sums over several heads of queries are more than a lane's registers hold; in 32 bits the tiles leave room for one workgroup only.)
+template <typename T> inline bool bagel_attention_keys_fit(int key_width, int value_width, int heads_to_a_memory)
+{
+    return sizeof(T) == 2 && (key_width <= 64) == (value_width <= 64) && (key_width <= 64 || heads_to_a_memory == 1);
+}
 
 // Zeros in the results' rows behind the last sequence, by workgroup number `group` of `groups`.
 template <typename T> __device__ __forceinline__ void bagel_clear_behind(const bagel_attention_pass<T> &p, int64_t group, int64_t groups)

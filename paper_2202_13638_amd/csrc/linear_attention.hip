@@ -97,38 +97,34 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
     }
 }
 
-// Rows of a segment: enough segments for the card, but no shorter than is worth a memory that is written and read.  Where there are sequences enough, they are
-// left whole, and only one that is far longer than the others is shared out.
+// Rows of a segment: as many segments as the card takes at a time, some less, as one more would be a round of its own; but no shorter than is worth a memory that is
+// written and read.  Where there are sequences enough, they are left whole, and only one that is far longer than the others is shared out.
 int64_t segment_rows(const bagel_attention &b)
 {
-    constexpr int64_t LEAST = 256, WANTED = 768, chunk = BAGEL_ATTENTION_CHUNK;
-    int64_t rows = b.rows * b.states / WANTED;
-    if (b.sequences > 0 && (int64_t)b.sequences * b.states >= 512) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
+    constexpr int64_t LEAST = 512, chunk = BAGEL_ATTENTION_CHUNK;
+    const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 240 : 480;       // one or two workgroups to a compute unit
+    int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
+    if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
     return rows < LEAST ? LEAST : (rows + chunk - 1) / chunk * chunk;
 }
 
-// Numbers of segments, and whether a sequence may have more than one.
+// A segment's rows, and how many numbers there are for segments that are not the first of their sequence.
 struct segments {
-    int64_t rows, slots;
-    bool several;
+    int64_t rows, further;
 };
-segments segments_of(const bagel_attention &b)
+segments segments_of(const bagel_attention &b, bool offsets)
 {
-    segments s = {segment_rows(b), 0, false};
-    const int64_t longest = b.sequences == 0 ? 0 : b.offsets ? b.rows : b.rows / b.sequences;
-    s.several = longest > s.rows;
-    if (!s.several) s.rows = longest > 0 ? (longest + BAGEL_ATTENTION_CHUNK - 1) / BAGEL_ATTENTION_CHUNK * BAGEL_ATTENTION_CHUNK : BAGEL_ATTENTION_CHUNK;
-    s.slots = b.offsets ? b.rows / s.rows + b.sequences : b.sequences * (longest > 0 ? (longest + s.rows - 1) / s.rows : 1);
-    return s;
+    const int64_t rows = segment_rows(b), each = b.sequences > 0 ? b.rows / b.sequences : 0;
+    return {rows, offsets ? (b.rows > rows ? b.rows / rows : 0) : each > 0 ? (each - 1) / rows * b.sequences : 0};
 }
-int64_t memories_bytes(const bagel_attention &b, const segments &s)
+int64_t memories_floats(const bagel_attention &b, const segments &s)
 {
-    return s.several ? s.slots * b.states * b.key_width * b.value_width * (int64_t)sizeof(float) : 0;
+    return s.further > 0 ? (b.sequences + s.further) * b.states * b.key_width * b.value_width : 0;
 }
 
 template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
 {
-    const segments s = segments_of(b);
+    const segments s = segments_of(b, b.offsets);
     bagel_attention_pass<T> p{};
     p.rows = b.rows;
     p.sequences = b.sequences;
@@ -138,31 +134,37 @@ template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
     p.log_decay = b.log_decay;
     p.scale = p.scale_b = 1.0f;
     p.segment = s.rows;
-    p.slots = s.slots;
-    p.memories = s.several ? (float *)b.workspace : nullptr;
+    p.further = s.further;
+    p.qs = p.ks = 1;
     return p;
 }
 
-// S is [key][value]; `turned`: the memory of the pass is its transpose.  The matrix kernels load packs of 16 bytes; heads that are shorter than that go row by row.
-template <typename T> hipError_t launch_pass(bagel_attention_pass<T> &p, bool back, const bagel_attention &b, bool turned, hipStream_t stream)
+// S is [key][value]; a pass whose memory is its transpose.
+template <typename T> void turned(bagel_attention_pass<T> &p, const bagel_attention &b, bool turned)
 {
-    p.back = back;
+    p.wb = turned ? b.value_width : b.key_width;
+    p.wc = turned ? b.key_width : b.value_width;
     p.step_b = turned ? 1 : b.value_width;
     p.step_c = turned ? b.value_width : 1;
-    constexpr int PACK = 16 / sizeof(T);
-    if (p.wb >= PACK && p.wc >= PACK) return bagel_launch_attention_pass(p, stream);
+}
+
+// The matrix kernels load packs of 16 bytes; heads that are shorter than that go row by row.
+template <typename T> bool by_rows(const bagel_attention &b) { return b.key_width < 16 / (int)sizeof(T) || b.value_width < 16 / (int)sizeof(T); }
+
+template <typename T> hipError_t launch_pass(const bagel_attention_pass<T> &p, const bagel_attention &b, hipStream_t stream)
+{
+    if (!by_rows<T>(b)) return bagel_launch_attention_pass(p, stream);
     const int64_t work = (int64_t)p.sequences * p.states, clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
     if (work + clear > 0) rows_kernel<T><<<(unsigned)(work + clear), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 
-template <typename T> hipError_t launch_attention(const bagel_attention &b, hipStream_t stream)
+// S along the rows, and R from the last row to the first.
+template <typename T> bagel_attention_pass<T> forward_pass(const bagel_attention &b)
 {
     bagel_attention_pass<T> p = args_of<T>(b);
+    turned(p, b, false);
     p.qs = b.heads / b.states;
-    p.ks = 1;
-    p.wb = b.key_width;
-    p.wc = b.value_width;
     p.scale = b.scale;
     p.a = bagel_heads_from<T>(b.query);
     p.b = bagel_heads_from<T>(b.key);
@@ -170,55 +172,67 @@ template <typename T> hipError_t launch_attention(const bagel_attention &b, hipS
     p.out = bagel_heads_from<T>(b.out);
     p.first = b.initial;
     p.last = b.final_state;
-    return launch_pass(p, false, b, false, stream);
+    p.memories = (float *)b.workspace;
+    return p;
+}
+template <typename T> bagel_attention_pass<T> backward_pass(const bagel_attention &b, float *memories)
+{
+    bagel_attention_pass<T> p = args_of<T>(b);
+    turned(p, b, false);
+    p.back = true;
+    p.ks = b.heads / b.states;
+    p.scale_b = b.scale;
+    p.a = bagel_heads_from<T>(b.key);
+    p.b = bagel_heads_from<T>(b.query);
+    p.c = bagel_heads_from<T>(b.d_out);
+    p.out = bagel_heads_from<T>(b.d_value);
+    p.first = b.d_final;
+    p.last = b.d_initial;
+    p.memories = memories;
+    return p;
+}
+
+template <typename T> hipError_t launch_attention(const bagel_attention &b, hipStream_t stream)
+{
+    const bagel_attention_pass<T> p = forward_pass<T>(b);
+    if (!by_rows<T>(b))
+        if (const hipError_t e = bagel_launch_attention_memories(&p, 1, stream)) return e;
+    return launch_pass(p, b, stream);
 }
 
 template <typename T> hipError_t launch_attention_grad(const bagel_attention &b, hipStream_t stream)
 {
-    const int each = b.heads / b.states;
-    bagel_attention_pass<T> p = args_of<T>(b);
-    const bagel_heads_of<T> q = bagel_heads_from<T>(b.query), k = bagel_heads_from<T>(b.key), v = bagel_heads_from<T>(b.value), d = bagel_heads_from<T>(b.d_out);
+    const bool queries = b.d_query.data, values = b.d_value.data || b.d_initial, keys = b.d_key.data;
+    bagel_attention_pass<T> s = forward_pass<T>(b), r = backward_pass<T>(b, (float *)b.workspace + memories_floats(b, segments_of(b, b.offsets)));
     hipError_t e = hipSuccess;
-    if (b.d_query.data) {
-        p.qs = each;
-        p.ks = 1;
-        p.wb = b.value_width;
-        p.wc = b.key_width;
-        p.scale = b.scale;
-        p.a = d;
-        p.b = v;
-        p.c = k;
-        p.out = bagel_heads_from<T>(b.d_query);
-        p.first = b.initial;
-        if ((e = launch_pass(p, false, b, true, stream)) != hipSuccess) return e;
+    if (!by_rows<T>(b)) {
+        const bagel_attention_pass<T> both[2] = {s, r};
+        if (queries && (values || keys)) e = bagel_launch_attention_memories(both, 2, stream);
+        else if (queries) e = bagel_launch_attention_memories(&s, 1, stream);
+        else if (values || keys) e = bagel_launch_attention_memories(&r, 1, stream);
     }
-    p = args_of<T>(b);
-    p.qs = 1;
-    p.ks = each;
-    if (b.d_value.data || b.d_initial) {
-        p.wb = b.key_width;
-        p.wc = b.value_width;
-        p.scale_b = b.scale;
-        p.a = k;
-        p.b = q;
-        p.c = d;
-        p.out = bagel_heads_from<T>(b.d_value);
-        p.first = b.d_final;
-        p.last = b.d_initial;
-        if ((e = launch_pass(p, true, b, false, stream)) != hipSuccess) return e;
+    if (e == hipSuccess && queries) {
+        turned(s, b, true);
+        s.a = bagel_heads_from<T>(b.d_out);
+        s.b = bagel_heads_from<T>(b.value);
+        s.c = bagel_heads_from<T>(b.key);
+        s.out = bagel_heads_from<T>(b.d_query);
+        s.last = nullptr;
+        e = launch_pass(s, b, stream);
     }
-    if (b.d_key.data) {
-        p.wb = b.value_width;
-        p.wc = b.key_width;
-        p.scale_b = b.scale;
-        p.a = v;
-        p.b = d;
-        p.c = q;
-        p.out = bagel_heads_from<T>(b.d_key);
-        p.first = b.d_final;
-        p.last = nullptr;
-        e = launch_pass(p, true, b, true, stream);
+    bagel_attention_pass<T> t = r;
+    turned(t, b, true);
+    t.a = bagel_heads_from<T>(b.value);
+    t.b = r.c;
+    t.c = r.b;
+    t.out = bagel_heads_from<T>(b.d_key);
+    t.last = nullptr;
+    if constexpr (sizeof(T) == 2) {
+        if (e == hipSuccess && keys && b.d_value.data && !by_rows<T>(b) && bagel_attention_keys_fit<T>(b.key_width, b.value_width, r.ks))
+            return bagel_launch_attention_keys(r, t, stream);
     }
+    if (e == hipSuccess && values) e = launch_pass(r, b, stream);
+    if (e == hipSuccess && keys) e = launch_pass(t, b, stream);
     return e;
 }
 
@@ -304,12 +318,8 @@ const char *check_attention(const bagel_attention *b, bool grad)
 extern "C" int64_t bagel_linear_attention_workspace(const bagel_attention *b, int32_t grad)
 {
     if (check_sizes(b)) return BAGEL_EINVAL;
-    bagel_attention with = *b, without = *b;         // (whether there are offsets may not be known yet)
-    if (!with.offsets) with.offsets = reinterpret_cast<const int32_t *>(1);
-    without.offsets = nullptr;
-    (void)grad;                                      // one pass after the other has it
-    const int64_t x = memories_bytes(with, segments_of(with)), y = memories_bytes(without, segments_of(without));
-    return x > y ? x : y;
+    const int64_t with = memories_floats(*b, segments_of(*b, true)), without = memories_floats(*b, segments_of(*b, false));      // (which it is may not be known yet)
+    return (with > without ? with : without) * (grad ? 2 : 1) * (int64_t)sizeof(float);
 }
 
 extern "C" int bagel_linear_attention(const bagel_attention *b, void *hip_stream)

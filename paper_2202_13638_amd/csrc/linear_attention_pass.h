@@ -6,6 +6,8 @@
 // No power of l is negative, so nothing grows that the definition does not let grow.
 #pragma once
 
+#include <type_traits>
+
 #include "linear_attention.h"
 
 namespace {
@@ -185,10 +187,12 @@ template <typename T, int W> __device__ __forceinline__ void clear(tile<T, W> &t
 }
 
 // The wait states between the products in 32 bits and whatever uses their results, ahead of a branch: the compiler may count them along the longer way only.
+__device__ __forceinline__ void settle(floats &x) { asm volatile("s_nop 9" : "+v"(x)); }
 template <int N> __device__ __forceinline__ void settle(floats (&x)[N])
 {
-    static_assert(N == 4 || N == 8, "a memory's tiles");
-    if constexpr (N == 4) asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+    static_assert(N == 2 || N == 4 || N == 8, "a memory's tiles, or a piece of P");
+    if constexpr (N == 2) asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]));
+    else if constexpr (N == 4) asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
     else asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
 }
 
@@ -222,476 +226,740 @@ struct place {
     int sequence;
     int64_t base;                // its first row, in the order they are gone through
     int64_t rows;
-    bool first, last;            // of its sequence
-    bool there;
+    int64_t before;              // the number of the segment before, -1: it is the first
+    bool last, there;
 };
 
-// Which sequence a number of a segment belongs to: the last that does not begin behind it.  All lanes look, at one in 64 of the sequences each time.
-template <typename T> __device__ __forceinline__ place place_of(const bagel_attention_pass<T> &p, int64_t slot)
+// A sequence's rows; offsets that break the rules lead nowhere outside.
+template <typename T> __device__ __forceinline__ void sequence_rows(const bagel_attention_pass<T> &p, int i, int64_t &begin, int64_t &end)
 {
-    place r;
-    int64_t begin, end, s;
     if (!p.offsets) {
-        const int64_t each = max((p.each + p.segment - 1) / p.segment, (int64_t)1);
-        r.sequence = (int)(slot / each);
-        s = slot - r.sequence * each;
-        begin = (int64_t)r.sequence * p.each;
+        begin = (int64_t)i * p.each;
         end = begin + p.each;
     } else {
-        const int lane = threadIdx.x & 63;
-        const auto number = [&](int i) { return (int64_t)p.offsets[i] / p.segment + i; };
-        int lo = 0, count = p.sequences;
-        while (count > 1) {
-            const int step = (count + 63) / 64;
-            const uint64_t ok = __ballot(lane * step < count && number(lo + min(lane * step, count - 1)) <= slot);
-            const int k = max(__popcll(ok) - 1, 0);
-            lo += k * step;
-            count = min(step, count - k * step);
-        }
-        r.sequence = __builtin_amdgcn_readfirstlane(lo);
-        // (offsets that break the rules lead nowhere outside of the rows)
-        begin = min(max((int64_t)p.offsets[r.sequence], (int64_t)0), p.rows);
-        end = min(max((int64_t)p.offsets[r.sequence + 1], begin), p.rows);
-        s = slot - (begin / p.segment + r.sequence);
+        begin = min(max((int64_t)p.offsets[i], (int64_t)0), p.rows);
+        end = min(max((int64_t)p.offsets[i + 1], begin), p.rows);
     }
+}
+template <typename T> __device__ __forceinline__ int64_t further_of_each(const bagel_attention_pass<T> &p) { return p.each > 0 ? (p.each - 1) / p.segment : 0; }
+
+template <typename T> __device__ __forceinline__ place place_of(const bagel_attention_pass<T> &p, int64_t number)
+{
+    place r;
+    int64_t s = 0;
+    if (number < p.sequences) {
+        r.sequence = (int)number;
+        r.before = -1;
+    } else {
+        const int64_t further = number - p.sequences;
+        if (!p.offsets) {
+            const int64_t each = max(further_of_each(p), (int64_t)1);
+            r.sequence = (int)(further / each);
+            s = further - r.sequence * each + 1;
+        } else {
+            // The last sequence whose further segments do not begin behind it.  All lanes look, at one in 64 of the sequences each time.
+            const int lane = threadIdx.x & 63;
+            int lo = 0, count = p.sequences;
+            while (count > 1) {
+                const int step = (count + 63) / 64;
+                const uint64_t ok = __ballot(lane * step < count && (int64_t)p.offsets[lo + min(lane * step, count - 1)] / p.segment <= further);
+                const int k = max(__popcll(ok) - 1, 0);
+                lo += k * step;
+                count = min(step, count - k * step);
+            }
+            r.sequence = __builtin_amdgcn_readfirstlane(lo);
+            s = further - min(max((int64_t)p.offsets[r.sequence], (int64_t)0), p.rows) / p.segment + 1;
+        }
+        r.before = s == 1 ? r.sequence : number - 1;
+    }
+    int64_t begin, end;
+    sequence_rows(p, r.sequence, begin, end);
     const int64_t length = end - begin, from = s * p.segment;
-    r.first = s == 0;
-    r.there = s == 0 || (s > 0 && from < length);
+    r.there = number < p.sequences || (s > 0 && from < length);
     r.rows = min(length - from, p.segment);
     r.last = from + p.segment >= length;
     r.base = p.back ? end - 1 - from : begin + from;
     return r;
 }
 
+// Workgroups go to the eight dies in turn.  Each die takes work that follows each other, so that the heads of the same rows, which lie side by side in memory,
+// are read by one: the first segments, and then the further ones, which may not be there.
+__device__ __forceinline__ int64_t by_dies(int64_t group, int64_t first, int64_t all)
+{
+    const int64_t begin = group < first ? 0 : first, n = group < first ? first : all - first, i = group - begin, die = i % 8;
+    return begin + die * (n / 8) + min(die, n % 8) + i / 8;
+}
+
+// A lane's parts of addresses in shared memory.
+template <typename T, int WB, int WC, int THREADS> struct lane_parts {
+    const int along_a = tile<T, WB>::lane_along(), along_p = tile<T, CHUNK>::lane_along(), spread_b = tile<T, WB>::lane_spread();
+    const int across_b = tile<T, WB>::lane_across(true), across_c = tile<T, WC>::lane_across(false), entries_o = tile<T, WC>::lane_entries();
+    const int pack_b = packs_of<T, WB, THREADS>::lane_part(), pack_c = packs_of<T, WC, THREADS>::lane_part();
+};
+
+// Powers of l that are the same for all chunks, in shared memory.
+struct powers {
+    floats out[CHUNK / 4];       // from the rows to the memory behind the chunk, times scale_b
+    floats p[3][2][64];          // between rows of a piece of P (a lane's eight entries) that begins 0, 16 and 32 rows before, times scale_b
+    int exponent[2][4][2];       // of the pieces (float16)
+    __device__ __forceinline__ void weigh_out(float l2, int behind, float scale_b, int n)
+    {
+        if ((int)threadIdx.x < CHUNK) reinterpret_cast<float *>(out)[threadIdx.x] = power(l2, max(n - 1 - (int)threadIdx.x, 0) + behind) * scale_b;
+    }
+    __device__ __forceinline__ void weigh_p(float l2, float scale_b)
+    {
+        const int lane = threadIdx.x & 63;
+        for (int i = threadIdx.x >> 6; i < 6; i += blockDim.x >> 6) {
+            floats x;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = 16 * (i / 2) + lane % 16 - (lane / 16 * 8 + i % 2 * 4 + j);
+                x[j] = d >= 0 ? power(l2, d) * scale_b : 0.0f;
+            }
+            p[i / 2][i % 2][lane] = x;
+        }
+    }
+};
+
+// A wave's 16 columns of a memory in float32, a lane one of them: S[2 kb + half][j] is entry 32 kb + 8 g + 4 half + j of it.
+template <int NB> __device__ __forceinline__ int memory_row(int bt, int j) { return bt / 2 * 32 + (threadIdx.x & 63) / 16 * 8 + bt % 2 * 4 + j; }
+template <int NB> __device__ __forceinline__ void read_memory(floats (&S)[NB], const float *from, int64_t step_b, int64_t step_c, int column, int wb, int wc)
+{
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S[bt][j] = from && memory_row<NB>(bt, j) < wb && column < wc ? from[memory_row<NB>(bt, j) * step_b + column * step_c] : 0.0f;
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt) asm volatile("" : "+v"(S[bt]));      // it is there before anything else is asked for, so that no later wait is one for it
+}
+template <int NB> __device__ __forceinline__ void write_memory(const floats (&S)[NB], float *to, int64_t step_b, int64_t step_c, int column, int wb, int wc)
+{
+    asm volatile("" : "+v"(step_b));                 // its multiples are not kept from the beginning: they would take all scalar registers
+    if (!to || column >= wc) return;
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (memory_row<NB>(bt, j) < wb) to[memory_row<NB>(bt, j) * step_b + column * step_c] = S[bt][j];
+}
+
+// A memory as operands, and the exponent that was taken off (float16).
+template <typename T, int NB> __device__ __forceinline__ int as_operands(const floats (&S)[NB], operand<T> (&s)[NB / 2])
+{
+    int e = 0;
+    float down = 1.0f;
+    if constexpr (NARROW<T>) {
+        float top = 0.0f;
+#pragma unroll
+        for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(S[bt][j]));
+        e = exponent_for(wave_largest(top));
+        down = ldexpf(1.0f, -e);
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB / 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[kb][i] = (T)(NARROW<T> ? S[2 * kb + i / 4][i % 4] * down : S[2 * kb + i / 4][i % 4]);
+    return e;
+}
+
+// A piece of P, rows 16 it by rows 32 kb of b, transposed: a lane has eight entries of a row.
+template <typename T, int W>
+__device__ __forceinline__ void make_piece(tile<T, W> &a, const tile<T, W> &b, tile<T, CHUNK> &to, powers &w, int which, int it, int kb, float tile_on, int along_a, int along_p,
+                                           int spread_b)
+{
+    const int lane = threadIdx.x & 63, before = it - 2 * kb;
+    floats P[2] = {(floats)0.0f, (floats)0.0f};
+#pragma unroll
+    for (int q = 0; q < W / 32; ++q) {
+        const operand<T> x = a.along(along_a, it, q);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) P[half] = product(b.spread(spread_b, kb, half, q), x, P[half]);
+    }
+    if constexpr (sizeof(T) == 4) settle(P);
+    const float far = before == 3 ? tile_on : 1.0f;  // 48 rows before: l^16 more than 32
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const floats x = w.p[min(before, 2)][half][lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) P[half][j] *= x[j] * far;
+    }
+    float down = 1.0f;
+    if constexpr (NARROW<T>) {
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(P[i / 4][i % 4]));
+        const int e = exponent_for(wave_largest(top));
+        down = ldexpf(1.0f, -e);
+        if (lane == 0) w.exponent[which][it][kb] = e;
+    }
+    operand<T> x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (T)(NARROW<T> ? P[i / 4][i % 4] * down : P[i / 4][i % 4]);
+    to.along(along_p, it, kb) = x;
+}
+
+// The six pieces of P that are not zero, shared out among the waves; `shift`: which wave comes first.
+template <int WAVES, typename T, int W, typename L>
+__device__ __forceinline__ void make_pieces(tile<T, W> &a, const tile<T, W> &b, tile<T, CHUNK> &to, powers &w, int which, float tile_on, int along_a, int spread_b, const L &l, int wave)
+{
+    const auto piece = [&](int it, int kb) { make_piece(a, b, to, w, which, it, kb, tile_on, along_a, l.along_p, spread_b); };
+    if constexpr (WAVES == 4) {
+        piece(wave < 2 ? 3 : 2, wave & 1);
+        if (wave >= 2) piece(wave - 2, 0);
+    } else {
+        if (wave < 6) piece(wave < 4 ? 3 - wave / 2 : wave - 4, wave < 4 ? wave & 1 : 0);
+    }
+}
+
+// The memory behind a chunk: S times `keep`, and the rows of b times those of c.  c is weighed, and what that makes is held to 24 bits as a sum of operands (22
+// in float16): the memory is kept in float32, and one rounding to 8 or 11 bits of every row would be left in it.
+template <typename T, int W, int NB> __device__ __forceinline__ void remember(floats (&S)[NB], const tile<T, W> &b, const operand<T> (&c)[2], const powers &p, float keep, int across_b)
+{
+    const int g = (threadIdx.x & 63) >> 4;
+    int e = 0;
+    float w[2][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const floats lo = p.out[8 * t + 2 * g], hi = p.out[8 * t + 2 * g + 1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[t][i] = (float)c[t][i] * (i < 4 ? lo[i & 3] : hi[i & 3]);
+    }
+    if constexpr (NARROW<T>) {
+        float top = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(w[t][i]));
+        e = exponent_for(wave_largest(top));
+        const float down = ldexpf(1.0f, -e);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[t][i] *= down;
+    }
+    constexpr int PARTS = sizeof(T) == 4 ? 1 : NARROW<T> ? 2 : 3;
+    operand<T> part[PARTS][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) {
+                part[q][t][i] = (T)w[t][i];
+                w[t][i] -= (float)part[q][t][i];
+            }
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt) {
+        const operand<T> b0 = b.across_spread(across_b, 0, bt / 2, bt % 2), b1 = b.across_spread(across_b, 1, bt / 2, bt % 2);
+        floats x = NARROW<T> ? (floats)0.0f : S[bt];
+        if constexpr (!NARROW<T>)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] *= keep;
+#pragma unroll
+        for (int q = PARTS - 1; q >= 0; --q) {
+            x = product(b0, part[q][0], x);
+            x = product(b1, part[q][1], x);
+        }
+        if constexpr (NARROW<T>) {
+            const float up = ldexpf(1.0f, e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(S[bt][j], keep, x[j] * up);
+        }
+        S[bt] = x;
+    }
+    if constexpr (sizeof(T) == 4) settle(S);
+}
+
+// Rows 16 it of the results, a wave's 16 columns, transposed: a lane has four entries of a row.  o: what the memory before the chunk gives them (`weight`: the power of l
+// that is missing there) ...
+template <typename T, int W, int KB> __device__ __forceinline__ floats from_memory(tile<T, W> &a, const operand<T> (&s)[KB], int it, float weight, int along_a)
+{
+    floats o = (floats)0.0f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) o = product(s[kb], a.along(along_a, it, kb), o);
+    if constexpr (sizeof(T) == 4) settle(o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] *= weight;
+    return o;
+}
+// ... and what the rows of the chunk add.
+template <typename T> __device__ __forceinline__ void from_rows(floats &o, const operand<T> (&c)[2], tile<T, CHUNK> &P, const powers &w, int which, int it, int along_p)
+{
+#pragma unroll
+    for (int kb = 0; kb <= it / 2; ++kb) {
+        if constexpr (NARROW<T>) {
+            const floats more = product(c[kb], P.along(along_p, it, kb), (floats)0.0f);
+            const float up = ldexpf(1.0f, w.exponent[which][it][kb]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = fmaf(more[j], up, o[j]);
+        } else {
+            o = product(c[kb], P.along(along_p, it, kb), o);
+        }
+    }
+    if constexpr (sizeof(T) == 4) settle(o);
+}
+template <typename T> __device__ __forceinline__ bagel_pack<T, 4> rounded(const floats &o, float scale)
+{
+    bagel_pack<T, 4> x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = (T)(o[j] * scale);
+    return x;
+}
+
+// Goes through a segment's rows: `ask(tiles, base, h)` asks for the 64 rows from `base` on of head h, ask_few for those that are there of fewer, and `go(tiles,
+// h, n, base, next)` takes a step: it puts the tiles away and calls `next`, which asks for those of the steps to come: DEEP of them are on their way.  Behind the
+// last ones the same are asked for again, which nobody reads: a branch around the loads would make every wait one for all of them.
+template <int DEEP, bool ONE_HEAD, typename Tiles, typename Ask, typename Few, typename Go>
+__device__ __forceinline__ void go_through(const place &at, int heads, int step, Tiles (&coming)[DEEP], Ask &&ask, Few &&ask_few, Go &&go)
+{
+    static_assert(DEEP == 1 || DEEP == 2, "steps on their way");
+    const int64_t chunks = at.rows / CHUNK;
+    const int rest = (int)(at.rows % CHUNK);
+    int64_t ask_chunk = 0, chunk = 0;
+    int ask_head = 0, h = 0;
+    const auto ask_next = [&](Tiles &to) {
+        ask(to, at.base + step * min(ask_chunk * CHUNK, at.rows - CHUNK), ask_head);
+        if (ONE_HEAD || ++ask_head == heads) {
+            ask_head = 0;
+            ++ask_chunk;
+        }
+    };
+    const auto whole_step = [&](const Tiles &come, Tiles &then) {
+        go(come, h, CHUNK, at.base + step * (chunk * CHUNK), [&] { ask_next(then); });
+        if (ONE_HEAD || ++h == heads) {
+            h = 0;
+            ++chunk;
+        }
+    };
+    if constexpr (DEEP == 1) {
+        if (chunks > 0) ask_next(coming[0]);
+        while (chunk < chunks) whole_step(coming[0], coming[0]);
+    } else {
+        // Two steps to a round, after one on its own where they are odd in number; what is left is then on its way in the first place.
+        if ((chunks * heads) & 1) {
+            Tiles alone;
+            ask_next(alone);
+            ask_next(coming[0]);
+            whole_step(alone, coming[1]);
+        } else if (chunks > 0) {
+            ask_next(coming[0]);
+            ask_next(coming[1]);
+        }
+        while (chunk < chunks) {
+            whole_step(coming[0], coming[0]);
+            whole_step(coming[1], coming[1]);
+        }
+    }
+    if (rest == 0) return;
+    // the rows that are left: further heads, or all of them where there are no others, are not on their way yet
+    for (h = 0; h < heads; ++h) {
+        if (chunks == 0) ask_few(coming[0], h, rest);
+        else if (h > 0) ask(coming[0], at.base + step * (at.rows - CHUNK), h);
+        go(coming[0], h, rest, at.base + step * (chunks * CHUNK), [] {});
+    }
+}
+
 // How many heads there are to a memory: one; several of a and out; several of b and c, whose sums are made in turn.
 enum heads_kind { ONE, MANY_A, MANY_B };
 
-// A wave to 16 columns of a memory, of c and of out, in float32 in its registers.  The rows' products with each other, P, are shared out
-// among the waves by pieces (16 rows of it, 32 rows they are multiplied with), of which six are not zero, and meet in shared memory.
-// SUMS: only the memory behind the segment, from zero where it is not the first of its sequence.
+template <typename T> struct two_passes {
+    bagel_attention_pass<T> p[2];
+};
+
+// What a segment adds to the memory, or, of the first one of a sequence, the memory behind it.  Segments that are the last of theirs are nobody's to add, so there are
+// as many to do as further ones, each of which waits for the one before it.
+template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch_bounds__(4 * WC, 2) void sums_kernel(two_passes<T> both)
+{
+    bagel_attention_pass<T> p = blockIdx.y ? both.p[1] : both.p[0];
+    if constexpr (WHOLE) {
+        p.wb = WB;
+        p.wc = WC;
+    }
+    constexpr int THREADS = 4 * WC;
+    __shared__ tile<T, WB> sb;
+    __shared__ tile<T, WC> sc;
+    __shared__ powers w;
+    const int64_t work = by_dies(blockIdx.x, 0, p.further * p.states), further = work / p.states;
+    const int state = (int)(work - further * p.states);
+    const place behind_it = place_of(p, p.sequences + further);
+    if (!behind_it.there) return;
+    place at = behind_it;
+    at.rows = p.segment;
+    at.base = behind_it.base + (p.back ? p.segment : -p.segment);
+    const bool first = behind_it.before < p.sequences;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = wave * 16 + (threadIdx.x & 15), step = p.back ? -1 : 1;
+    const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f, whole = power(l2, CHUNK);
+    floats S[WB / 16];
+    const int64_t size = (int64_t)p.wb * p.wc;
+    read_memory(S, first && p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr, p.step_b, p.step_c, column, p.wb, p.wc);
+    w.weigh_out(l2, p.back ? 1 : 0, p.scale_b, CHUNK);
+    const lane_parts<T, WB, WC, THREADS> l;
+    if constexpr (!WHOLE) {
+        clear(sb, p.wb);
+        clear(sc, p.wc);
+    }
+    struct tiles {
+        incoming<T, WB, THREADS> b;
+        incoming<T, WC, THREADS> c;
+    } coming[2];
+    const int heads = MANY ? p.ks : 1;
+    go_through<2, !MANY>(at, heads, step, coming,
+        [&](tiles &to, int64_t base, int h) {
+            to.b.load(p.b.at(base, state * heads + h), step * p.b.stride, p.wb);
+            to.c.load(p.c.at(base, state * heads + h), step * p.c.stride, p.wc);
+        },
+        [](tiles &, int, int) {},
+        [&](const tiles &come, int h, int n, int64_t, auto &&next) {
+            __syncthreads();
+            come.b.put(sb, l.pack_b, n, p.wb);
+            come.c.put(sc, l.pack_c, n, p.wc);
+            __syncthreads();
+            next();
+            const operand<T> c[2] = {sc.across(l.across_c, 0, wave), sc.across(l.across_c, 1, wave)};
+            remember(S, sb, c, w, MANY && h > 0 ? 1.0f : whole, l.across_b);
+        });
+    write_memory(S, p.memories + (behind_it.before * p.states + state) * size, p.step_b, p.step_c, column, p.wb, p.wc);
+}
+
+// What segments have added to the memory, into the memory behind each: a thread to an entry, along its sequence's segments but the last.
+template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two_passes<T> both, int blocks)
+{
+    const bagel_attention_pass<T> p = blockIdx.y ? both.p[1] : both.p[0];
+    const int size = p.wb * p.wc;
+    for (int64_t work = blockIdx.x; work < (int64_t)p.sequences * p.states * blocks; work += gridDim.x) {
+        const int state = (int)(work / blocks % p.states), sequence = (int)(work / blocks / p.states);
+        int64_t begin, end;
+        sequence_rows(p, sequence, begin, end);
+        const int64_t first = p.offsets ? begin / p.segment : sequence * further_of_each(p), each = (int64_t)p.states * size;
+        const int64_t n = min((end - begin + p.segment - 1) / p.segment - 2, p.further - first);     // segments to join: neither the first nor the last
+        if (n < 1) continue;
+        const float keep = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
+        for (int i = (int)(work % blocks) * 256 + threadIdx.x; i < size; i += blocks * 256) {
+            float s = p.memories[((int64_t)sequence * p.states + state) * size + i];
+            float *m = p.memories + ((p.sequences + first) * p.states + state) * size + i;
+            constexpr int AHEAD = 16;
+            for (int64_t k = 0; k < n; k += AHEAD) {
+                float add[AHEAD];
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) add[j] = k + j < n ? m[(k + j) * each] : 0.0f;
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j)
+                    if (k + j < n) m[(k + j) * each] = s = fmaf(keep, s, add[j]);
+            }
+        }
+    }
+}
+
+// The memory that a segment begins with.
+template <typename T> __device__ __forceinline__ const float *memory_before(const bagel_attention_pass<T> &p, const place &at, int state)
+{
+    const int64_t size = (int64_t)p.wb * p.wc;
+    if (at.before >= 0) return p.memories + (at.before * p.states + state) * size;
+    return p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr;
+}
+
+// A pass over a segment.  A wave to 16 columns of a memory, of c and of out, in float32 in its registers.  The rows' products with each other, P, are shared out
+// among the waves by pieces (16 rows of it, 32 rows they are multiplied with), and meet in shared memory.
 // WHOLE: a and b are as wide as their tiles, and so are c and out.
-template <typename T, int WB, int WC, bool WHOLE, bool SUMS, heads_kind HEADS, int ON_SIMD>
-__global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention_pass<T> p)
+template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD> __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention_pass<T> p)
 {
     if constexpr (WHOLE) {
         p.wb = WB;
         p.wc = WC;
     }
-    constexpr int NB = WB / 16, KB = WB / 32, WAVES = WC / 16, THREADS = 4 * WC;
-    __shared__ tile<T, WB> sb;
-    __shared__ tile<T, WC> sc;
-    __shared__ tile<T, SUMS ? 16 : WB> sa;
-    __shared__ tile<T, SUMS ? 16 : CHUNK> sp;
+    constexpr int WAVES = WC / 16, THREADS = 4 * WC;
     // Results go through shared memory, and from there while the next step's tiles come, so that rows are written in packs; in 32 bits a lane has a pack
-    constexpr bool THROUGH = !SUMS && sizeof(T) == 2;
+    constexpr bool THROUGH = sizeof(T) == 2;
+    __shared__ tile<T, WB> sa, sb;
+    __shared__ tile<T, WC> sc;
+    __shared__ tile<T, CHUNK> sp;
     __shared__ tile<T, THROUGH ? WC : 16> so;
-    __shared__ int sp_exponent[4][2];
-    __shared__ floats weight_out[CHUNK / 4];         // powers of l from the rows to the memory behind the chunk
-    __shared__ floats weight_p[SUMS ? 1 : 3][2][64]; // and between rows of a piece of P (a lane's eight entries), that begins 0, 16 and 32 rows before
-    const int64_t segments = p.slots * p.states;
-    if ((int64_t)blockIdx.x >= segments) return bagel_clear_behind(p, blockIdx.x - segments, gridDim.x - segments);
-    // Workgroups go to the eight dies in turn.  Each die takes segments that follow each other, so that the heads of the same rows, which lie side by side in
-    // memory, are read by one.
-    const int64_t die = blockIdx.x % 8, work = die * (segments / 8) + min(die, segments % 8) + blockIdx.x / 8;
-    const int64_t slot = work / p.states;
-    const int state = (int)(work - slot * p.states);
-    const place at = place_of(p, slot);
-    if (!at.there || (SUMS && at.last)) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, j16 = lane & 15;
-    const int mine = wave * 16 + j16;                                // the lane's column of the memory
+    __shared__ powers w;
+    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
+    if ((int64_t)blockIdx.x >= all) return bagel_clear_behind(p, blockIdx.x - all, gridDim.x - all);
+    const int64_t work = by_dies(blockIdx.x, first, all), number = work / p.states;
+    const int state = (int)(work - number * p.states);
+    const place at = place_of(p, number);
+    if (!at.there) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = (threadIdx.x & 63) >> 4, j16 = threadIdx.x & 15, column = wave * 16 + j16;
     const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
     const int step = p.back ? -1 : 1, behind = p.back ? 1 : 0;       // of powers of l
-
-    // S[2 kb + half][j]: entry (32 kb + 8 g + 4 half + j, mine) of the memory
-    floats S[NB];
-    const auto row_of = [&](int bt, int j) { return bt / 2 * 32 + 8 * g + bt % 2 * 4 + j; };
-    const int64_t size = (int64_t)p.wb * p.wc, memory = ((int64_t)at.sequence * p.states + state) * size;
-    {
-        const float *from = at.first ? p.first : SUMS ? nullptr : p.memories + ((slot - 1) * p.states + state) * size;
-        const int64_t start = at.first ? memory : 0, step_b = at.first ? p.step_b : p.wc, step_c = at.first ? p.step_c : 1;
-#pragma unroll
-        for (int bt = 0; bt < NB; ++bt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[bt][j] = from && row_of(bt, j) < p.wb && mine < p.wc ? from[start + row_of(bt, j) * step_b + mine * step_c] : 0.0f;
-    }
-    const auto weigh_out = [&](int n) {
-        if ((int)threadIdx.x < CHUNK) reinterpret_cast<float *>(weight_out)[threadIdx.x] = power(l2, max(n - 1 - (int)threadIdx.x, 0) + behind) * p.scale_b;
-    };
-    weigh_out(CHUNK);
-    if constexpr (!SUMS)
-        for (int i = wave; i < 6; i += WAVES) {
-            floats x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = 16 * (i / 2) + j16 - (8 * g + i % 2 * 4 + j);
-                x[j] = d >= 0 ? power(l2, d) * p.scale_b : 0.0f;
-            }
-            weight_p[i / 2][i % 2][lane] = x;
-        }
-    // 48 rows before: l^16 more than 32.  From a row to the memory before the chunk; over a chunk:
+    floats S[WB / 16];
+    read_memory(S, memory_before(p, at, state), p.step_b, p.step_c, column, p.wb, p.wc);
+    w.weigh_out(l2, behind, p.scale_b, CHUNK);
+    w.weigh_p(l2, p.scale_b);
     const float tile_on = power(l2, 16), weight_in = power(l2, j16 + 1 - behind), whole = power(l2, CHUNK);
-
-    // a lane's parts of addresses in shared memory
-    const int along_a = tile<T, WB>::lane_along(), along_p = tile<T, CHUNK>::lane_along(), spread_b = tile<T, WB>::lane_spread();
-    const int across_b = tile<T, WB>::lane_across(true), across_c = tile<T, WC>::lane_across(false), entries_o = tile<T, WC>::lane_entries();
-    const int pack_b = packs_of<T, WB, THREADS>::lane_part(), pack_c = packs_of<T, WC, THREADS>::lane_part();
+    const lane_parts<T, WB, WC, THREADS> l;
     if constexpr (!WHOLE) {
+        clear(sa, p.wb);
         clear(sb, p.wb);
         clear(sc, p.wc);
-        if constexpr (!SUMS) clear(sa, p.wb);
     }
-    const int heads = HEADS == MANY_B ? p.ks : HEADS == MANY_A && !SUMS ? p.qs : 1;
+    const int heads = HEADS == MANY_B ? p.ks : HEADS == MANY_A ? p.qs : 1;
     const auto head_a = [&](int h) { return HEADS == MANY_A ? state * heads + h : state; };
     const auto head_b = [&](int h) { return HEADS == MANY_B ? state * heads + h : state; };
-    // The tiles of a step, on their way: two steps' at a time, as one alone would leave too little of the memory's rate in use
+    // Two steps are on their way, as one alone would leave too little of the memory's rate in use.  (What is asked for in every step comes last: what is waited for
+    // is counted from there, whether there were others or not.)
     struct tiles {
-        incoming<T, SUMS ? 64 : WB, THREADS> a;
-        incoming<T, WB, THREADS> b;
+        incoming<T, WB, THREADS> a, b;
         incoming<T, WC, THREADS> c;
     } coming[2];
-    const auto ask = [&](tiles &to, int64_t base, int h) {
-        // (those of every step come last: what is waited for is counted from there, whether there were others or not)
-        const auto ask_a = [&] {
-            if constexpr (!SUMS) to.a.load(p.a.at(base, head_a(h)), step * p.a.stride, p.wb);
-        };
-        const auto ask_b = [&] {
-            to.b.load(p.b.at(base, head_b(h)), step * p.b.stride, p.wb);
-            to.c.load(p.c.at(base, head_b(h)), step * p.c.stride, p.wc);
-        };
-        if constexpr (HEADS == MANY_B) {
-            if (h == 0) ask_a();
-            ask_b();
-        } else {
-            if (h == 0) ask_b();
-            ask_a();
-        }
+    floats O[HEADS == MANY_B ? 4 : 1];
+    T *ready = nullptr;                              // where the rows in `so` go, and how many there are
+    int ready_rows = 0;
+    const auto flush = [&] {
+        if constexpr (THROUGH)
+            if (ready) write_rows<T, WC, THREADS>(so, l.pack_c, ready, step * p.out.stride, ready_rows, p.wc);
     };
-    const auto ask_few = [&](tiles &to, int h, int n) {
-        if constexpr (!SUMS)
-            if (HEADS != MANY_B || h == 0) to.a.load_few(p.a.at(at.base, head_a(h)), n, step * p.a.stride, p.wb);
-        if (HEADS == MANY_B || h == 0) {
+    go_through<2, HEADS == ONE>(at, heads, step, coming,
+        [&](tiles &to, int64_t base, int h) {
+            const auto ask_a = [&] { to.a.load(p.a.at(base, head_a(h)), step * p.a.stride, p.wb); };
+            const auto ask_b = [&] {
+                to.b.load(p.b.at(base, head_b(h)), step * p.b.stride, p.wb);
+                to.c.load(p.c.at(base, head_b(h)), step * p.c.stride, p.wc);
+            };
+            if constexpr (HEADS == MANY_B) {
+                if (h == 0) ask_a();
+                ask_b();
+            } else {
+                if (h == 0) ask_b();
+                ask_a();
+            }
+        },
+        [&](tiles &to, int h, int n) {
+            to.a.load_few(p.a.at(at.base, head_a(h)), n, step * p.a.stride, p.wb);
             to.b.load_few(p.b.at(at.base, head_b(h)), n, step * p.b.stride, p.wb);
             to.c.load_few(p.c.at(at.base, head_b(h)), n, step * p.c.stride, p.wc);
-        }
-    };
-    floats O[HEADS == MANY_B ? 4 : 1];
-    // One step: head h of the chunk at `base`, of which n rows are there, whose tiles were asked for.  `next` asks for the next one's; `before` takes away what
-    // the step before left in `so`.
-    const auto go = [&](const tiles &come, int h, const int n, T *out, auto &&before, auto &&next) {
-        __syncthreads();
-        before();
-        if constexpr (!SUMS)
-            if (HEADS != MANY_B || h == 0) come.a.put(sa, pack_b, n, p.wb);
-        if (HEADS == MANY_B || h == 0) {
-            come.b.put(sb, pack_b, n, p.wb);
-            come.c.put(sc, pack_c, n, p.wc);
-        }
-        if (n != CHUNK) weigh_out(n);
-        __syncthreads();
-        next();
-
-        operand<T> c[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) c[t] = sc.across(across_c, t, wave);
-        const bool enter = !SUMS && (HEADS != MANY_B || h == 0), leave = !SUMS && (HEADS != MANY_B || h == heads - 1);
-        // the memory before the chunk as operands
-        operand<T> s[KB];
-        int s_exponent = 0;
-        if (enter) {
-            float down = 1.0f;
-            if constexpr (NARROW<T>) {
-                float top = 0.0f;
-#pragma unroll
-                for (int bt = 0; bt < NB; ++bt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(S[bt][j]));
-                s_exponent = exponent_for(wave_largest(top));
-                down = ldexpf(1.0f, -s_exponent);
+        },
+        [&](const tiles &come, int h, const int n, int64_t base, auto &&next) {
+            __syncthreads();
+            flush();
+            if (HEADS != MANY_B || h == 0) come.a.put(sa, l.pack_b, n, p.wb);
+            if (HEADS == MANY_B || h == 0) {
+                come.b.put(sb, l.pack_b, n, p.wb);
+                come.c.put(sc, l.pack_c, n, p.wc);
             }
+            if (n != CHUNK) w.weigh_out(l2, behind, p.scale_b, n);
+            __syncthreads();
+            next();
+            const bool enter = HEADS != MANY_B || h == 0, leave = HEADS != MANY_B || h == heads - 1;
+            const operand<T> c[2] = {sc.across(l.across_c, 0, wave), sc.across(l.across_c, 1, wave)};
+            operand<T> s[WB / 32];
+            const int e = enter ? as_operands<T>(S, s) : 0;
+            make_pieces<WAVES>(sa, sb, sp, w, 0, tile_on, l.along_a, l.spread_b, l, wave);
+            if (HEADS == MANY_B || h == heads - 1) remember(S, sb, c, w, HEADS == MANY_B && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n), l.across_b);
+            __syncthreads();
+            if (!p.out.data) return;
+            T *const out = p.out.at(base, head_a(h));
+            float weight = NARROW<T> ? ldexpf(weight_in, e) : weight_in;
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[kb][i] = (T)(NARROW<T> ? S[2 * kb + i / 4][i % 4] * down : S[2 * kb + i / 4][i % 4]);
-        }
-        if constexpr (!SUMS) {
-            // rows 16 it of P by rows 32 kb of b, transposed: a lane has eight entries of a row
-            const auto make_piece = [&](int it, int kb) {
-                floats P[2] = {(floats)0.0f, (floats)0.0f};
-#pragma unroll
-                for (int q = 0; q < KB; ++q) {
-                    const operand<T> a = sa.along(along_a, it, q);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) P[half] = product(sb.spread(spread_b, kb, half, q), a, P[half]);
-                }
-                const int before = it - 2 * kb;
-                const float far = before == 3 ? tile_on : 1.0f;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const floats w = weight_p[SUMS ? 0 : min(before, 2)][half][lane];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) P[half][j] *= w[j] * far;
-                }
-                float down = 1.0f;
-                if constexpr (NARROW<T>) {
-                    float top = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(P[i / 4][i % 4]));
-                    const int e = exponent_for(wave_largest(top));
-                    down = ldexpf(1.0f, -e);
-                    if (lane == 0) sp_exponent[it][kb] = e;
-                }
-                operand<T> x;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = (T)(NARROW<T> ? P[i / 4][i % 4] * down : P[i / 4][i % 4]);
-                sp.along(along_p, it, kb) = x;
-            };
-            if constexpr (WAVES == 4) {
-                make_piece(wave < 2 ? 3 : 2, wave & 1);
-                if (wave >= 2) make_piece(wave - 2, 0);
-            } else {
-                if (wave < 6) make_piece(wave < 4 ? 3 - wave / 2 : wave - 4, wave < 4 ? wave & 1 : 0);
-            }
-        }
-        // The memory behind the chunk.  c is weighed, and what that makes is held to 24 bits as a sum of operands (22 in float16): the memory is kept in
-        // float32, and one rounding to 8 or 11 bits of every row would be left in it.
-        if (HEADS == MANY_B || h == heads - 1) {
-            const float keep = HEADS == MANY_B && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n);
-            int e = 0;
-            float w[2][8];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const floats lo = weight_out[8 * t + 2 * g], hi = weight_out[8 * t + 2 * g + 1];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[t][i] = (float)c[t][i] * (i < 4 ? lo[i & 3] : hi[i & 3]);
-            }
-            if constexpr (NARROW<T>) {
-                float top = 0.0f;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(w[t][i]));
-                e = exponent_for(wave_largest(top));
-                const float down = ldexpf(1.0f, -e);
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[t][i] *= down;
-            }
-            constexpr int PARTS = sizeof(T) == 4 ? 1 : NARROW<T> ? 2 : 3;
-            operand<T> part[PARTS][2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int q = 0; q < PARTS; ++q) {
-                        part[q][t][i] = (T)w[t][i];
-                        w[t][i] -= (float)part[q][t][i];
-                    }
-#pragma unroll
-            for (int bt = 0; bt < NB; ++bt) {
-                const operand<T> b0 = sb.across_spread(across_b, 0, bt / 2, bt % 2), b1 = sb.across_spread(across_b, 1, bt / 2, bt % 2);
-                floats x = NARROW<T> ? (floats)0.0f : S[bt];
-                if constexpr (!NARROW<T>)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] *= keep;
-#pragma unroll
-                for (int q = PARTS - 1; q >= 0; --q) {
-                    x = product(b0, part[q][0], x);
-                    x = product(b1, part[q][1], x);
-                }
-                if constexpr (NARROW<T>) {
-                    const float up = ldexpf(1.0f, e);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = fmaf(S[bt][j], keep, x[j] * up);
-                }
-                S[bt] = x;
-            }
-            if constexpr (sizeof(T) == 4) settle(S);
-        }
-        if constexpr (SUMS) return;
-        __syncthreads();
-        if (!p.out.data) return;
-        float w = NARROW<T> ? ldexpf(weight_in, s_exponent) : weight_in;
-#pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            floats &o = O[HEADS == MANY_B ? it : 0];
-            if (enter) {
-                o = (floats)0.0f;
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) o = product(s[kb], sa.along(along_a, it, kb), o);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] *= w;
-                w *= tile_on;
-            }
-#pragma unroll
-            for (int kb = 0; kb <= it / 2; ++kb) {
-                if constexpr (NARROW<T>) {
-                    const floats more = product(c[kb], sp.along(along_p, it, kb), (floats)0.0f);
-                    const float up = ldexpf(1.0f, sp_exponent[it][kb]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = fmaf(more[j], up, o[j]);
-                } else {
-                    o = product(c[kb], sp.along(along_p, it, kb), o);
-                }
-            }
-            if (leave) {
-                bagel_pack<T, 4> x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = (T)(o[j] * p.scale);
+            for (int it = 0; it < 4; ++it) {
+                floats &o = O[HEADS == MANY_B ? it : 0];
+                if (enter) o = from_memory(sa, s, it, weight, l.along_a);
+                weight *= tile_on;
+                from_rows(o, c, sp, w, 0, it, l.along_p);
+                if (!leave) continue;
+                const bagel_pack<T, 4> x = rounded<T>(o, p.scale);
                 if constexpr (THROUGH) {
-                    so.entries(entries_o, it, wave) = x;
+                    so.entries(l.entries_o, it, wave) = x;
                 } else {
-                    const int first = 16 * wave + 4 * g;
-                    if (16 * it + j16 >= n || first >= p.wc) continue;
-                    T *to = out + (16 * it + j16) * (step * p.out.stride) + first;
-                    if (first + 4 <= p.wc) reinterpret_cast<bagel_loose_pack<T, 4> *>(to)->x = x;
+                    const int from = 16 * wave + 4 * g;
+                    if (16 * it + j16 >= n || from >= p.wc) continue;
+                    T *to = out + (16 * it + j16) * (step * p.out.stride) + from;
+                    if (from + 4 <= p.wc) reinterpret_cast<bagel_loose_pack<T, 4> *>(to)->x = x;
                     else
 #pragma unroll
                         for (int j = 0; j < 3; ++j)
-                            if (first + j < p.wc) to[j] = x[j];
+                            if (from + j < p.wc) to[j] = x[j];
                 }
             }
-        }
-    };
-    const int64_t chunks = at.rows / CHUNK;
-    const int rest = (int)(at.rows % CHUNK);
-    // The steps of whole chunks are asked for, and those of the rows that are left, as the 64 rows up to the last one; behind these the same again, which nobody
-    // reads: a branch around the loads would make every wait one for all of them.
-    int64_t ask_chunk = 0;
-    int ask_head = 0;
-    const auto ask_next = [&](tiles &to) {
-        ask(to, at.base + step * min(ask_chunk * CHUNK, at.rows - CHUNK), ask_head);
-        if (HEADS == ONE || ++ask_head == heads) {
-            ask_head = 0;
-            ++ask_chunk;
-        }
-    };
-#pragma unroll
-    for (int bt = 0; bt < NB; ++bt) asm volatile("" : "+v"(S[bt]));      // the memory is there before anything else is asked for, so that no wait in the loop is one for it
-    T *ready = nullptr;                              // where the whole rows in `so` go
-    const auto before = [&] {
-        if constexpr (THROUGH)
-            if (ready) write_rows<T, WC, THREADS>(so, pack_c, ready, step * p.out.stride, CHUNK, p.wc);
-    };
-    int64_t chunk = 0;
-    int h = 0;
-    const auto whole_step = [&](const tiles &come, tiles &then) {
-        T *out = !SUMS && p.out.data ? p.out.at(at.base + step * (chunk * CHUNK), head_a(h)) : nullptr;
-        go(come, h, CHUNK, out, before, [&] { ask_next(then); });
-        ready = HEADS == MANY_B && h < heads - 1 ? nullptr : out;
-        if (HEADS == ONE || ++h == heads) {
-            h = 0;
-            ++chunk;
-        }
-    };
-    // Two steps to a round, after one on its own where they are odd in number; what is left is then on its way in the first place.
-    if ((chunks * heads) & 1) {
-        tiles alone;
-        ask_next(alone);
-        ask_next(coming[0]);
-        whole_step(alone, coming[1]);
-    } else if (chunks > 0) {
-        ask_next(coming[0]);
-        ask_next(coming[1]);
-    }
-    while (chunk < chunks) {
-        whole_step(coming[0], coming[0]);
-        whole_step(coming[1], coming[1]);
-    }
-    if (rest > 0) {                                  // the rows that are left: further heads, or all of them where there are no others, are not on their way yet
-        T *out = nullptr;
-        for (h = 0; h < heads; ++h) {
-            if (chunks == 0) ask_few(coming[0], h, rest);
-            else if (h > 0) ask(coming[0], at.base + step * (at.rows - CHUNK), h);
-            if (!SUMS && p.out.data) out = p.out.at(at.base + step * (chunks * CHUNK), head_a(h));
-            go(coming[0], h, rest, out, before, [] {});
-            ready = nullptr;
-            if constexpr (THROUGH) {
-                __syncthreads();
-                if (out && (HEADS != MANY_B || h == heads - 1)) write_rows<T, WC, THREADS>(so, pack_c, out, step * p.out.stride, rest, p.wc);
-            }
-        }
-    } else if constexpr (THROUGH) {
+            ready = leave ? out : nullptr;
+            ready_rows = n;
+        });
+    if constexpr (THROUGH) {
         __syncthreads();
-        before();
+        flush();
     }
-    float *to = SUMS ? p.memories + (slot * p.states + state) * size : at.last && p.last ? p.last + memory : nullptr;
-    if (!to || mine >= p.wc) return;
-    int64_t step_b = SUMS ? p.wc : p.step_b, step_c = SUMS ? 1 : p.step_c;
-    asm volatile("" : "+s"(step_b));                 // its multiples are not kept from the beginning: they would take all scalar registers
-#pragma unroll
-    for (int bt = 0; bt < NB; ++bt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (row_of(bt, j) < p.wb) to[row_of(bt, j) * step_b + mine * step_c] = S[bt][j];
+    if (at.last && p.last) write_memory(S, p.last + ((int64_t)at.sequence * p.states + state) * p.wb * p.wc, p.step_b, p.step_c, column, p.wb, p.wc);
 }
 
-// What segments have added to the memory, into the memory behind each: a thread to an entry, along its sequence's segments but the last.
-template <typename T> __global__ __launch_bounds__(256) void memories_kernel(bagel_attention_pass<T> p, int blocks)
+// The gradients of keys and values: two such passes at once, whose memories are each other's transpose, from the same tiles.
+template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__(4 * W, 2) void keys_kernel(bagel_attention_pass<T> p, bagel_attention_pass<T> q)
 {
-    const int size = p.wb * p.wc;
-    for (int64_t work = blockIdx.x; work < (int64_t)p.sequences * p.states * blocks; work += gridDim.x) {
-        const int state = (int)(work / blocks % p.states), sequence = (int)(work / blocks / p.states);
-        int64_t length = p.each, slot;
-        if (!p.offsets) {
-            slot = (int64_t)sequence * max((length + p.segment - 1) / p.segment, (int64_t)1);
-        } else {
-            const int64_t begin = min(max((int64_t)p.offsets[sequence], (int64_t)0), p.rows);
-            length = min(max((int64_t)p.offsets[sequence + 1], begin), p.rows) - begin;
-            slot = begin / p.segment + sequence;
-        }
-        const int64_t segments = (length + p.segment - 1) / p.segment, each = (int64_t)p.states * size;
-        if (segments < 3) continue;                  // (of two, the first one's is whole)
-        const float keep = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
-        for (int i = (int)(work % blocks) * 256 + threadIdx.x; i < size; i += blocks * 256) {
-            float *m = p.memories + (slot * p.states + state) * size + i;
-            float s = m[0];
-            constexpr int AHEAD = 16;
-            for (int64_t k = 1; k < segments - 1; k += AHEAD) {
-                float add[AHEAD];
-#pragma unroll
-                for (int j = 0; j < AHEAD; ++j) add[j] = k + j < segments - 1 ? m[(k + j) * each] : 0.0f;
-#pragma unroll
-                for (int j = 0; j < AHEAD; ++j)
-                    if (k + j < segments - 1) m[(k + j) * each] = s = fmaf(keep, s, add[j]);
+    if constexpr (WHOLE) p.wb = p.wc = q.wb = q.wc = W;
+    constexpr int WAVES = W / 16, THREADS = 4 * W;
+    __shared__ tile<T, W> sk, sv, sq, sd, so[2];
+    __shared__ tile<T, CHUNK> sp[2];
+    __shared__ powers w;
+    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
+    if ((int64_t)blockIdx.x >= all) {
+        bagel_clear_behind(p, blockIdx.x - all, gridDim.x - all);
+        return bagel_clear_behind(q, blockIdx.x - all, gridDim.x - all);
+    }
+    const int64_t work = by_dies(blockIdx.x, first, all), number = work / p.states;
+    const int state = (int)(work - number * p.states);
+    const place at = place_of(p, number);
+    if (!at.there) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = wave * 16 + (threadIdx.x & 15);
+    const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
+    floats R[W / 16], Rt[W / 16];
+    read_memory(R, memory_before(p, at, state), p.step_b, p.step_c, column, p.wb, p.wc);
+    read_memory(Rt, memory_before(q, at, state), q.step_b, q.step_c, column, q.wb, q.wc);
+    w.weigh_out(l2, 1, p.scale_b, CHUNK);
+    w.weigh_p(l2, p.scale_b);
+    const float tile_on = power(l2, 16), weight_in = power(l2, threadIdx.x & 15), whole = power(l2, CHUNK);
+    const lane_parts<T, W, W, THREADS> l;
+    if constexpr (!WHOLE) {
+        clear(sk, p.wb);
+        clear(sq, p.wb);
+        clear(sv, p.wc);
+        clear(sd, p.wc);
+    }
+    const int heads = MANY ? p.ks : 1;
+    struct tiles {
+        incoming<T, W, THREADS> k, v, q, d;
+    } coming[1];
+    floats O[2][MANY ? 4 : 1];
+    T *ready[2] = {nullptr, nullptr};
+    int ready_rows = 0;
+    const auto flush = [&] {
+        if (ready[0]) write_rows<T, W, THREADS>(so[0], l.pack_b, ready[0], -p.out.stride, ready_rows, p.wc);
+        if (ready[1]) write_rows<T, W, THREADS>(so[1], l.pack_b, ready[1], -q.out.stride, ready_rows, q.wc);
+    };
+    go_through<1, !MANY>(at, heads, -1, coming,
+        [&](tiles &to, int64_t base, int h) {
+            if (!MANY || h == 0) {
+                to.k.load(p.a.at(base, state), -p.a.stride, p.wb);
+                to.v.load(q.a.at(base, state), -q.a.stride, p.wc);
             }
-        }
-    }
+            to.q.load(p.b.at(base, state * heads + h), -p.b.stride, p.wb);
+            to.d.load(p.c.at(base, state * heads + h), -p.c.stride, p.wc);
+        },
+        [&](tiles &to, int h, int n) {
+            to.k.load_few(p.a.at(at.base, state), n, -p.a.stride, p.wb);
+            to.v.load_few(q.a.at(at.base, state), n, -q.a.stride, p.wc);
+            to.q.load_few(p.b.at(at.base, state * heads + h), n, -p.b.stride, p.wb);
+            to.d.load_few(p.c.at(at.base, state * heads + h), n, -p.c.stride, p.wc);
+        },
+        [&](const tiles &come, int h, const int n, int64_t base, auto &&next) {
+            __syncthreads();
+            flush();
+            if (!MANY || h == 0) {
+                come.k.put(sk, l.pack_b, n, p.wb);
+                come.v.put(sv, l.pack_b, n, p.wc);
+            }
+            come.q.put(sq, l.pack_b, n, p.wb);
+            come.d.put(sd, l.pack_b, n, p.wc);
+            if (n != CHUNK) w.weigh_out(l2, 1, p.scale_b, n);
+            __syncthreads();
+            next();
+            const bool enter = !MANY || h == 0, leave = !MANY || h == heads - 1;
+            const float keep = MANY && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n);
+            const operand<T> d[2] = {sd.across(l.across_c, 0, wave), sd.across(l.across_c, 1, wave)}, c[2] = {sq.across(l.across_c, 0, wave), sq.across(l.across_c, 1, wave)};
+            operand<T> s[W / 32], t[W / 32];
+            int e = 0, f = 0;
+            if (enter) {
+                e = as_operands<T>(R, s);
+                f = as_operands<T>(Rt, t);
+            }
+            make_pieces<WAVES>(sk, sq, sp[0], w, 0, tile_on, l.along_a, l.spread_b, l, wave);
+            make_pieces<WAVES>(sv, sd, sp[1], w, 1, tile_on, l.along_a, l.spread_b, l, WAVES - 1 - wave);
+            remember(R, sq, d, w, keep, l.across_b);
+            remember(Rt, sd, c, w, keep, l.across_b);
+            __syncthreads();
+            const auto results = [&](tile<T, W> &a, const operand<T> (&memory)[W / 32], int exponent, const operand<T> (&x)[2], int which) {
+                float weight = NARROW<T> ? ldexpf(weight_in, exponent) : weight_in;
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    floats &o = O[which][MANY ? it : 0];
+                    if (enter) o = from_memory(a, memory, it, weight, l.along_a);
+                    weight *= tile_on;
+                    from_rows(o, x, sp[which], w, which, it, l.along_p);
+                    if (leave) so[which].entries(l.entries_o, it, wave) = rounded<T>(o, 1.0f);
+                }
+            };
+            results(sk, s, e, d, 0);
+            results(sv, t, f, c, 1);
+            ready[0] = leave ? p.out.at(base, state) : nullptr;
+            ready[1] = leave ? q.out.at(base, state) : nullptr;
+            ready_rows = n;
+        });
+    __syncthreads();
+    flush();
+    if (at.last && p.last) write_memory(R, p.last + ((int64_t)at.sequence * p.states + state) * p.wb * p.wc, p.step_b, p.step_c, column, p.wb, p.wc);
 }
 
-template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS> hipError_t launch_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
+// f with constants for the widths of the tiles, and whether the rows fill them.
+template <typename T, typename F> void by_widths(const bagel_attention_pass<T> &p, F &&f)
 {
-    constexpr int THREADS = 4 * WC, ON_SIMD = sizeof(T) == 4 && WB == 128 && WC == 64 ? 1 : 2;
-    constexpr heads_kind SUMS_HEADS = HEADS == MANY_A ? ONE : HEADS;
-    const int64_t work = p.slots * p.states;
-    if (p.memories) {
-        chunks_kernel<T, WB, WC, WHOLE, true, SUMS_HEADS, ON_SIMD><<<(unsigned)work, THREADS, 0, stream>>>(p);
-        // some workgroups to a memory where there are few of them
-        const int64_t all = (int64_t)p.sequences * p.states, most = (p.wb * p.wc + 255) / 256, wanted = 1024 / all;
-        const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
-        memories_kernel<T><<<(unsigned)(all * blocks < 1 << 16 ? all * blocks : 1 << 16), 256, 0, stream>>>(p, blocks);
-    }
-    const int64_t clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
-    if (work + clear > 0) chunks_kernel<T, WB, WC, WHOLE, false, HEADS, ON_SIMD><<<(unsigned)(work + clear), THREADS, 0, stream>>>(p);
-    return hipGetLastError();
+    const std::integral_constant<int, 64> narrow;
+    const std::integral_constant<int, 128> wide;
+    const auto filled = [&](auto wb, auto wc) {
+        if (p.wb == wb && p.wc == wc) f(wb, wc, std::true_type());
+        else f(wb, wc, std::false_type());
+    };
+    if (p.wb <= 64) p.wc <= 64 ? filled(narrow, narrow) : filled(narrow, wide);
+    else p.wc <= 64 ? filled(wide, narrow) : filled(wide, wide);
 }
 
-template <typename T, int WB, int WC, bool WHOLE> hipError_t launch_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
+template <typename T> unsigned groups_of(const bagel_attention_pass<T> &p)
 {
-    if (p.ks > 1) return launch_pass<T, WB, WC, WHOLE, MANY_B>(p, stream);
-    return p.qs > 1 ? launch_pass<T, WB, WC, WHOLE, MANY_A>(p, stream) : launch_pass<T, WB, WC, WHOLE, ONE>(p, stream);
-}
-
-template <typename T, int WB, int WC> hipError_t launch_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
-{
-    return p.wb == WB && p.wc == WC ? launch_pass<T, WB, WC, true>(p, stream) : launch_pass<T, WB, WC, false>(p, stream);
+    return (unsigned)((p.sequences + p.further) * p.states + (p.offsets && p.out.data && p.rows > 0 ? 32 : 0));
 }
 
 }  // namespace
 
+template <typename T> hipError_t bagel_launch_attention_memories(const bagel_attention_pass<T> *passes, int n, hipStream_t stream)
+{
+    two_passes<T> both;
+    both.p[0] = passes[0];
+    both.p[1] = passes[n - 1];
+    const bagel_attention_pass<T> &p = both.p[0];
+    const unsigned work = (unsigned)(p.further * p.states);
+    if (work == 0) return hipSuccess;
+    const bool many = p.ks > 1 || both.p[1].ks > 1;
+    by_widths(p, [&](auto wb, auto wc, auto whole) {
+        constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value;
+        if (many) sums_kernel<T, WB, WC, decltype(whole)::value, true><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
+        else sums_kernel<T, WB, WC, decltype(whole)::value, false><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
+    });
+    // some workgroups to a memory where there are few of them
+    const int64_t all = (int64_t)p.sequences * p.states, most = (p.wb * p.wc + 255) / 256, wanted = 1024 / all;
+    const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+    memories_kernel<T><<<dim3((unsigned)(all * blocks < 1 << 16 ? all * blocks : 1 << 16), n), 256, 0, stream>>>(both, blocks);
+    return hipGetLastError();
+}
+
 template <typename T> hipError_t bagel_launch_attention_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
 {
-    if (p.wb <= 64) return p.wc <= 64 ? launch_pass<T, 64, 64>(p, stream) : launch_pass<T, 64, 128>(p, stream);
-    return p.wc <= 64 ? launch_pass<T, 128, 64>(p, stream) : launch_pass<T, 128, 128>(p, stream);
+    const unsigned groups = groups_of(p);
+    if (groups == 0) return hipSuccess;
+    by_widths(p, [&](auto wb, auto wc, auto whole) {
+        constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value, ON_SIMD = sizeof(T) == 4 && WB == 128 && WC == 64 ? 1 : 2;
+        constexpr bool WHOLE = decltype(whole)::value;
+        if (p.ks > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_B, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+        else if (p.qs > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_A, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+        else chunks_kernel<T, WB, WC, WHOLE, ONE, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+    });
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t bagel_launch_attention_keys(const bagel_attention_pass<T> &p, const bagel_attention_pass<T> &q, hipStream_t stream)
+{
+    const unsigned groups = groups_of(p);
+    if (groups == 0) return hipSuccess;
+    const auto launch = [&](auto w, auto whole) {
+        constexpr int W = decltype(w)::value;
+        constexpr bool WHOLE = decltype(whole)::value;
+        if constexpr (W == 64)
+            if (p.ks > 1) return keys_kernel<T, W, WHOLE, true><<<groups, 4 * W, 0, stream>>>(p, q);
+        keys_kernel<T, W, WHOLE, false><<<groups, 4 * W, 0, stream>>>(p, q);
+    };
+    const std::integral_constant<int, 64> narrow;
+    const std::integral_constant<int, 128> wide;
+    if (p.wb <= 64) p.wb == 64 && p.wc == 64 ? launch(narrow, std::true_type()) : launch(narrow, std::false_type());
+    else p.wb == 128 && p.wc == 128 ? launch(wide, std::true_type()) : launch(wide, std::false_type());
+    return hipGetLastError();
 }
