@@ -63,6 +63,14 @@ template <int MOVE> __device__ __forceinline__ float bagel_moved(float v)
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), MOVE, 0xF, 0xF, false));
 }
 
+// The sum over 8 lanes, the same in all of them.
+__device__ __forceinline__ float bagel_sum_of_8(float v)
+{
+    v += bagel_moved<0xB1>(v);
+    v += bagel_moved<0x4E>(v);
+    return v + bagel_moved<0x141>(v);
+}
+
 // The sum over 16 lanes, the same in all of them.
 __device__ __forceinline__ float bagel_sum_of_16(float v)
 {

@@ -21,6 +21,7 @@ struct clip_args {
     uint32_t first[TENSORS];     // the first piece of each
     uint32_t pieces;             // of all tensors
     int n;
+    bool last;                   // whether no launch follows
     int have;                    // sums that launches before this one have left
     double *sums;                // [GROUPS]
 };
@@ -47,31 +48,32 @@ template <int THREADS> __device__ __forceinline__ double group_sum(double v)
     return v;
 }
 
-template <typename T, int THREADS> __device__ __forceinline__ double squares(const clip_args &a)
+// What threads `lane` of `THREADS` find in pieces number `first`, first + step, ...
+template <typename T, int THREADS> __device__ __forceinline__ double squares(const clip_args &a, uint32_t first, uint32_t step, int lane)
 {
     constexpr int V = 16 / sizeof(T);
     double sum = 0.0;
-    for (uint32_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
+    for (uint32_t piece = first; piece < a.pieces; piece += step) {
         const int k = tensor_of(a, piece);
         const T *g = (const T *)a.tensor[k].grad;
         const int64_t from = (int64_t)(piece - a.first[k]) * PIECE, to = min(from + PIECE, a.tensor[k].count);
-        for (int64_t i = from + V * threadIdx.x; i < to; i += V * THREADS) {
-            if (i + V <= to) {
-                float v[V];
-                bagel_load<T, V>(g + i, v);
+        const int whole = (int)((to - from) / V);
+#pragma unroll 8
+        for (int i = lane; i < whole; i += THREADS) {
+            float v[V];
+            bagel_load<T, V>(g + from + V * i, v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
-            } else {
-                for (int64_t j = i; j < to; ++j) sum = fma((double)(float)g[j], (double)(float)g[j], sum);
-            }
+            for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
         }
+        const int64_t last = from + (int64_t)whole * V + lane;
+        if (last < to) sum = fma((double)(float)g[last], (double)(float)g[last], sum);       // (fewer than a pack are left)
     }
     return sum;
 }
 
 template <typename T> __global__ __launch_bounds__(256) void squares_kernel(clip_args a)
 {
-    const double sum = group_sum<256>(squares<T, 256>(a));
+    const double sum = group_sum<256>(squares<T, 256>(a, blockIdx.x, gridDim.x, threadIdx.x));
     if (threadIdx.x == 0) a.sums[blockIdx.x] = (int)blockIdx.x < a.have ? a.sums[blockIdx.x] + sum : sum;
 }
 
@@ -95,6 +97,14 @@ __global__ __launch_bounds__(256) void factor_kernel(factor_args f)
     double sum = 0.0;
     for (int i = threadIdx.x; i < f.count; i += 256) sum += f.sums[i];
     sum = group_sum<256>(sum);
+    if (threadIdx.x == 0) finish(f, sum);
+}
+
+// Few values in one launch: a piece to a wave of a single workgroup.
+constexpr uint32_t FEW = 32;
+template <typename T> __global__ __launch_bounds__(1024) void few_kernel(clip_args a, factor_args f)
+{
+    const double sum = group_sum<1024>(squares<T, 64>(a, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 16, threadIdx.x & 63));
     if (threadIdx.x == 0) finish(f, sum);
 }
 
@@ -132,6 +142,7 @@ template <typename F> hipError_t in_launches(const bagel_clip_tensor *tensors, i
     a.have = 0;
     a.sums = nullptr;
     hipError_t e = hipSuccess;
+    a.last = false;
     const auto launch = [&] {
         f(a);
         e = hipGetLastError();
@@ -148,6 +159,7 @@ template <typename F> hipError_t in_launches(const bagel_clip_tensor *tensors, i
         a.first[a.n++] = a.pieces;
         a.pieces += pieces;
     }
+    a.last = true;
     if (e == hipSuccess && a.n > 0) launch();
     return e;
 }
@@ -155,7 +167,13 @@ template <typename F> hipError_t in_launches(const bagel_clip_tensor *tensors, i
 template <typename T> hipError_t launch_clip(const bagel_clip_tensor *tensors, int32_t n, const bagel_clip &o, hipStream_t stream)
 {
     factor_args f = {(const double *)o.workspace, 0, o.max_norm, o.eps, o.grad_scale, o.norm, o.factor};
+    bool done = false;
     hipError_t e = in_launches(tensors, n, false, [&](clip_args &a) {
+        if (f.count == 0 && a.last && a.pieces <= FEW) {
+            few_kernel<T><<<1, 1024, 0, stream>>>(a, f);
+            done = true;
+            return;
+        }
         a.sums = (double *)o.workspace;
         const int groups = (int)(a.pieces < GROUPS ? a.pieces : GROUPS);
         a.have = f.count;
@@ -163,7 +181,7 @@ template <typename T> hipError_t launch_clip(const bagel_clip_tensor *tensors, i
         f.count = groups > f.count ? groups : f.count;
     });
     if (e != hipSuccess) return e;
-    factor_kernel<<<1, 256, 0, stream>>>(f);
+    if (!done) factor_kernel<<<1, 256, 0, stream>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return in_launches(tensors, n, true, [&](clip_args &a) {
         scale_kernel<T><<<(unsigned)(a.pieces < GROUPS ? a.pieces : GROUPS), 256, 0, stream>>>(a, o.factor);

@@ -120,12 +120,22 @@ __global__ __launch_bounds__((tile<V, K, WAVES, LANES>::threads)) void norm_grad
 #pragma unroll
         for (int i = 0; i < V; ++i) sw[k][i] = sb[k][i] = 0.0f;
     const bagel_rows<T> from = part_of(a, a.x, at.group), dy = part_of(a, a.d_out, at.group), to = part_of(a, a.d_x, at.group);
-    for (; at.there(a); at.next(a)) {
+    struct row {
         typename tl::template packed<T> x, d;
-        x.load(from, at.row, a.width);
-        d.load(dy, at.row, a.width);
+    } next;
+    const auto ask = [&](int64_t r) {
+        next.x.load(from, r, a.width);
+        next.d.load(dy, r, a.width);
+    };
+    constexpr bool ahead = WAVES < 16;       // sixteen waves leave 128 registers to a lane: no room for two rows
+    if (ahead && at.there(a)) ask(at.row);
+    for (; at.there(a); at.next(a)) {
+        if (!ahead) ask(at.row);
+        row now = next;
+        typename tl::template packed<T> &x = now.x, &d = now.d;
         x.arrived(a.width);
         d.arrived(a.width);
+        if (ahead && at.part + tl::next_row() < a.parts) ask(at.row + a.each);   // on its way while this row waits for its sums
         float s[1] = {0.0f}, t[3] = {0.0f, 0.0f, 0.0f}, c[K][V];
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -264,6 +274,7 @@ template <typename T> pass run_rows(norm_args<T> &a, bool grad, bool launch, hip
     constexpr int V = 16 / sizeof(T);
     const int packs = (a.width + V - 1) / V;
     if (a.width < V) return run_tile<T, 1, 1, 1, 16>(a, grad, launch, stream);
+    if (packs <= 8) return run_tile<T, V, 1, 1, 8>(a, grad, launch, stream);
     if (packs <= 16) return run_tile<T, V, 1, 1, 16>(a, grad, launch, stream);
     if (packs <= 64) return run_tile<T, V, 1, 1>(a, grad, launch, stream);
     if (packs <= 128) return run_tile<T, V, 2, 1>(a, grad, launch, stream);

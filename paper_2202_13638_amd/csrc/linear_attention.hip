@@ -67,32 +67,70 @@ template <typename T> __global__ __launch_bounds__(256) void rows_kernel(bagel_a
     }
 }
 
-template <typename T>
+// One row of each of many sequences.  A workgroup to a memory: V columns to a thread, whose rows follow each other by as many as there are threads for; the
+// memory is read and written once, where no more than HEADS heads share it (more of them read it again, out of the cache).
+template <typename T, int V>
 __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, bagel_heads_of<T> q,
                                                    bagel_heads_of<T> k, bagel_heads_of<T> v, bagel_heads_of<T> out, float *state)
 {
-    __shared__ float sk[BAGEL_ATTENTION_MAX_WIDTH], sv[BAGEL_ATTENTION_MAX_WIDTH], sq[BAGEL_ATTENTION_MAX_WIDTH], part[256];
+    constexpr int HEADS = 4, AHEAD = 4, MOST = BAGEL_ATTENTION_MAX_WIDTH;
+    __shared__ float sk[MOST], sq[HEADS][MOST], part[HEADS][256 * V];
+    const int t = threadIdx.x, columns = wv / V, apart = 256 / columns, c = t % columns * V, first = t / columns;
+    const bool here = first < apart;
     for (int64_t i = blockIdx.x; i < rows * states; i += gridDim.x) {
         const int64_t row = i / states;
-        const int s = (int)(i - row * states), t = threadIdx.x, col = t & 127, half = t >> 7;
+        const int s = (int)(i - row * states);
+        float *S = state + i * wk * wv + c;
         const float decay = expf(log_decay[s]);
-        float *S = state + i * wk * wv;
-        __syncthreads();
-        if (t < wk) sk[t] = (float)k.at(row, s)[t];
-        if (t < wv) sv[t] = (float)v.at(row, s)[t];
-        __syncthreads();
-        if (col < wv)
-            for (int r = half; r < wk; r += 2) S[r * wv + col] = fmaf(sk[r], sv[col], S[r * wv + col] * decay);
-        for (int g = 0; g < each; ++g) {
+        for (int h0 = 0; h0 < each; h0 += HEADS) {
+            float x[V], o[HEADS][V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x[j] = (float)v.at(row, s)[c + j];
+#pragma unroll
+                for (int h = 0; h < HEADS; ++h) o[h][j] = 0.0f;
+            }
+            // the first rows of the memory are on their way while the keys and queries are put where all threads read them
+            float m[AHEAD][V];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a)
+                if (here && first + a * apart < wk) bagel_load<float, V>(S + (first + a * apart) * wv, m[a]);
             __syncthreads();
-            if (t < wk) sq[t] = (float)q.at(row, s * each + g)[t];
+            if (t < wk) sk[t] = (float)k.at(row, s)[t];
+            for (int j = t; j < HEADS * wk; j += 256) {
+                const int h = j / wk;
+                sq[h][j - h * wk] = h0 + h < each ? (float)q.at(row, s * each + h0 + h)[j - h * wk] : 0.0f;
+            }
             __syncthreads();
-            float o = 0.0f;
-            if (col < wv)
-                for (int r = half; r < wk; r += 2) o = fmaf(sq[r], S[r * wv + col], o);
-            part[t] = o;
+            for (int r0 = first; here && r0 < wk; r0 += AHEAD * apart) {
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) {
+                    const int r = r0 + a * apart;
+                    if (r >= wk) continue;
+                    if (r0 != first) bagel_load<float, V>(S + r * wv, m[a]);
+                    if (h0 == 0) {
+#pragma unroll
+                        for (int j = 0; j < V; ++j) m[a][j] = fmaf(sk[r], x[j], m[a][j] * decay);
+                        bagel_store<float, V>(S + r * wv, m[a]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) o[h][j] = fmaf(sq[h][r], m[a][j], o[h][j]);
+                }
+            }
+            if (here)
+#pragma unroll
+                for (int h = 0; h < HEADS; ++h)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) part[h][first * wv + c + j] = o[h][j];
             __syncthreads();
-            if (half == 0 && col < wv) out.at(row, s * each + g)[col] = (T)((part[col] + part[col + 128]) * scale);
+            for (int j = t; j < min(HEADS, each - h0) * wv; j += 256) {
+                const int h = j / wv;
+                float sum = 0.0f;
+                for (int a = 0; a < apart; ++a) sum += part[h][a * wv + j - h * wv];
+                out.at(row, s * each + h0 + h)[j - h * wv] = (T)(sum * scale);
+            }
         }
     }
 }
@@ -101,11 +139,13 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
 // written and read.  Where there are sequences enough, they are left whole, and only one that is far longer than the others is shared out.
 int64_t segment_rows(const bagel_attention &b)
 {
-    constexpr int64_t LEAST = 512, chunk = BAGEL_ATTENTION_CHUNK;
+    constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
+    // what a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits
+    const int64_t step = (b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 2 : 1), least = chunk * (step < 4 ? 8 / step : 2);
     const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 240 : 480;       // one or two workgroups to a compute unit
     int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
     if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
-    return rows < LEAST ? LEAST : (rows + chunk - 1) / chunk * chunk;
+    return rows < least ? least : (rows + chunk - 1) / chunk * chunk;
 }
 
 // A segment's rows, and how many numbers there are for segments that are not the first of their sequence.
@@ -239,9 +279,13 @@ template <typename T> hipError_t launch_attention_grad(const bagel_attention &b,
 template <typename T> hipError_t launch_step(const bagel_attention &b, hipStream_t stream)
 {
     const int64_t groups = b.rows * b.states;
-    step_kernel<T><<<(unsigned)(groups < 1 << 20 ? groups : 1 << 20), 256, 0, stream>>>(
-        b.rows, b.states, b.heads / b.states, b.key_width, b.value_width, b.scale, b.log_decay, bagel_heads_from<T>(b.query), bagel_heads_from<T>(b.key),
-        bagel_heads_from<T>(b.value), bagel_heads_from<T>(b.out), b.state);
+    const auto launch = [&](auto kernel) {
+        kernel<<<(unsigned)(groups < 1 << 20 ? groups : 1 << 20), 256, 0, stream>>>(b.rows, b.states, b.heads / b.states, b.key_width, b.value_width, b.scale, b.log_decay,
+                                                                                   bagel_heads_from<T>(b.query), bagel_heads_from<T>(b.key),
+                                                                                   bagel_heads_from<T>(b.value), bagel_heads_from<T>(b.out), b.state);
+    };
+    if (b.value_width % 4 == 0) launch(step_kernel<T, 4>);
+    else launch(step_kernel<T, 1>);
     return hipGetLastError();
 }
 

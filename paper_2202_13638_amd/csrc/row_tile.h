@@ -11,7 +11,7 @@ namespace {
 template <int WAVES, int N, int LANES = 64> __device__ __forceinline__ void row_sum(float (&v)[N], float (*shared)[WAVES][4], int &turn)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = LANES == 16 ? bagel_sum_of_16(v[i]) : bagel_wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = LANES == 8 ? bagel_sum_of_8(v[i]) : LANES == 16 ? bagel_sum_of_16(v[i]) : bagel_wave_sum(v[i]);
     if constexpr (WAVES > 1) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0)
@@ -28,11 +28,11 @@ template <int WAVES, int N, int LANES = 64> __device__ __forceinline__ void row_
     }
 }
 
-// A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i, or (LANES = 16) by a quarter of a wave.  One
+// A row is held in registers by WAVES waves, K packs of V entries a lane: entry V (64 WAVES k + lane) + i, or (LANES = 16, 8) by a quarter or an eighth of a wave.  One
 // wave or less to a row leaves several rows to a workgroup, which need nothing of each other.  Packs need not be aligned.  One that would reach over the end
 // of the row is moved back to end there: its first entries are another pack's, and count as zero here.
 template <int V, int K, int WAVES, int LANES = 64> struct tile {
-    static_assert(LANES == 64 || (LANES == 16 && WAVES == 1), "a row has whole waves, or 16 lanes of one");
+    static_assert(LANES == 64 || ((LANES == 16 || LANES == 8) && WAVES == 1), "a row has whole waves, or 16 lanes or 8 of one");
     static constexpr int threads = WAVES == 1 ? 256 : 64 * WAVES, lanes = LANES * WAVES, rows = WAVES == 1 ? 256 / LANES : 1;
     __device__ static __forceinline__ int place(int k) { return V * (lanes * k + (int)threadIdx.x % lanes); }
     __device__ static __forceinline__ bool here(int k, int width) { return place(k) < width; }
