@@ -13,9 +13,9 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbagel.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
-SOURCES = ["adamw.hip", "backward.hip", "bagel_api.hip", "block_join.hip", "clip.hip", "gp_step.hip", "lane.hip", "layer_norm.hip", "linear_attention.hip", "model.hip", "policy.hip", "policy16.hip", "posterior.hip", "prepare.hip", "recurrence.hip", "rollout.hip"]
-# those with matrix instructions of 16-bit operands, whose results are waited for by other rules (tests/test_more_matrix_wait_states.py)
-MATRIX_16_SOURCES = ["linear_attention_bf16.hip", "linear_attention_f16.hip", "linear_attention_f32.hip"]
+SOURCES = ["adamw.hip", "backward.hip", "bagel_api.hip", "block_join.hip", "clip.hip", "gp_step.hip", "lane.hip", "layer_norm.hip", "model.hip", "policy.hip", "policy16.hip", "posterior.hip", "prepare.hip", "recurrence.hip", "rollout.hip"]
+# linear attention: what has matrix instructions of 16-bit operands, whose results are waited for by other rules (tests/test_more_matrix_wait_states.py)
+MATRIX_16_SOURCES = ["linear_attention.hip", "linear_attention_bf16.hip", "linear_attention_f16.hip", "linear_attention_f32.hip"]
 # -packed-fp32-ops is switched off on purpose: no packed float32 VALU instructions in this library
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
