@@ -126,11 +126,11 @@ class _Attention(C.Structure):
 
 
 class _ClipTensor(C.Structure):
-    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64)]
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_int64), ("dtype", C.c_int32)]
 
 
 class _Clip(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("max_norm", C.c_float), ("eps", C.c_float), ("grad_scale", C.c_void_p), ("norm", C.c_void_p),
+    _fields_ = [("max_norm", C.c_float), ("eps", C.c_float), ("grad_scale", C.c_void_p), ("norm", C.c_void_p),
                 ("factor", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
 
 
@@ -482,9 +482,9 @@ def bagel_adamw_step(params, grads, m, v, step, *, m_scale=None, v_scale=None, c
 
 
 NORM_MAX_WIDTH, ATTENTION_MAX_WIDTH = 16384, 128
-_NORM_HEAD, _ATTENTION_HEAD, _CLIP_OPTIONS = (struct.Struct(f) for f in ("qiiif", "qiiiiiifPP", "iffPPP"))
+_NORM_HEAD, _ATTENTION_HEAD, _CLIP_OPTIONS = (struct.Struct(f) for f in ("qiiif", "qiiiiiifPP", "ffPPP"))
 assert (_NORM_HEAD.size, _ATTENTION_HEAD.size, _CLIP_OPTIONS.size) == (_Norm.x.offset, _Attention.query.offset, _Clip.workspace.offset)
-_NORM_FIELDS, _CLIP_FIELDS = ("rows", "width", "dtype", "groups", "eps"), ("grads", "max_norm", "eps", "grad_scale", "norm", "factor")
+_NORM_FIELDS, _CLIP_FIELDS = ("rows", "width", "dtype", "groups", "eps"), ("max_norm", "eps", "grad_scale", "norm", "factor")
 _ATTENTION_FIELDS = ("rows", "key's width", "value's width", "heads", "heads of key", "dtype", "offsets", "scale", "offsets", "log_decay")
 
 
@@ -589,11 +589,11 @@ def bagel_clip_norm(grads, max_norm, norm, factor, *, grad_scale=None, out=None,
     """norm = |grad_scale| sqrt(sum of squares of all gradients), factor = grad_scale min(1, max_norm / (norm + eps)), out = gradients * factor
     (see include/bagel.h).
 
-    grads: a list of contiguous tensors of one type; norm, factor and grad_scale (None: one): float32 tensors of one value.  out: None, or a list with
+    grads: a list of contiguous tensors, of any of the three types each; norm, factor and grad_scale (None: one): float32 tensors of one value.  out: None, or a list with
     a tensor or None for every gradient, which may be the gradient itself.  `factor` is a grad_scale for bagel_adamw_step."""
     lib = _load()
     on, device = _stream(stream)
-    n, table, code = _marshal.clip(device, grads, out)
+    n, table = _marshal.clip(device, grads, out)
     places = []
     for name, t in (("grad_scale", grad_scale), ("norm", norm), ("factor", factor)):
         if t is None and name == "grad_scale":
@@ -604,9 +604,9 @@ def bagel_clip_norm(grads, max_norm, norm, factor, *, grad_scale=None, out=None,
         places.append(t.data_ptr())
     workspace, space = _workspace(workspace, lib.bagel_clip_norm_workspace(n), device, stream)
     try:
-        options = _CLIP_OPTIONS.pack(code, max_norm, eps, *places)
+        options = _CLIP_OPTIONS.pack(max_norm, eps, *places)
     except _UNFIT:
-        raise _unfit(_CLIP_OPTIONS, _CLIP_FIELDS, code, max_norm, eps, *places) from None
+        raise _unfit(_CLIP_OPTIONS, _CLIP_FIELDS, max_norm, eps, *places) from None
     _done(lib, lib.bagel_clip_norm(table, n, options + space, on))
 
 

@@ -2,11 +2,15 @@
 //
 // Every gradient is read once for the norm, and, where the clipped ones are wanted, once more to be written: the factor is not known before the last
 // of them.  Memory bounds both.  Squares and their sums are in float64, where neither the largest gradients overflow nor the smallest vanish.
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "activations.h"
 
 namespace {
 
-constexpr int TENSORS = 96;                  // 28 bytes each, within the 4 KB of a kernel's arguments
+constexpr int TENSORS = 96;                  // 36 bytes each, within the 4 KB of a kernel's arguments
 constexpr int PIECE = 8192;                  // entries that a workgroup takes at a time
 constexpr int GROUPS = 2048;                 // workgroups of a launch, at most
 
@@ -14,6 +18,7 @@ struct clip_tensor {
     const void *grad;
     void *out;
     int64_t count;
+    int dtype;
 };
 
 struct clip_args {
@@ -48,32 +53,43 @@ template <int THREADS> __device__ __forceinline__ double group_sum(double v)
     return v;
 }
 
-// What threads `lane` of `THREADS` find in pieces number `first`, first + step, ...
-template <typename T, int THREADS> __device__ __forceinline__ double squares(const clip_args &a, uint32_t first, uint32_t step, int lane)
+// f<type>() for a tensor's type, the same for all threads.
+template <typename F> __device__ __forceinline__ void by_type(int dtype, F &&f)
 {
-    constexpr int V = 16 / sizeof(T);
+    if (dtype == BAGEL_FLOAT32) f(bagel_type<float>());
+    else if (dtype == BAGEL_BFLOAT16) f(bagel_type<__bf16>());
+    else f(bagel_type<_Float16>());
+}
+
+// What threads `lane` of `THREADS` find in pieces number `first`, first + step, ...
+template <int THREADS> __device__ __forceinline__ double squares(const clip_args &a, uint32_t first, uint32_t step, int lane)
+{
     double sum = 0.0;
     for (uint32_t piece = first; piece < a.pieces; piece += step) {
         const int k = tensor_of(a, piece);
-        const T *g = (const T *)a.tensor[k].grad;
         const int64_t from = (int64_t)(piece - a.first[k]) * PIECE, to = min(from + PIECE, a.tensor[k].count);
-        const int whole = (int)((to - from) / V);
+        by_type(a.tensor[k].dtype, [&](auto t) {
+            using T = typename decltype(t)::type;
+            constexpr int V = 16 / sizeof(T);
+            const T *g = (const T *)a.tensor[k].grad;
+            const int whole = (int)((to - from) / V);
 #pragma unroll 8
-        for (int i = lane; i < whole; i += THREADS) {
-            float v[V];
-            bagel_load<T, V>(g + from + V * i, v);
+            for (int i = lane; i < whole; i += THREADS) {
+                float v[V];
+                bagel_load<T, V>(g + from + V * i, v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
-        }
-        const int64_t last = from + (int64_t)whole * V + lane;
-        if (last < to) sum = fma((double)(float)g[last], (double)(float)g[last], sum);       // (fewer than a pack are left)
+                for (int j = 0; j < V; ++j) sum = fma((double)v[j], (double)v[j], sum);
+            }
+            const int64_t last = from + (int64_t)whole * V + lane;
+            if (last < to) sum = fma((double)(float)g[last], (double)(float)g[last], sum);   // (fewer than a pack are left)
+        });
     }
     return sum;
 }
 
-template <typename T> __global__ __launch_bounds__(256) void squares_kernel(clip_args a)
+__global__ __launch_bounds__(256) void squares_kernel(clip_args a)
 {
-    const double sum = group_sum<256>(squares<T, 256>(a, blockIdx.x, gridDim.x, threadIdx.x));
+    const double sum = group_sum<256>(squares<256>(a, blockIdx.x, gridDim.x, threadIdx.x));
     if (threadIdx.x == 0) a.sums[blockIdx.x] = (int)blockIdx.x < a.have ? a.sums[blockIdx.x] + sum : sum;
 }
 
@@ -102,34 +118,36 @@ __global__ __launch_bounds__(256) void factor_kernel(factor_args f)
 
 // Few values in one launch: a piece to a wave of a single workgroup.
 constexpr uint32_t FEW = 32;
-template <typename T> __global__ __launch_bounds__(1024) void few_kernel(clip_args a, factor_args f)
+__global__ __launch_bounds__(1024) void few_kernel(clip_args a, factor_args f)
 {
-    const double sum = group_sum<1024>(squares<T, 64>(a, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 16, threadIdx.x & 63));
+    const double sum = group_sum<1024>(squares<64>(a, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 16, threadIdx.x & 63));
     if (threadIdx.x == 0) finish(f, sum);
 }
 
-template <typename T> __global__ __launch_bounds__(256) void scale_kernel(clip_args a, const float *factor)
+__global__ __launch_bounds__(256) void scale_kernel(clip_args a, const float *factor)
 {
-    constexpr int V = 16 / sizeof(T);
     const float f = factor[0];
     if (!isfinite(f)) return;
     for (uint32_t piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
         const int k = tensor_of(a, piece);
-        const T *g = (const T *)a.tensor[k].grad;
-        T *out = (T *)a.tensor[k].out;
-        if (!out) continue;
         const int64_t from = (int64_t)(piece - a.first[k]) * PIECE, to = min(from + PIECE, a.tensor[k].count);
-        for (int64_t i = from + V * threadIdx.x; i < to; i += V * 256) {
-            if (i + V <= to) {
-                float v[V];
-                bagel_load<T, V>(g + i, v);
+        by_type(a.tensor[k].dtype, [&](auto t) {
+            using T = typename decltype(t)::type;
+            constexpr int V = 16 / sizeof(T);
+            const T *g = (const T *)a.tensor[k].grad;
+            T *out = (T *)a.tensor[k].out;
+            for (int64_t i = from + V * threadIdx.x; i < to; i += V * 256) {
+                if (i + V <= to) {
+                    float v[V];
+                    bagel_load<T, V>(g + i, v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] *= f;
-                bagel_store<T, V>(out + i, v);
-            } else {
-                for (int64_t j = i; j < to; ++j) out[j] = (T)((float)g[j] * f);
+                    for (int j = 0; j < V; ++j) v[j] *= f;
+                    bagel_store<T, V>(out + i, v);
+                } else {
+                    for (int64_t j = i; j < to; ++j) out[j] = (T)((float)g[j] * f);
+                }
             }
-        }
+        });
     }
 }
 
@@ -155,7 +173,7 @@ template <typename F> hipError_t in_launches(const bagel_clip_tensor *tensors, i
         const uint32_t pieces = (uint32_t)((t.count + PIECE - 1) / PIECE);
         if (a.n == TENSORS || (a.n > 0 && a.pieces + pieces > 1u << 30)) launch();
         if (e != hipSuccess) break;
-        a.tensor[a.n] = {t.grad, t.out, t.count};
+        a.tensor[a.n] = {t.grad, t.out, t.count, t.dtype};
         a.first[a.n++] = a.pieces;
         a.pieces += pieces;
     }
@@ -164,35 +182,66 @@ template <typename F> hipError_t in_launches(const bagel_clip_tensor *tensors, i
     return e;
 }
 
-template <typename T> hipError_t launch_clip(const bagel_clip_tensor *tensors, int32_t n, const bagel_clip &o, hipStream_t stream)
+hipError_t launch_clip(const bagel_clip_tensor *tensors, int32_t n, const bagel_clip &o, hipStream_t stream)
 {
     factor_args f = {(const double *)o.workspace, 0, o.max_norm, o.eps, o.grad_scale, o.norm, o.factor};
     bool done = false;
     hipError_t e = in_launches(tensors, n, false, [&](clip_args &a) {
         if (f.count == 0 && a.last && a.pieces <= FEW) {
-            few_kernel<T><<<1, 1024, 0, stream>>>(a, f);
+            few_kernel<<<1, 1024, 0, stream>>>(a, f);
             done = true;
             return;
         }
         a.sums = (double *)o.workspace;
         const int groups = (int)(a.pieces < GROUPS ? a.pieces : GROUPS);
         a.have = f.count;
-        squares_kernel<T><<<groups, 256, 0, stream>>>(a);
+        squares_kernel<<<groups, 256, 0, stream>>>(a);
         f.count = groups > f.count ? groups : f.count;
     });
     if (e != hipSuccess) return e;
     if (!done) factor_kernel<<<1, 256, 0, stream>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     return in_launches(tensors, n, true, [&](clip_args &a) {
-        scale_kernel<T><<<(unsigned)(a.pieces < GROUPS ? a.pieces : GROUPS), 256, 0, stream>>>(a, o.factor);
+        scale_kernel<<<(unsigned)(a.pieces < GROUPS ? a.pieces : GROUPS), 256, 0, stream>>>(a, o.factor);
     });
+}
+
+// What the pass that writes reads and writes.
+struct span {
+    uintptr_t begin, end;
+    bool written;
+};
+const char *check_written(const bagel_clip_tensor *tensors, int32_t n)
+{
+    int written = 0;
+    for (int i = 0; i < n; ++i) written += tensors[i].out && tensors[i].count > 0;
+    if (written == 0) return nullptr;
+    span few[128];
+    const std::unique_ptr<span[]> many(written > 64 ? new (std::nothrow) span[2 * (size_t)written] : nullptr);
+    if (written > 64 && !many) return "no memory to compare the tensors' places";
+    span *const spans = many ? many.get() : few;
+    int m = 0;
+    for (int i = 0; i < n; ++i) {
+        const bagel_clip_tensor &t = tensors[i];
+        if (!t.out || t.count == 0) continue;
+        const uintptr_t bytes = (uintptr_t)t.count * bagel_type_bytes(t.dtype), grad = (uintptr_t)t.grad, out = (uintptr_t)t.out;
+        spans[m++] = {out, out + bytes, true};
+        if (out != grad) spans[m++] = {grad, grad + bytes, false};
+    }
+    std::sort(spans, spans + m, [](const span &x, const span &y) { return x.begin < y.begin; });
+    uintptr_t all = 0, outs = 0;                     // where those before end
+    for (int i = 0; i < m; ++i) {
+        if (spans[i].begin < (spans[i].written ? all : outs)) return "a result overlaps another tensor";
+        all = std::max(all, spans[i].end);
+        if (spans[i].written) outs = std::max(outs, spans[i].end);
+    }
+    return nullptr;
 }
 
 const char *check_clip(const bagel_clip_tensor *tensors, int32_t n, const bagel_clip *o)
 {
     if (n < 0) return "n_tensors must be >= 0";
     if (!o || (n > 0 && !tensors)) return "null argument";
-    if (!bagel_type_ok(o->dtype)) return "unknown dtype";
     if (!(o->max_norm >= 0.0f)) return "max_norm must be >= 0";
     if (!(o->eps > 0.0f) || !isfinite(o->eps)) return "eps must be positive";
     if (!o->norm || !o->factor) return "norm and factor are needed";
@@ -201,8 +250,10 @@ const char *check_clip(const bagel_clip_tensor *tensors, int32_t n, const bagel_
         if (t.count < 0 || t.count >= 1ll << 38) return "count must be >= 0 and below 2^38";
         if (t.count == 0) continue;
         if (!t.grad) return "a tensor has a null argument";
-        if (((uintptr_t)t.grad | (uintptr_t)t.out) & (bagel_type_bytes(o->dtype) - 1)) return "a tensor does not start at a multiple of its type";
+        if (!bagel_type_ok(t.dtype)) return "unknown dtype";
+        if (((uintptr_t)t.grad | (uintptr_t)t.out) & (bagel_type_bytes(t.dtype) - 1)) return "a tensor does not start at a multiple of its type";
     }
+    if (const char *msg = check_written(tensors, n)) return msg;
     if (!o->workspace) return "a workspace is needed";
     if (o->workspace_bytes < bagel_clip_norm_workspace(n)) return "the workspace is too small";
     if ((uintptr_t)o->workspace & 15) return "the workspace must start at a multiple of 16 bytes";
@@ -216,7 +267,7 @@ extern "C" int64_t bagel_clip_norm_workspace(int32_t n_tensors) { return n_tenso
 extern "C" int bagel_clip_norm(const bagel_clip_tensor *tensors, int32_t n_tensors, const bagel_clip *o, void *hip_stream)
 {
     if (const char *msg = check_clip(tensors, n_tensors, o)) return bagel_refuse(BAGEL_EINVAL, "bagel_clip_norm: %s", msg);
-    const hipError_t e = bagel_by_type(o->dtype, [&](auto t) { return launch_clip<typename decltype(t)::type>(tensors, n_tensors, *o, (hipStream_t)hip_stream); });
+    const hipError_t e = launch_clip(tensors, n_tensors, *o, (hipStream_t)hip_stream);
     if (e != hipSuccess) return bagel_refuse(BAGEL_EHIP, "bagel_clip_norm: %s", hipGetErrorString(e));
     return BAGEL_OK;
 }

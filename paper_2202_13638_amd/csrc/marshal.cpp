@@ -295,7 +295,7 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n_args)
     });
 }
 
-// clip(device, grads, out) -> (n, bagel_clip_tensor for each, type code)
+// clip(device, grads, out) -> (n, bagel_clip_tensor for each)
 PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
 {
     return guarded([&]() -> PyObject * {
@@ -309,15 +309,14 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
         list g, out;
         g.beside(args[1], n, "grads");
         out.beside(args[2], n, "out");
-        at::ScalarType type = at::kFloat;
-        if (n > 0) type = tensor_of(g[0], "grads").scalar_type();
-        if (type_code(type) < 0) throw refused{"grads must be float32, bfloat16 or float16 tensors"};
         PyObject *table = PyBytes_FromStringAndSize(nullptr, n * (Py_ssize_t)sizeof(bagel_clip_tensor));
         if (!table) return nullptr;
         try {
             bagel_clip_tensor *to = (bagel_clip_tensor *)PyBytes_AS_STRING(table);
             for (Py_ssize_t i = 0; i < n; ++i) {
                 const at::Tensor &grad = tensor_of(g[i], "grads");
+                const at::ScalarType type = grad.scalar_type();
+                if (type_code(type) < 0) throw refused{"grads must be float32, bfloat16 or float16 tensors"};
                 const auto held = [&](PyObject *o, const char *name) {
                     const at::Tensor &t = tensor_of(o, name);
                     if (t.scalar_type() != type || t.sizes() != grad.sizes() || !t.is_contiguous() || !on(t, device))
@@ -330,13 +329,14 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t n_args)
                 x.grad = held(g[i], "grads");
                 x.out = out.items && out[i] != Py_None ? held(out[i], "out") : nullptr;
                 x.count = grad.numel();
+                x.dtype = type_code(type);
                 to[i] = x;
             }
         } catch (...) {
             Py_DECREF(table);
             throw;
         }
-        return Py_BuildValue("nNi", n, table, type_code(type));
+        return Py_BuildValue("nN", n, table);
     });
 }
 

@@ -486,7 +486,9 @@ def test_more_gradients_against_differences():
 
 # ---------------------------------------------------------------------------------------------------------------- clipping
 def _clip_case(shapes, t, max_norm, grad_scale=0.37, scale=1e-2, write="all", shift=0):
-    g = [_normal(s, 20 + i, t, scale) for i, s in enumerate(shapes)]
+    """t: the tensors' type, or types that they have in turn."""
+    types = t if isinstance(t, list) else [t]
+    g = [_normal(s, 20 + i, types[i % len(types)], scale) for i, s in enumerate(shapes)]
 
     def placed(x):
         return torch.cat([x.new_zeros(shift), x.flatten()]).cuda()[shift:].view(x.shape)
@@ -518,6 +520,15 @@ CLIP_SHAPES = [(256, 5), (256,), (256, 256), (1,), (777, 333), (2,), (8193,), (0
 def test_clip_norm(write, max_norm, dtype):
     _clip_case(CLIP_SHAPES, TYPES[dtype], max_norm, write=write)
     _clip_case([(3,)], TYPES[dtype], max_norm, grad_scale=None, write=write)
+
+
+@gpu
+@pytest.mark.parametrize("write", ["none", "all"])
+def test_clip_norm_of_several_types(write):
+    types = [torch.bfloat16, torch.float32, torch.float16]
+    _clip_case(CLIP_SHAPES, types, 0.5, write=write)
+    _clip_case([(40,), (7,), (9,), (300,)], types, 0.5, write=write)
+    _clip_case([(20000,)] * 150, types, 0.5, write=write)
 
 
 @gpu
@@ -738,14 +749,14 @@ def test_null_arguments_and_sizes_of_work_spaces():
 
 
 @pytest.mark.parametrize("change,tensor,text", [
-    (dict(dtype=7), {}, "dtype"), (dict(max_norm=-1.0), {}, "max_norm"), (dict(max_norm=NAN), {}, "max_norm"), (dict(eps=0.0), {}, "eps"),
+    ({}, dict(dtype=7), "dtype"), (dict(max_norm=-1.0), {}, "max_norm"), (dict(max_norm=NAN), {}, "max_norm"), (dict(eps=0.0), {}, "eps"),
     (dict(norm=None), {}, "norm"), (dict(factor=None), {}, "factor"), (dict(workspace=None), {}, "workspace"), (dict(workspace_bytes=8), {}, "too small"),
     (dict(workspace=0x10004), {}, "16 bytes"), ({}, dict(count=-1), "count"), ({}, dict(grad=None), "null"), ({}, dict(grad=0x10001), "multiple"),
     ({}, dict(out=0x10001), "multiple")])
 def test_clip_norm_refuses(change, tensor, text):
     o, t = binding._Clip(), (binding._ClipTensor * 1)()
-    o.dtype, o.max_norm, o.eps, o.norm, o.factor, o.workspace, o.workspace_bytes = 1, 1.0, 1e-6, 0x10000, 0x10004, 0x10000, 1 << 20
-    t[0].grad, t[0].count = 0x10000, 5
+    o.max_norm, o.eps, o.norm, o.factor, o.workspace, o.workspace_bytes = 1.0, 1e-6, 0x10000, 0x10004, 0x10000, 1 << 20
+    t[0].grad, t[0].count, t[0].dtype = 0x10000, 5, 1
     for k, v in change.items():
         setattr(o, k, v)
     for k, v in tensor.items():
@@ -832,7 +843,7 @@ def test_binding_refuses_more_on_the_gpu():
         binding.bagel_linear_attention(wide, wide, wide, torch.empty_like(wide), 1, ld)
     one = torch.zeros(1, device="cuda")
     with pytest.raises(ValueError, match="tensor 1"):
-        binding.bagel_clip_norm([x, x.half()], 1.0, one, torch.zeros_like(one))
+        binding.bagel_clip_norm([x, x.half()], 1.0, one, torch.zeros_like(one), out=[x, x])
     with pytest.raises(ValueError, match="factor"):
         binding.bagel_clip_norm([x], 1.0, one, ld)
     with pytest.raises(ValueError, match="max_norm"):
