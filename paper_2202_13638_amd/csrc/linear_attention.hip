@@ -137,15 +137,18 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
 
 // Rows of a segment: as many segments as the card takes at a time, some less, as one more would be a round of its own; but no shorter than is worth a memory that is
 // written and read.  Where there are sequences enough, they are left whole, and only one that is far longer than the others is shared out.
+//   An odd number of chunks: workgroups go through their rows side by side, and with a power of two between them they ask the same channels of the memory
+// (131072 rows, 8 heads of 128 on 2 memories, bf16: 259 us with 16 chunks and 256 workgroups, 162 with 18 chunks and 228).
 int64_t segment_rows(const bagel_attention &b)
 {
     constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
     // what a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits
-    const int64_t step = (b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 2 : 1), least = chunk * (step < 4 ? 8 / step : 2);
-    const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 240 : 480;       // one or two workgroups to a compute unit
+    const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 2 : 1), least = step < 4 ? 8 / step : 2;
+    const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 248 : 496;       // one or two workgroups to a compute unit
     int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
     if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
-    return rows < least ? least : (rows + chunk - 1) / chunk * chunk;
+    const int64_t chunks = (rows + chunk - 1) / chunk;
+    return chunk * (chunks <= least ? least : chunks | 1);
 }
 
 // A segment's rows, and how many numbers there are for segments that are not the first of their sequence.
@@ -195,7 +198,8 @@ template <typename T> hipError_t launch_pass(const bagel_attention_pass<T> &p, c
 {
     if (!by_rows<T>(b)) return bagel_launch_attention_pass(p, stream);
     const int64_t work = (int64_t)p.sequences * p.states, clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
-    if (work + clear > 0) rows_kernel<T><<<(unsigned)(work + clear), 256, 0, stream>>>(p);
+    if (work + clear == 0) return hipSuccess;
+    rows_kernel<T><<<(unsigned)(work + clear), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -307,6 +311,7 @@ const char *check_heads(const bagel_heads &h, int64_t rows, int heads, int width
     if (!h.data) return nullptr;
     if ((uintptr_t)h.data & (bagel_type_bytes(dtype) - 1)) return "heads do not start at a multiple of their type";
     if (h.stride < 0 || h.head < 0 || h.stride >= 1ll << 40 || h.head >= 1ll << 40) return "a stride of heads or rows must be >= 0 and below 2^40";
+    if (rows > 1 && h.stride > (1ll << 60) / rows) return "rows reach past 2^60 entries";
     if (!written) return nullptr;
     const bool side_by_side = (heads <= 1 || h.head >= width) && (rows <= 1 || h.stride >= (heads - 1) * h.head + width);
     const bool one_after_the_other = (rows <= 1 || h.stride >= width) && (heads <= 1 || h.head >= (rows - 1) * h.stride + width);
