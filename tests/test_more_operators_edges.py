@@ -1,0 +1,169 @@
+"""Layer norm, linear attention and clipping at sizes and in calls where they can go wrong, against plain implementations in 64 bits (tests/test_more_operators.py,
+whose tolerances count roundings)."""
+import pytest
+import torch
+
+from paper_2202_13638_amd import binding
+from test_more_operators import (NAN, TYPES, _attention_all, _attention_check, _attention_inputs, _attention_struct, _attention_want, _near, _norm_case, _normal, _offsets, _refused)
+
+gpu = pytest.mark.gpu
+
+
+def _case(lengths, heads, states, dk, dv, t, seed, ld=None, offsets=None):
+    x, decays = _attention_inputs(lengths, heads, states, dk, dv, t, seed=seed)
+    decays = decays if ld is None else torch.full((states,), ld)
+    want, terms = _attention_want(x, lengths, decays, 0.2)
+    got = _attention_all(x, lengths, decays, 0.2, offsets=offsets)
+    _attention_check(got, want, terms, t)
+    return x, decays, got
+
+
+# four heads to a memory: what is shared out is two chunks long
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[127], [128], [129], [255, 1], [256], [257], [385, 0, 0, 127], [1, 640], [128] * 4, [129] * 4, [256, 0, 256, 1, 127, 384]],
+                         ids=lambda v: "x".join(map(str, v)))
+def test_lengths_at_the_ends_of_what_is_shared_out(lengths, dtype):
+    _case(lengths, 8, 2, 24, 32, TYPES[dtype], seed=20 + len(lengths))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("long_at", [0, 77, 200])
+def test_many_sequences_of_which_one_is_long(long_at, dtype):
+    lengths = [(7 * i) % 5 for i in range(201)]
+    lengths[long_at] = 700
+    _case(lengths, 4, 1, 16, 16, TYPES[dtype], seed=30)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_equal_lengths_that_are_shared_out_without_offsets(dtype):
+    x, ld, got = _case([400] * 3, 4, 1, 64, 40, TYPES[dtype], seed=31)
+    again = _attention_all(x, [400] * 3, ld, 0.2, offsets=3)
+    assert all(torch.equal(got[k], again[k]) for k in got)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("heads,states,dk,dv", [(2, 2, 128, 128), (4, 1, 64, 64), (4, 1, 128, 100), (4, 2, 64, 128), (2, 2, 8, 128), (3, 1, 9, 8), (2, 1, 7, 64)])
+def test_gradients_asked_for_one_by_one(heads, states, dk, dv, dtype):
+    """Those of keys and values are made together where both are wanted; each alone, and each with another one, is held to the same bounds."""
+    t, lengths = TYPES[dtype], [70, 0, 300]
+    x, ld = _attention_inputs(lengths, heads, states, dk, dv, t, seed=32)
+    want, terms = _attention_want(x, lengths, ld, 0.2)
+    g = {k: v.cuda() for k, v in x.items()}
+    for wanted in ("q", "k", "v", "qk", "qv", "kv"):
+        outs = [torch.full_like(g[k], NAN) if k in wanted else None for k in "qkv"]
+        binding.bagel_linear_attention_grad(g["q"], g["k"], g["v"], g["d_out"], *outs, _offsets(lengths), ld.cuda(), scale=0.2, initial=g["initial"], d_final=g["d_final"])
+        _attention_check({n: o for n, o in zip(("d_query", "d_key", "d_value"), outs) if o is not None}, want, terms, t)
+
+
+@gpu
+def test_float16_of_small_and_large_inputs():
+    """Inputs times powers of two that bring their products far below and above what float16 holds, while the results are what they were: the same up to the
+    roundings of what is multiplied."""
+    t, lengths = torch.float16, [150, 40]
+    x, ld = _attention_inputs(lengths, 2, 1, 64, 48, t, seed=33)
+    x["d_final"].zero_()                             # (which no power of two stands against)
+    want, terms = _attention_want(x, lengths, ld, 0.2)
+    for q, k in ((-8, -6), (9, 10)):                 # products of 2^-14, where float16 has few bits left, and of 2^19, which it does not hold
+        y = dict(x, q=x["q"] * 2.0 ** q, k=x["k"] * 2.0 ** k, initial=x["initial"] * 2.0 ** k)
+        exact = dict(q=(y["q"].double() * 2.0 ** -q), k=(y["k"].double() * 2.0 ** -k))
+        if any(not torch.equal(exact[n], x[n].double()) for n in exact):       # what the scaling itself rounds away is not the kernels'
+            w, a = _attention_want(dict(x, **{n: e for n, e in exact.items()}), lengths, ld, 0.2)
+        else:
+            w, a = want, terms
+        got = _attention_all(y, lengths, ld, 0.2 * 2.0 ** -(q + k))
+        _attention_check({"out": got["out"], "d_value": got["d_value"]}, w, a, t)
+
+
+@gpu
+def test_large_memories_stay_what_float32_holds():
+    """A memory that is a million times its rows: the decay of nothing, and keys of nothing, leave it as it was."""
+    for dtype, t in TYPES.items():
+        x, _ = _attention_inputs([130], 2, 2, 64, 64, t, seed=34)
+        x["initial"] *= 1e6
+        x["k"].zero_()
+        got = _attention_all(x, [130], torch.zeros(2), 0.2)
+        assert torch.equal(got["final"].cpu(), x["initial"]), dtype
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width,groups", [(1, 1, 1), (3, 64, 64), (5, 16384, 1), (2, 16384, 16384), (1, 16383, 3), (1000, 24, 3), (257, 1000, 1000)])
+def test_layer_norm_of_the_smallest_and_largest_parts(rows, width, groups, dtype):
+    t = TYPES[dtype]
+    _norm_case(_normal((rows, width), 41, t), _normal((rows, width), 42, t), _normal((width,), 43, mean=1.0), _normal((width,), 44), groups)
+
+
+@gpu
+def test_a_result_in_another_gradients_place_is_refused():
+    a, b = torch.randn(300, device="cuda"), torch.randn(300, device="cuda")
+    norm, factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    for grads, out in (([a, a], [a, a]), ([a, a], [b, b]), ([a[:200], b], [a[1:201], None]), ([a, b], [b, b])):
+        with pytest.raises(binding.BagelError, match="overlaps"):
+            binding.bagel_clip_norm(grads, 1.0, norm, factor, out=out)
+    binding.bagel_clip_norm([a, b], 1.0, norm, factor, out=[b, None])        # b is read for the norm alone, before it is written
+    _near(b, a.double().cpu() * float(factor), "out", a.double().cpu().abs() * float(factor))
+
+
+@gpu
+def test_a_graph_of_a_training_pass_is_the_pass():
+    """Forward, gradient, norm and clipping captured together, replayed with eager calls of other sizes and synchronizations between."""
+    t, lengths = torch.bfloat16, [300, 5, 200]
+    x, ld = _attention_inputs(lengths, 4, 1, 64, 64, t, seed=35)
+    g, at, ld = {k: v.cuda() for k, v in x.items()}, _offsets(lengths), ld.cuda()
+    r = {k: torch.zeros_like(v) for k, v in dict(out=g["d_out"], y=g["d_out"], d=g["d_out"], dq=g["q"], dk=g["k"], dv=g["v"]).items()}
+    w = torch.randn(4 * 64, device="cuda")
+    dw, db, norm, factor = torch.zeros_like(w), torch.zeros_like(w), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+
+    def go():
+        flat = lambda z: z.view(505, 256)
+        binding.bagel_linear_attention(g["q"], g["k"], g["v"], r["out"], at, ld, scale=0.2)
+        binding.bagel_layer_norm(flat(r["out"]), flat(r["y"]), weight=w, groups=4)
+        binding.bagel_layer_norm_grad(flat(r["out"]), flat(g["d_out"]), flat(r["d"]), weight=w, groups=4, d_weight=dw, d_bias=db)
+        binding.bagel_linear_attention_grad(g["q"], g["k"], g["v"], r["d"], r["dq"], r["dk"], r["dv"], at, ld, scale=0.2)
+        binding.bagel_clip_norm([r["dq"], r["dk"], r["dv"], dw, db], 0.5, norm, factor, out=[r["dq"], None, None, dw, db])
+
+    def results():
+        torch.cuda.synchronize()
+        return [z.clone() for z in (*r.values(), dw, db, norm, factor)]
+
+    go()
+    want = results()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for turn in range(4):
+        for z in (*r.values(), dw, db, norm, factor):
+            z.fill_(NAN)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(results(), want)), turn
+        other, o = _attention_inputs([90 + turn], 2, 2, 32, 32, t, seed=36)
+        _attention_all(other, [90 + turn], o, 0.2)
+
+
+@gpu
+def test_two_streams_at_once():
+    """Each call has work space of its own."""
+    t, lengths = torch.bfloat16, [3000]
+    x, ld = _attention_inputs(lengths, 4, 1, 64, 64, t, seed=37)
+    want = _attention_all(x, lengths, ld, 0.2)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(3)], []
+    for s in streams * 2:
+        with torch.cuda.stream(s):
+            got.append(_attention_all(x, lengths, ld, 0.2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(r[k], want[k]) for r in got for k in want)
+
+
+def test_heads_that_lead_too_far_are_refused():
+    for call, name in (("bagel_linear_attention", "value"), ("bagel_linear_attention_grad", "d_key"), ("bagel_linear_attention", "out")):
+        _refused(call, _attention_struct(rows=(1 << 28) - 1, sequences=1, **{name + "_stride": (1 << 33) + 1}), "2^60")
