@@ -142,13 +142,15 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
 int64_t segment_rows(const bagel_attention &b)
 {
     constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
-    // what a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits
-    const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 2 : 1), least = step < 4 ? 8 / step : 2;
+    // What a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits, two in 32.  (Of 8 heads of 64 in
+    // bf16 on 8 memories, 20 sequences of up to 4000 rows: 486 us by segments of one chunk, 249 by eight.  10007 rows, 61 sequences, 6 heads of 40 and 77 on 3
+    // memories, float32: between 356 and 375 us with one to four chunks, 563 with seven.)
+    const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 4 : 1), least = step < 8 ? 8 / step : 1;
     const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 248 : 496;       // one or two workgroups to a compute unit
     int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
     if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
     const int64_t chunks = (rows + chunk - 1) / chunk;
-    return chunk * (chunks <= least ? least : chunks | 1);
+    return chunk * (chunks <= least ? least : chunks == 2 ? 2 : chunks | 1);
 }
 
 // A segment's rows, and how many numbers there are for segments that are not the first of their sequence.
