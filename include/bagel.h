@@ -522,6 +522,7 @@ int bagel_layer_norm_grad(const bagel_norm *args, void *hip_stream);
  * Rows behind the last sequence: what they hold is not used, and their results are zero.  Products take their operands in the type of the activations, which
  * for sums within a chunk of rows means one rounding of what is multiplied; the memories, their sums and decays are in float32.
  * (Offsets that break their rules give wrong numbers, but no access outside of the arrays.)
+ * What is not finite in a row stays in its sequence and memory, and in the rows from there on (back to the front, in a gradient).
  *
  * bagel_linear_attention_grad: from the same inputs, d_out (the gradient for out) and d_final (for final_state, NULL: zero): d_query, d_key, d_value of the shapes of
  * query, key and value, and d_initial, any of which may be left out.  Gradients of a shared memory's key and value are sums over its heads.  Nothing of the

@@ -10,7 +10,7 @@
 
 namespace {
 
-// A pass row after row: a workgroup to a memory, an entry of its columns in each of 128 threads for half of its rows.
+// A pass row after row, for heads that are shorter than a pack: a workgroup to a memory, an entry of its columns in each of 128 threads for half of its rows.
 template <typename T> __global__ __launch_bounds__(256) void rows_kernel(bagel_attention_pass<T> p)
 {
     constexpr int MOST = BAGEL_ATTENTION_MAX_WIDTH;
@@ -69,6 +69,8 @@ template <typename T> __global__ __launch_bounds__(256) void rows_kernel(bagel_a
 
 // One row of each of many sequences.  A workgroup to a memory: V columns to a thread, whose rows follow each other by as many as there are threads for; the
 // memory is read and written once, where no more than HEADS heads share it (more of them read it again, out of the cache).
+//   The memories bound it, 8 bytes an entry: 256 sequences of 8 memories of 64 x 64 take 16.2 us (4.2 TB/s) of whole calls, 13 to 15 of the kernel, one sequence 6.8 us, of which
+// 5 are the kernel's latency.  Packs of four columns: by single columns 22.6 and 8.7 us.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int each, int wk, int wv, float scale, const float *log_decay, bagel_heads_of<T> q,
                                                    bagel_heads_of<T> k, bagel_heads_of<T> v, bagel_heads_of<T> out, float *state)

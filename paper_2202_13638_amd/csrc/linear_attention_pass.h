@@ -4,6 +4,9 @@
 //   out_m = scale (l^(m+1) S^T a_m + sum_{n<=m} P_mn c_n),   P_mn = scale_b l^(m-n) a_m.b_n
 //   S <- l^64 S + sum_n scale_b l^(63-n) b_n c_n^T                     (back: l^m S^T a_m, and l^(64-n))
 // No power of l is negative, so nothing grows that the definition does not let grow.
+//   By the definition, row after row, the work is 3 to 5 operations for every entry of a memory and row, none of which a matrix instruction can do, and each row waits for the one
+// before it.  By chunks it is matrix products throughout, and a chunk waits for a memory instead.  64 rows: with more of them P, which grows by their square, takes
+// longer than the memory's update, with fewer the update, made once a chunk, takes longer than P.
 #pragma once
 
 #include <type_traits>
@@ -193,7 +196,7 @@ template <typename T, int W> __device__ __forceinline__ void clear(tile<T, W> &t
         for (int i = threadIdx.x; i < CHUNK * t.pitch; i += blockDim.x) t.x[i] = (T)0.0f;
 }
 
-// The wait states between the products in 32 bits and whatever uses their results, ahead of a branch: the compiler may count them along the longer way only.
+// The wait states between products and whatever uses their results, ahead of a branch: the compiler may count them along the longer way only.
 __device__ __forceinline__ void settle(floats &x) { asm volatile("s_nop 9" : "+v"(x)); }
 template <int N> __device__ __forceinline__ void settle(floats (&x)[N])
 {
@@ -407,7 +410,7 @@ __device__ __forceinline__ void make_piece(tile<T, W> &a, const tile<T, W> &b, t
     to.along(along_p, it, kb) = x;
 }
 
-// The six pieces of P that are not zero, shared out among the waves; `shift`: which wave comes first.
+// The six pieces of P that are not zero, shared out among the waves.
 template <int WAVES, typename T, int W, typename L>
 __device__ __forceinline__ void make_pieces(tile<T, W> &a, const tile<T, W> &b, tile<T, CHUNK> &to, powers &w, int which, float tile_on, int along_a, int spread_b, const L &l, int wave)
 {
@@ -515,6 +518,81 @@ template <typename T> __device__ __forceinline__ bagel_pack<T, 4> rounded(const 
     return x;
 }
 
+// Whether results are finite: zero as long as they are.
+__device__ __forceinline__ void look_at(float &seen, const floats &o)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) seen = fmaf(o[j], 0.0f, seen);
+}
+
+// The memory that a segment begins with.
+template <typename T> __device__ __forceinline__ const float *memory_before(const bagel_attention_pass<T> &p, const place &at, int state)
+{
+    const int64_t size = (int64_t)p.wb * p.wc;
+    if (at.before >= 0) return p.memories + (at.before * p.states + state) * size;
+    return p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr;
+}
+
+// A segment once more, row after row, a wave its 16 columns.  By chunks, what is not finite in a row reaches the rows of its chunk that come before it, whose weight is zero:
+// zero times those is NaN.  So a wave that has seen results that are not finite makes all of its results again.  (To look at the operands in every step and to leave
+// such ones out of the products took 14 to 17 % more time for its registers and branches; to look at the results takes 0 to 3 %.)
+//   It needs nothing that the chunks have made, the kernel's arguments are read anew (`which`: of the passes that they hold), so that no register is taken in the loop.
+template <typename T, int NB> __device__ __forceinline__ void again(int which)
+{
+    uint64_t arguments = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(arguments));
+    const bagel_attention_pass<T> p = ((const bagel_attention_pass<T> *)arguments)[which];
+    const int64_t first = (int64_t)p.sequences * p.states, work = by_dies(blockIdx.x, first, first + p.further * p.states), number = work / p.states;
+    const int state = (int)(work - number * p.states), column = afresh(threadIdx.x >> 6) * 16 + (threadIdx.x & 15);
+    const place at = place_of(p, number);
+    const float *before = memory_before(p, at, state);
+    const int step = p.back ? -1 : 1, g = (threadIdx.x & 63) >> 4;
+    const float decay = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f);
+    const auto entry = [&](const T *row, int bt, int j) {
+        const int r = memory_row<NB>(bt, j);
+        return r < p.wb ? (float)row[r] : 0.0f;
+    };
+    floats S[NB];
+    read_memory(S, before, p.step_b, p.step_c, column, p.wb, p.wc);
+    for (int64_t n = 0; n < at.rows; ++n) {
+        const int64_t row = at.base + step * n;
+        const float keep = p.back ? 1.0f : decay, after = p.back ? decay : 1.0f;
+#pragma unroll
+        for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[bt][j] *= keep;
+        for (int h = 0; h < p.ks; ++h) {
+            const T *b = p.b.at(row, state * p.ks + h);
+            const float c = column < p.wc ? (float)p.c.at(row, state * p.ks + h)[column] * p.scale_b : 0.0f;
+#pragma unroll
+            for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[bt][j] = fmaf(entry(b, bt, j), c, S[bt][j]);
+        }
+        for (int h = 0; h < p.qs; ++h) {
+            const T *a = p.a.at(row, state * p.qs + h);
+            float o = 0.0f;
+#pragma unroll
+            for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o = fmaf(entry(a, bt, j), S[bt][j], o);
+            o += __shfl_xor(o, 16);
+            o += __shfl_xor(o, 32);
+            if (g == 0 && column < p.wc) p.out.at(row, state * p.qs + h)[column] = (T)(o * p.scale);
+        }
+#pragma unroll
+        for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[bt][j] *= after;
+    }
+}
+// All of a workgroup's results are in memory.
+__device__ __forceinline__ void all_written()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // Goes through a segment's rows: `ask(tiles, base, h)` asks for the 64 rows from `base` on of head h, ask_few for those that are there of fewer, and `go(tiles,
 // h, n, base, next)` takes a step: it puts the tiles away and calls `next`, which asks for those of the steps to come: DEEP of them are on their way.  Behind the
 // last ones the same are asked for again, which nobody reads: a branch around the loads would make every wait one for all of them.
@@ -577,6 +655,7 @@ template <typename T> struct two_passes {
 
 // What a segment adds to the memory, or, of the first one of a sequence, the memory behind it.  Segments that are the last of theirs are nobody's to add, so there are
 // as many to do as further ones, each of which waits for the one before it.
+//   It reads b and c once more than the pass itself: one head of 128 in bf16, 131072 rows, 2 memories, 42 us (134 MB, 3.2 TB/s).
 template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch_bounds__(4 * WC, 2) void sums_kernel(two_passes<T> both)
 {
     bagel_attention_pass<T> p = blockIdx.y ? both.p[1] : both.p[0];
@@ -630,7 +709,8 @@ template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch
     write_memory(S, p.memories + (behind_it.before * p.states + state) * size, p.step_b, p.step_c, column, p.wb, p.wc);
 }
 
-// What segments have added to the memory, into the memory behind each: a thread to an entry, along its sequence's segments but the last.
+// What segments have added to the memory, into the memory behind each: a thread to an entry, along its sequence's segments but the last, 16 of which are asked for at
+// a time (114 segments of 2 memories of 128 x 128: 14 us).
 template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two_passes<T> both, int blocks)
 {
     const bagel_attention_pass<T> p = blockIdx.y ? both.p[1] : both.p[0];
@@ -659,17 +739,13 @@ template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two
     }
 }
 
-// The memory that a segment begins with.
-template <typename T> __device__ __forceinline__ const float *memory_before(const bagel_attention_pass<T> &p, const place &at, int state)
-{
-    const int64_t size = (int64_t)p.wb * p.wc;
-    if (at.before >= 0) return p.memories + (at.before * p.states + state) * size;
-    return p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr;
-}
-
 // A pass over a segment.  A wave to 16 columns of a memory, of c and of out, in float32 in its registers.  The rows' products with each other, P, are shared out
 // among the waves by pieces (16 rows of it, 32 rows they are multiplied with), and meet in shared memory.
 // WHOLE: a and b are as wide as their tiles, and so are c and out.
+//   In 16 bits the memory's rate bounds it: 64000 rows, 8 heads of 64, bf16, 56 us (262 MB, 4.7 TB/s); 131072 rows, 8 heads of 128 on 2 memories 157 to 180 us (671 MB, 4.3 to 3.7 TB/s).
+// What brought it there: one chunk of the next step on its way 175 -> 129 us (the former case with its other launches), loads without a branch and results in packs -> 79,
+// slots without bank conflicts and two steps on their way -> 62.  A workgroup has two compute units' neighbours at most (its tiles take 57 to 90 KB), so what is on its
+// way, not how many waves there are, keeps the memory busy.  In 32 bits the matrix instructions have a sixteenth of the rate, and padded widths count as whole.
 template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD> __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention_pass<T> p)
 {
     if constexpr (WHOLE) {
@@ -714,6 +790,7 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
         incoming<T, WC, THREADS> c;
     } coming[2];
     floats O[HEADS == MANY_B ? 4 : 1];
+    float seen = 0.0f;
     T *ready = nullptr;                              // where the rows in `so` go, and how many there are
     int ready_rows = 0;
     const auto flush = [&] {
@@ -767,7 +844,9 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
                 if (enter) o = from_memory(sa, s, it, weight, l.along_a);
                 weight *= tile_on;
                 from_rows(o, c, sp, w, 0, it, l.along_p);
+                if constexpr (HEADS == MANY_B) settle(o);
                 if (!leave) continue;
+                look_at(seen, o);
                 const bagel_pack<T, 4> x = rounded<T>(o, p.scale);
                 if constexpr (THROUGH) {
                     so.entries(l.entries_o, it, wave) = x;
@@ -790,9 +869,12 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
         flush();
     }
     if (at.last && p.last) write_memory(S, p.last + ((int64_t)at.sequence * p.states + state) * p.wb * p.wc, p.step_b, p.step_c, column, p.wb, p.wc);
+    all_written();
+    if (__any(seen != 0.0f)) again<T, WB / 16>(0);
 }
 
-// The gradients of keys and values: two such passes at once, whose memories are each other's transpose, from the same tiles.
+// The gradients of keys and values: two such passes at once, whose memories are each other's transpose, from the same tiles.  Four tiles are read in the place of six
+// (64000 rows, 8 heads of 64, bf16: 92 us for 393 MB, 4.3 TB/s; two passes one after the other took 130).
 template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__(4 * W, 2) void keys_kernel(bagel_attention_pass<T> p, bagel_attention_pass<T> q)
 {
     if constexpr (WHOLE) p.wb = p.wc = q.wb = q.wc = W;
@@ -829,6 +911,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
         incoming<T, W, THREADS> k, v, q, d;
     } coming[1];
     floats O[2][MANY ? 4 : 1];
+    float seen[2] = {0.0f, 0.0f};
     T *ready[2] = {nullptr, nullptr};
     int ready_rows = 0;
     const auto flush = [&] {
@@ -884,7 +967,10 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
                     if (enter) o = from_memory(a, memory, it, weight, l.along_a);
                     weight *= tile_on;
                     from_rows(o, x, sp[which], w, which, it, l.along_p);
-                    if (leave) so[which].entries(l.entries_o, it, wave) = rounded<T>(o, 1.0f);
+                    if constexpr (MANY) settle(o);
+                    if (!leave) continue;
+                    look_at(seen[which], o);
+                    so[which].entries(l.entries_o, it, wave) = rounded<T>(o, 1.0f);
                 }
             };
             results(sk, s, e, d, 0);
@@ -896,6 +982,9 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     __syncthreads();
     flush();
     if (at.last && p.last) write_memory(R, p.last + ((int64_t)at.sequence * p.states + state) * p.wb * p.wc, p.step_b, p.step_c, column, p.wb, p.wc);
+    all_written();
+    if (__any(seen[0] != 0.0f)) again<T, W / 16>(0);
+    if (__any(seen[1] != 0.0f)) again<T, W / 16>(1);
 }
 
 // f with constants for the widths of the tiles, and whether the rows fill them.

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2202_13638_amd import binding
-from test_more_operators import (NAN, TYPES, _attention_all, _attention_check, _attention_inputs, _attention_struct, _attention_want, _near, _norm_case, _normal, _offsets, _refused)
+from test_more_operators import (HALF_ULP, NAN, TYPES, _attention_all, _attention_check, _attention_inputs, _attention_struct, _attention_want, _near, _norm_case, _normal, _offsets, _refused)
 
 gpu = pytest.mark.gpu
 
@@ -167,3 +167,26 @@ def test_two_streams_at_once():
 def test_heads_that_lead_too_far_are_refused():
     for call, name in (("bagel_linear_attention", "value"), ("bagel_linear_attention_grad", "d_key"), ("bagel_linear_attention", "out")):
         _refused(call, _attention_struct(rows=(1 << 28) - 1, sequences=1, **{name + "_stride": (1 << 33) + 1}), "2^60")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,states,dk,dv", [(2, 2, 64, 64), (4, 2, 40, 77), (4, 2, 128, 128), (2, 2, 128, 24), (3, 1, 5, 4)])
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+def test_what_is_not_finite_reaches_no_row_before_it(bad, heads, states, dk, dv, dtype):
+    """Results of earlier rows (in the gradients of keys and values: of later ones) are what they are without it; from its row on nothing finite is left where
+    it is."""
+    t, n, at = TYPES[dtype], 150, 77
+    x, ld = _attention_inputs([n], heads, states, dk, dv, t, seed=50)
+    want, terms = _attention_want(x, [n], ld, 0.2)
+    for name, places in (("v", {"out": slice(0, at)}), ("k", {"out": slice(0, at), "d_query": slice(0, at)}), ("q", {"d_key": slice(at + 1, n), "d_value": slice(at + 1, n)}),
+                         ("d_out", {"d_key": slice(at + 1, n), "d_value": slice(at + 1, n)})):
+        y = dict(x, **{name: x[name].clone()})
+        y[name][at, 0, 2] = bad
+        got = _attention_all(y, [n], ld, 0.2)
+        for k, rows in places.items():
+            _near(got[k][rows], want[k][rows], f"{k} for {name}", terms[k][rows], 0.0 if dtype == "f32" else 2 * HALF_ULP[t])
+        if name == "v":
+            assert not got["out"][at:, 0, 2].isfinite().any()
+        if name == "d_out":
+            assert not got["d_value"][:at + 1, 0, 2].isfinite().any()
