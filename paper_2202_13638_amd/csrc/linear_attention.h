@@ -32,6 +32,7 @@ template <typename T> struct bagel_attention_pass {
     int64_t step_b, step_c;                          // of a memory's entries, wb times wc in either order; [sequences][states] of them
     int64_t segment;                                 // a multiple of the chunk
     int64_t further;                                 // numbers of segments that are not the first of their sequence
+    bool join;                                       // whether a segment joins what those before it have added, which then no launch has done
     float *memories;                                 // [sequences + further][states][..]: behind every segment but the last; null: one segment to a sequence
 };
 

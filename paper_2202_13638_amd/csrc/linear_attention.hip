@@ -141,6 +141,7 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
 // written and read.  Where there are sequences enough, they are left whole, and only one that is far longer than the others is shared out.
 //   An odd number of chunks: workgroups go through their rows side by side, and with a power of two between them they ask the same channels of the memory
 // (131072 rows, 8 heads of 128 on 2 memories, bf16: 259 us with 16 chunks and 256 workgroups, 162 with 18 chunks and 228).
+int64_t wanted_groups(const bagel_attention &b) { return b.key_width > 64 || b.value_width > 64 ? 248 : 496; }      // one or two workgroups to a compute unit
 int64_t segment_rows(const bagel_attention &b)
 {
     constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
@@ -148,7 +149,7 @@ int64_t segment_rows(const bagel_attention &b)
     // bf16 on 8 memories, 20 sequences of up to 4000 rows: 486 us by segments of one chunk, 249 by eight.  10007 rows, 61 sequences, 6 heads of 40 and 77 on 3
     // memories, float32: between 356 and 375 us with one to four chunks, 563 with seven.)
     const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 4 : 1), least = step < 8 ? 8 / step : 1;
-    const int64_t wanted = b.key_width > 64 || b.value_width > 64 ? 248 : 496;       // one or two workgroups to a compute unit
+    const int64_t wanted = wanted_groups(b);
     int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
     if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
     const int64_t chunks = (rows + chunk - 1) / chunk;
@@ -169,6 +170,10 @@ int64_t memories_floats(const bagel_attention &b, const segments &s)
     return s.further > 0 ? (b.sequences + s.further) * b.states * b.key_width * b.value_width : 0;
 }
 
+// Whether segments join the memories before them themselves, which saves a launch of 5 us: where there can be few, and where there are sequences enough, so that
+// mostly there are none.  (Each reads all that its sequence's segments before it have added: 16 of them take as long as the launch.)
+bool joined(const bagel_attention &b, int64_t further) { return further <= 16 || (further <= 64 && (int64_t)b.sequences * b.states >= wanted_groups(b)); }
+
 template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
 {
     const segments s = segments_of(b, b.offsets);
@@ -182,6 +187,7 @@ template <typename T> bagel_attention_pass<T> args_of(const bagel_attention &b)
     p.scale = p.scale_b = 1.0f;
     p.segment = s.rows;
     p.further = s.further;
+    p.join = joined(b, s.further);
     p.qs = p.ks = 1;
     return p;
 }

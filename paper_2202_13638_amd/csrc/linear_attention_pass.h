@@ -237,6 +237,7 @@ struct place {
     int64_t base;                // its first row, in the order they are gone through
     int64_t rows;
     int64_t before;              // the number of the segment before, -1: it is the first
+    int64_t further;             // of its sequence's segments before, those that are not the first
     bool last, there;
 };
 
@@ -260,6 +261,7 @@ template <typename T> __device__ __forceinline__ place place_of(const bagel_atte
     if (number < p.sequences) {
         r.sequence = (int)number;
         r.before = -1;
+        r.further = 0;
     } else {
         const int64_t further = number - p.sequences;
         if (!p.offsets) {
@@ -281,6 +283,7 @@ template <typename T> __device__ __forceinline__ place place_of(const bagel_atte
             s = further - min(max((int64_t)p.offsets[r.sequence], (int64_t)0), p.rows) / p.segment + 1;
         }
         r.before = s == 1 ? r.sequence : number - 1;
+        r.further = s - 1;
     }
     int64_t begin, end;
     sequence_rows(p, r.sequence, begin, end);
@@ -525,12 +528,31 @@ __device__ __forceinline__ void look_at(float &seen, const floats &o)
     for (int j = 0; j < 4; ++j) seen = fmaf(o[j], 0.0f, seen);
 }
 
-// The memory that a segment begins with.
-template <typename T> __device__ __forceinline__ const float *memory_before(const bagel_attention_pass<T> &p, const place &at, int state)
+// What a segment's length leaves of the memory before it.
+template <typename T> __device__ __forceinline__ float kept(const bagel_attention_pass<T> &p, int state)
 {
-    const int64_t size = (int64_t)p.wb * p.wc;
-    if (at.before >= 0) return p.memories + (at.before * p.states + state) * size;
-    return p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr;
+    return __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
+}
+
+// The memory that a segment begins with: joined here, of what the segments before it have added, where that has not been done.
+template <typename T, int NB> __device__ __forceinline__ void read_before(floats (&S)[NB], const bagel_attention_pass<T> &p, const place &at, int state, int column)
+{
+    const int64_t size = (int64_t)p.wb * p.wc, each = p.states * size;
+    const float *from = p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr;
+    const int64_t join = p.join ? at.further : 0;
+    if (at.before >= 0) from = p.memories + ((join > 0 ? at.sequence : at.before) * p.states + state) * size;
+    read_memory(S, from, p.step_b, p.step_c, column, p.wb, p.wc);
+    if (join <= 0) return;
+    const float keep = kept(p, state);
+    from = p.memories + ((at.before + 1 - join) * p.states + state) * size;
+    for (int64_t k = 0; k < join; ++k, from += each) {
+        floats add[NB];
+        read_memory(add, from, p.step_b, p.step_c, column, p.wb, p.wc);
+#pragma unroll
+        for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[bt][j] = fmaf(keep, S[bt][j], add[bt][j]);
+    }
 }
 
 // A segment once more, row after row, a wave its 16 columns.  By chunks, what is not finite in a row reaches the rows of its chunk that come before it, whose weight is zero:
@@ -545,7 +567,6 @@ template <typename T, int NB> __device__ __forceinline__ void again(int which)
     const int64_t first = (int64_t)p.sequences * p.states, work = by_dies(blockIdx.x, first, first + p.further * p.states), number = work / p.states;
     const int state = (int)(work - number * p.states), column = afresh(threadIdx.x >> 6) * 16 + (threadIdx.x & 15);
     const place at = place_of(p, number);
-    const float *before = memory_before(p, at, state);
     const int step = p.back ? -1 : 1, g = (threadIdx.x & 63) >> 4;
     const float decay = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f);
     const auto entry = [&](const T *row, int bt, int j) {
@@ -553,7 +574,7 @@ template <typename T, int NB> __device__ __forceinline__ void again(int which)
         return r < p.wb ? (float)row[r] : 0.0f;
     };
     floats S[NB];
-    read_memory(S, before, p.step_b, p.step_c, column, p.wb, p.wc);
+    read_before(S, p, at, state, column);
     for (int64_t n = 0; n < at.rows; ++n) {
         const int64_t row = at.base + step * n;
         const float keep = p.back ? 1.0f : decay, after = p.back ? decay : 1.0f;
@@ -722,7 +743,7 @@ template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two
         const int64_t first = p.offsets ? begin / p.segment : sequence * further_of_each(p), each = (int64_t)p.states * size;
         const int64_t n = min((end - begin + p.segment - 1) / p.segment - 2, p.further - first);     // segments to join: neither the first nor the last
         if (n < 1) continue;
-        const float keep = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
+        const float keep = kept(p, state);
         for (int i = (int)(work % blocks) * 256 + threadIdx.x; i < size; i += blocks * 256) {
             float s = p.memories[((int64_t)sequence * p.states + state) * size + i];
             float *m = p.memories + ((p.sequences + first) * p.states + state) * size + i;
@@ -770,7 +791,7 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
     const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
     const int step = p.back ? -1 : 1, behind = p.back ? 1 : 0;       // of powers of l
     floats S[WB / 16];
-    read_memory(S, memory_before(p, at, state), p.step_b, p.step_c, column, p.wb, p.wc);
+    read_before(S, p, at, state, column);
     w.weigh_out(l2, behind, p.scale_b, CHUNK);
     w.weigh_p(l2, p.scale_b);
     const float tile_on = power(l2, 16), weight_in = power(l2, j16 + 1 - behind), whole = power(l2, CHUNK);
@@ -894,8 +915,8 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = wave * 16 + (threadIdx.x & 15);
     const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
     floats R[W / 16], Rt[W / 16];
-    read_memory(R, memory_before(p, at, state), p.step_b, p.step_c, column, p.wb, p.wc);
-    read_memory(Rt, memory_before(q, at, state), q.step_b, q.step_c, column, q.wb, q.wc);
+    read_before(R, p, at, state, column);
+    read_before(Rt, q, at, state, column);
     w.weigh_out(l2, 1, p.scale_b, CHUNK);
     w.weigh_p(l2, p.scale_b);
     const float tile_on = power(l2, 16), weight_in = power(l2, threadIdx.x & 15), whole = power(l2, CHUNK);
@@ -1021,6 +1042,7 @@ template <typename T> hipError_t bagel_launch_attention_memories(const bagel_att
         if (many) sums_kernel<T, WB, WC, decltype(whole)::value, true><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
         else sums_kernel<T, WB, WC, decltype(whole)::value, false><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
     });
+    if (p.join) return hipGetLastError();
     // some workgroups to a memory where there are few of them
     const int64_t all = (int64_t)p.sequences * p.states, most = (p.wb * p.wc + 255) / 256, wanted = 1024 / all;
     const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);

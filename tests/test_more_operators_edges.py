@@ -38,6 +38,14 @@ def test_many_sequences_of_which_one_is_long(long_at, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,states", [([10, 2900, 0, 150], 8, 1), ([20] * 69 + [1500], 64, 8), ([1300, 1] + [0] * 61 + [30], 64, 8)], ids=["alone", "last", "first"])
+def test_a_sequence_of_many_parts(lengths, heads, states, dtype):
+    """Parts of one or two chunks: their memories are joined by a launch of its own (the first case), or by the parts themselves."""
+    _case(lengths, heads, states, 8, 12, TYPES[dtype], seed=60, ld=-0.003)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
 def test_equal_lengths_that_are_shared_out_without_offsets(dtype):
     x, ld, got = _case([400] * 3, 4, 1, 64, 40, TYPES[dtype], seed=31)
     again = _attention_all(x, [400] * 3, ld, 0.2, offsets=3)
