@@ -519,8 +519,9 @@ int bagel_layer_norm_grad(const bagel_norm *args, void *hip_stream);
  *   initial[sequences][states][key_width][value_width]  S before the first row, NULL: zero
  *   final_state of the same shape or NULL: S after the last row; of an empty sequence, its initial state.  Not in the place of `initial`, nor d_initial
  *     in that of d_final (EINVAL)
- * Rows behind the last sequence: what they hold is not used, and their results are zero.  Products take their operands in the type of the activations, which
- * for sums within a chunk of rows means one rounding of what is multiplied; the memories, their sums and decays are in float32.
+ * Rows behind the last sequence: what they hold is not used, and their results are zero.  Sums, memories and decays are in float32.  Matrix
+ * products take operands in the type of the activations: query, key, value and d_out as they are; what is in float32, the memory and the products of rows with each
+ * other, as the sum of two such numbers (16 bits in bfloat16, 22 in float16), so that what is seen of it in a result is the one rounding to its type.
  * (Offsets that break their rules give wrong numbers, but no access outside of the arrays.)
  * What is not finite in a row stays in its sequence and memory, and in the rows from there on (back to the front, in a gradient).
  *

@@ -206,6 +206,15 @@ template <int N> __device__ __forceinline__ void settle(floats (&x)[N])
     else asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
 }
 
+// Reads of shared memory and products stay on their side of it: left to itself the compiler puts each read right before its product, which then waits for it
+// (131072 rows, 8 heads of 128 on 2 memories, bf16: 272 us without and 248 with what is read ahead; 64000 rows, 8 heads of 64: 64.0 and 62.8).  In 32 bits the products'
+// own time is longer than a read, and 128 x 64 has no registers for what is read ahead (bf16, 64000 rows, 8 heads: 107 us without, 130 with).
+template <typename T, int WB, int WC> constexpr bool AHEAD = sizeof(T) == 2 && !(WB == 128 && WC == 64);
+template <bool WANTED> __device__ __forceinline__ void reads_before_products()
+{
+    if constexpr (WANTED) __builtin_amdgcn_sched_barrier(0x216);
+}
+
 // l^e for whole e >= 0; l2 = log2(l), finite
 __device__ __forceinline__ float power(float l2, int e) { return __builtin_amdgcn_exp2f(l2 * (float)e); }
 
@@ -305,7 +314,7 @@ __device__ __forceinline__ int64_t by_dies(int64_t group, int64_t first, int64_t
 
 // A lane's parts of addresses in shared memory.
 template <typename T, int WB, int WC, int THREADS> struct lane_parts {
-    const int along_a = tile<T, WB>::lane_along(), along_p = tile<T, CHUNK>::lane_along(), spread_b = tile<T, WB>::lane_spread();
+    const int along_a = tile<T, WB>::lane_along(), spread_b = tile<T, WB>::lane_spread();
     const int across_b = tile<T, WB>::lane_across(true), across_c = tile<T, WC>::lane_across(false), entries_o = tile<T, WC>::lane_entries();
     const int pack_b = packs_of<T, WB, THREADS>::lane_part(), pack_c = packs_of<T, WC, THREADS>::lane_part();
 };
@@ -356,47 +365,117 @@ template <int NB> __device__ __forceinline__ void write_memory(const floats (&S)
             if (memory_row<NB>(bt, j) < wb) to[memory_row<NB>(bt, j) * step_b + column * step_c] = S[bt][j];
 }
 
-// A memory as operands, and the exponent that was taken off (float16).
-template <typename T, int NB> __device__ __forceinline__ int as_operands(const floats (&S)[NB], operand<T> (&s)[NB / 2])
+// What is in float32 and becomes an operand, the memory before a chunk and P, is a sum of so many of them.  In 16 bits one alone would round it to 8 or 11 bits, which would be
+// seen in the results (64000 rows, 8 heads of 64, bf16: 0.0023 from 64 bits, where the rounding of the results alone makes 0.0017).  Two hold 16 or 22 bits, of whose
+// rounding nothing is left in results of 8 or 11.  They take 5 to 10 % of the time (that case 57 us with one, 63 with two; its gradient 181 and 193).
+template <typename T> constexpr int PARTS = sizeof(T) == 4 ? 1 : 2;
+// All parts but the last are cut off: what is left is exact, as it would be behind a rounding, which the compiler makes once for the operand and once more for what is left
+// (842 instead of 612 vector instructions in two steps, 716 so).
+template <typename T, int N> __device__ __forceinline__ void in_parts(float (&x)[8], operand<T> (&part)[N])
 {
-    int e = 0;
-    float down = 1.0f;
-    if constexpr (NARROW<T>) {
-        float top = 0.0f;
+    using words = uint32_t __attribute__((ext_vector_type(4)));
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int bt = 0; bt < NB; ++bt)
+        for (int q = 0; q < N - 1; ++q) {
+            words w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(S[bt][j]));
-        e = exponent_for(wave_largest(top));
-        down = ldexpf(1.0f, -e);
+            for (int i = 0; i < 8; i += 2) {
+                if constexpr (NARROW<T>) {
+                    const auto both = __builtin_amdgcn_cvt_pkrtz(x[i], x[i + 1]);
+                    w[i / 2] = __builtin_bit_cast(uint32_t, both);
+                    x[i] = fmaf((float)both[0], -1.0f, x[i]);
+                    x[i + 1] = fmaf((float)both[1], -1.0f, x[i + 1]);
+                } else {
+                    w[i / 2] = __builtin_amdgcn_perm(__float_as_uint(x[i + 1]), __float_as_uint(x[i]), 0x07060302);     // their upper halves
+                    x[i] -= __uint_as_float(__float_as_uint(x[i]) & 0xFFFF0000u);
+                    x[i + 1] -= __uint_as_float(__float_as_uint(x[i + 1]) & 0xFFFF0000u);
+                }
+            }
+            part[q] = __builtin_bit_cast(operand<T>, w);
+        }
     }
 #pragma unroll
-    for (int kb = 0; kb < NB / 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[kb][i] = (T)(NARROW<T> ? S[2 * kb + i / 4][i % 4] * down : S[2 * kb + i / 4][i % 4]);
-    return e;
+    for (int i = 0; i < 8; ++i) part[N - 1][i] = (T)x[i];
 }
 
-// A piece of P, rows 16 it by rows 32 kb of b, transposed: a lane has eight entries of a row.
-template <typename T, int W>
-__device__ __forceinline__ void make_piece(tile<T, W> &a, const tile<T, W> &b, tile<T, CHUNK> &to, powers &w, int which, int it, int kb, float tile_on, int along_a, int along_p,
-                                           int spread_b)
+// The exponent that is taken off a memory that becomes operands (float16; otherwise none is), and its operands 32 kb.
+template <typename T, int NB> __device__ __forceinline__ int exponent_of(const floats (&S)[NB])
+{
+    if (!NARROW<T>) return 0;
+    float top = 0.0f;
+#pragma unroll
+    for (int bt = 0; bt < NB; ++bt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(S[bt][j]));
+    return exponent_for(wave_largest(top));
+}
+template <typename T, int NB> __device__ __forceinline__ void as_operands(const floats (&S)[NB], int kb, float down, operand<T> (&to)[PARTS<T>])
+{
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = NARROW<T> ? S[2 * kb + i / 4][i % 4] * down : S[2 * kb + i / 4][i % 4];
+    in_parts<T>(x, to);
+}
+
+// The pieces of P that are not zero, rows 16 it by rows 32 kb of b with kb <= it / 2, in shared memory as the operands that their lanes hold: slots of 16 bytes, one
+// lane's next to another's.
+template <typename T> struct pieces_of {
+    using slot = uint32_t __attribute__((ext_vector_type(4)));
+    static constexpr int SLOTS = sizeof(operand<T>) / 16;
+    struct parts {
+        slot x[SLOTS];
+    };
+    slot x[6][PARTS<T>][SLOTS][64];
+    __device__ static constexpr int number(int it, int kb) { return it + it / 3 + kb; }
+    __device__ __forceinline__ void put(int it, int kb, int q, operand<T> o)
+    {
+        const parts p = __builtin_bit_cast(parts, o);
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) x[number(it, kb)][q][i][threadIdx.x & 63] = p.x[i];
+    }
+    // those of rows 16 it
+    __device__ __forceinline__ void get(operand<T> (&to)[2][PARTS<T>], int it) const
+    {
+#pragma unroll
+        for (int kb = 0; kb <= it / 2; ++kb)
+#pragma unroll
+            for (int q = 0; q < PARTS<T>; ++q) {
+                parts p;
+#pragma unroll
+                for (int i = 0; i < SLOTS; ++i) p.x[i] = x[number(it, kb)][q][i][threadIdx.x & 63];
+                to[kb][q] = __builtin_bit_cast(operand<T>, p);
+            }
+    }
+};
+
+// A piece of P, transposed: a lane has eight entries of a row.
+template <bool EARLY, typename T, int W>
+__device__ __forceinline__ void make_piece(tile<T, W> &a, const tile<T, W> &b, pieces_of<T> &to, powers &w, int which, int it, int kb, float tile_on, int along_a, int spread_b)
 {
     const int lane = threadIdx.x & 63, before = it - 2 * kb;
     floats P[2] = {(floats)0.0f, (floats)0.0f};
+    operand<T> x[2], y[2][2];
+    const auto read = [&](int q) {
+        x[q & 1] = a.along(along_a, it, q);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) y[q & 1][half] = b.spread(spread_b, kb, half, q);
+    };
+    read(0);
 #pragma unroll
     for (int q = 0; q < W / 32; ++q) {
-        const operand<T> x = a.along(along_a, it, q);
+        if (q + 1 < W / 32) read(q + 1);
+        reads_before_products<EARLY>();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) P[half] = product(b.spread(spread_b, kb, half, q), x, P[half]);
+        for (int half = 0; half < 2; ++half) P[half] = product(y[q & 1][half], x[q & 1], P[half]);
+        reads_before_products<EARLY>();
     }
     if constexpr (sizeof(T) == 4) settle(P);
     const float far = before == 3 ? tile_on : 1.0f;  // 48 rows before: l^16 more than 32
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const floats x = w.p[min(before, 2)][half][lane];
+        const floats l = w.p[min(before, 2)][half][lane];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) P[half][j] *= x[j] * far;
+        for (int j = 0; j < 4; ++j) P[half][j] *= l[j] * far;
     }
     float down = 1.0f;
     if constexpr (NARROW<T>) {
@@ -407,17 +486,20 @@ __device__ __forceinline__ void make_piece(tile<T, W> &a, const tile<T, W> &b, t
         down = ldexpf(1.0f, -e);
         if (lane == 0) w.exponent[which][it][kb] = e;
     }
-    operand<T> x;
+    float z[8];
+    operand<T> part[PARTS<T>];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (T)(NARROW<T> ? P[i / 4][i % 4] * down : P[i / 4][i % 4]);
-    to.along(along_p, it, kb) = x;
+    for (int i = 0; i < 8; ++i) z[i] = NARROW<T> ? P[i / 4][i % 4] * down : P[i / 4][i % 4];
+    in_parts<T>(z, part);
+#pragma unroll
+    for (int q = 0; q < PARTS<T>; ++q) to.put(it, kb, q, part[q]);
 }
 
 // The six pieces of P that are not zero, shared out among the waves.
-template <int WAVES, typename T, int W, typename L>
-__device__ __forceinline__ void make_pieces(tile<T, W> &a, const tile<T, W> &b, tile<T, CHUNK> &to, powers &w, int which, float tile_on, int along_a, int spread_b, const L &l, int wave)
+template <bool EARLY, int WAVES, typename T, int W>
+__device__ __forceinline__ void make_pieces(tile<T, W> &a, const tile<T, W> &b, pieces_of<T> &to, powers &w, int which, float tile_on, int along_a, int spread_b, int wave)
 {
-    const auto piece = [&](int it, int kb) { make_piece(a, b, to, w, which, it, kb, tile_on, along_a, l.along_p, spread_b); };
+    const auto piece = [&](int it, int kb) { make_piece<EARLY>(a, b, to, w, which, it, kb, tile_on, along_a, spread_b); };
     if constexpr (WAVES == 4) {
         piece(wave < 2 ? 3 : 2, wave & 1);
         if (wave >= 2) piece(wave - 2, 0);
@@ -452,17 +534,10 @@ template <typename T, int W, int NB> __device__ __forceinline__ void remember(fl
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[t][i] *= down;
     }
-    constexpr int PARTS = sizeof(T) == 4 ? 1 : NARROW<T> ? 2 : 3;
-    operand<T> part[PARTS][2];
+    constexpr int KEPT = sizeof(T) == 4 ? 1 : NARROW<T> ? 2 : 3;
+    operand<T> part[2][KEPT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q) {
-                part[q][t][i] = (T)w[t][i];
-                w[t][i] -= (float)part[q][t][i];
-            }
+    for (int t = 0; t < 2; ++t) in_parts<T>(w[t], part[t]);
 #pragma unroll
     for (int bt = 0; bt < NB; ++bt) {
         const operand<T> b0 = b.across_spread(across_b, 0, bt / 2, bt % 2), b1 = b.across_spread(across_b, 1, bt / 2, bt % 2);
@@ -471,9 +546,9 @@ template <typename T, int W, int NB> __device__ __forceinline__ void remember(fl
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] *= keep;
 #pragma unroll
-        for (int q = PARTS - 1; q >= 0; --q) {
-            x = product(b0, part[q][0], x);
-            x = product(b1, part[q][1], x);
+        for (int q = KEPT - 1; q >= 0; --q) {
+            x = product(b0, part[0][q], x);
+            x = product(b1, part[1][q], x);
         }
         if constexpr (NARROW<T>) {
             const float up = ldexpf(1.0f, e);
@@ -485,30 +560,60 @@ template <typename T, int W, int NB> __device__ __forceinline__ void remember(fl
     if constexpr (sizeof(T) == 4) settle(S);
 }
 
-// Rows 16 it of the results, a wave's 16 columns, transposed: a lane has four entries of a row.  o: what the memory before the chunk gives them (`weight`: the power of l
-// that is missing there) ...
-template <typename T, int W, int KB> __device__ __forceinline__ floats from_memory(tile<T, W> &a, const operand<T> (&s)[KB], int it, float weight, int along_a)
+// Results, a wave's 16 columns, transposed: o[it] are rows 16 it, a lane has four entries of a row.  What the memory before the chunk gives them (`weight`: the power of l
+// that is missing in the first 16 rows, `tile_on` what is in the next) ...
+template <bool EARLY, typename T, int W, typename Part>
+__device__ __forceinline__ void from_operands(floats (&o)[4], tile<T, W> &a, Part &&part, float weight, float tile_on, int along_a)
 {
-    floats o = (floats)0.0f;
+    operand<T> s[2][PARTS<T>], x[2][4];
+    const auto read = [&](int kb) {
+        part(kb, s[kb & 1]);
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) o = product(s[kb], a.along(along_a, it, kb), o);
+        for (int it = 0; it < 4; ++it) x[kb & 1][it] = a.along(along_a, it, kb);
+    };
+#pragma unroll
+    for (int it = 0; it < 4; ++it) o[it] = (floats)0.0f;
+    read(0);
+#pragma unroll
+    for (int kb = 0; kb < W / 32; ++kb) {
+        if (kb + 1 < W / 32) read(kb + 1);
+        reads_before_products<EARLY>();
+#pragma unroll
+        for (int q = PARTS<T> - 1; q >= 0; --q)
+#pragma unroll
+            for (int it = 0; it < 4; ++it) o[it] = product(s[kb & 1][q], x[kb & 1][it], o[it]);
+        reads_before_products<EARLY>();
+    }
     if constexpr (sizeof(T) == 4) settle(o);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] *= weight;
-    return o;
+    for (int it = 0; it < 4; ++it) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[it][j] *= weight;
+        weight *= tile_on;
+    }
+}
+template <bool EARLY, typename T, int W, int NB>
+__device__ __forceinline__ void from_memory(floats (&o)[4], tile<T, W> &a, const floats (&S)[NB], float weight, float tile_on, int along_a)
+{
+    const int e = exponent_of<T>(S);
+    const float down = NARROW<T> ? ldexpf(1.0f, -e) : 1.0f;
+    from_operands<EARLY>(o, a, [&](int kb, operand<T> (&to)[PARTS<T>]) { as_operands<T>(S, kb, down, to); }, NARROW<T> ? ldexpf(weight, e) : weight, tile_on, along_a);
 }
 // ... and what the rows of the chunk add.
-template <typename T> __device__ __forceinline__ void from_rows(floats &o, const operand<T> (&c)[2], tile<T, CHUNK> &P, const powers &w, int which, int it, int along_p)
+template <typename T>
+__device__ __forceinline__ void from_rows(floats &o, const operand<T> (&c)[2], const operand<T> (&P)[2][PARTS<T>], const powers &w, int which, int it)
 {
 #pragma unroll
     for (int kb = 0; kb <= it / 2; ++kb) {
+        floats more = NARROW<T> ? (floats)0.0f : o;
+#pragma unroll
+        for (int q = PARTS<T> - 1; q >= 0; --q) more = product(c[kb], P[kb][q], more);
         if constexpr (NARROW<T>) {
-            const floats more = product(c[kb], P.along(along_p, it, kb), (floats)0.0f);
             const float up = ldexpf(1.0f, w.exponent[which][it][kb]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = fmaf(more[j], up, o[j]);
         } else {
-            o = product(c[kb], P.along(along_p, it, kb), o);
+            o = more;
         }
     }
     if constexpr (sizeof(T) == 4) settle(o);
@@ -773,12 +878,12 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
         p.wb = WB;
         p.wc = WC;
     }
-    constexpr int WAVES = WC / 16, THREADS = 4 * WC;
+    constexpr int WAVES = WC / 16, THREADS = 4 * WC, DEEP = NARROW<T> && WB == 128 && WC == 64 && HEADS == ONE ? 1 : 2;       // steps on their way
     // Results go through shared memory, and from there while the next step's tiles come, so that rows are written in packs; in 32 bits a lane has a pack
     constexpr bool THROUGH = sizeof(T) == 2;
     __shared__ tile<T, WB> sa, sb;
     __shared__ tile<T, WC> sc;
-    __shared__ tile<T, CHUNK> sp;
+    __shared__ pieces_of<T> sp;
     __shared__ tile<T, THROUGH ? WC : 16> so;
     __shared__ powers w;
     const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
@@ -804,13 +909,19 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
     const int heads = HEADS == MANY_B ? p.ks : HEADS == MANY_A ? p.qs : 1;
     const auto head_a = [&](int h) { return HEADS == MANY_A ? state * heads + h : state; };
     const auto head_b = [&](int h) { return HEADS == MANY_B ? state * heads + h : state; };
-    // Two steps are on their way, as one alone would leave too little of the memory's rate in use.  (What is asked for in every step comes last: what is waited for
+    // Two steps are on their way, as one alone would leave too little of the memory's rate in use (float16, 128 x 64, has no registers for two: 64000 rows, 8 heads, 172 us
+    // with two, 112 with one).  (What is asked for in every step comes last: what is waited for
     // is counted from there, whether there were others or not.)
     struct tiles {
         incoming<T, WB, THREADS> a, b;
         incoming<T, WC, THREADS> c;
-    } coming[2];
-    floats O[HEADS == MANY_B ? 4 : 1];
+    } coming[DEEP];
+    // Several heads of queries read one memory: it becomes operands for the first of them, which the others find in shared memory, a wave its own (131072 rows, 8 heads of 64 on
+    // 2 memories, bf16: 127 us made for every head, 119 so).  In 128 x 64 two workgroups of a compute unit would not have the room.
+    constexpr bool HELD = HEADS == MANY_A && AHEAD<T, WB, WC>;
+    __shared__ operand<T> held[HELD ? WAVES : 1][WB / 32][PARTS<T>][64];
+    int exponent = 0;
+    floats O[4];
     float seen = 0.0f;
     T *ready = nullptr;                              // where the rows in `so` go, and how many there are
     int ready_rows = 0;
@@ -818,7 +929,7 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
         if constexpr (THROUGH)
             if (ready) write_rows<T, WC, THREADS>(so, l.pack_c, ready, step * p.out.stride, ready_rows, p.wc);
     };
-    go_through<2, HEADS == ONE>(at, heads, step, coming,
+    go_through<DEEP, HEADS == ONE>(at, heads, step, coming,
         [&](tiles &to, int64_t base, int h) {
             const auto ask_a = [&] { to.a.load(p.a.at(base, head_a(h)), step * p.a.stride, p.wb); };
             const auto ask_b = [&] {
@@ -851,20 +962,42 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
             next();
             const bool enter = HEADS != MANY_B || h == 0, leave = HEADS != MANY_B || h == heads - 1;
             const operand<T> c[2] = {sc.across(l.across_c, 0, wave), sc.across(l.across_c, 1, wave)};
-            operand<T> s[WB / 32];
-            const int e = enter ? as_operands<T>(S, s) : 0;
-            make_pieces<WAVES>(sa, sb, sp, w, 0, tile_on, l.along_a, l.spread_b, l, wave);
+            if constexpr (HELD) {
+                const int lane = threadIdx.x & 63;
+                if (h == 0) {
+                    exponent = exponent_of<T>(S);
+                    const float down = NARROW<T> ? ldexpf(1.0f, -exponent) : 1.0f;
+#pragma unroll
+                    for (int kb = 0; kb < WB / 32; ++kb) {
+                        operand<T> s[PARTS<T>];
+                        as_operands<T>(S, kb, down, s);
+#pragma unroll
+                        for (int q = 0; q < PARTS<T>; ++q) held[wave][kb][q][lane] = s[q];
+                    }
+                }
+                from_operands<AHEAD<T, WB, WC>>(
+                    O, sa,
+                    [&](int kb, operand<T> (&to)[PARTS<T>]) {
+#pragma unroll
+                        for (int q = 0; q < PARTS<T>; ++q) to[q] = held[wave][kb][q][lane];
+                    },
+                    NARROW<T> ? ldexpf(weight_in, exponent) : weight_in, tile_on, l.along_a);
+            } else if (enter && p.out.data) {
+                from_memory<AHEAD<T, WB, WC>>(O, sa, S, weight_in, tile_on, l.along_a);
+            }
+            make_pieces<AHEAD<T, WB, WC>, WAVES>(sa, sb, sp, w, 0, tile_on, l.along_a, l.spread_b, wave);
             if (HEADS == MANY_B || h == heads - 1) remember(S, sb, c, w, HEADS == MANY_B && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n), l.across_b);
             __syncthreads();
             if (!p.out.data) return;
             T *const out = p.out.at(base, head_a(h));
-            float weight = NARROW<T> ? ldexpf(weight_in, e) : weight_in;
+            operand<T> P[2][2][PARTS<T>];
+            sp.get(P[0], 0);
 #pragma unroll
             for (int it = 0; it < 4; ++it) {
-                floats &o = O[HEADS == MANY_B ? it : 0];
-                if (enter) o = from_memory(sa, s, it, weight, l.along_a);
-                weight *= tile_on;
-                from_rows(o, c, sp, w, 0, it, l.along_p);
+                floats &o = O[it];
+                if (it < 3) sp.get(P[(it + 1) & 1], it + 1);
+                reads_before_products<AHEAD<T, WB, WC>>();
+                from_rows(o, c, P[it & 1], w, 0, it);
                 if constexpr (HEADS == MANY_B) settle(o);
                 if (!leave) continue;
                 look_at(seen, o);
@@ -901,7 +1034,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     if constexpr (WHOLE) p.wb = p.wc = q.wb = q.wc = W;
     constexpr int WAVES = W / 16, THREADS = 4 * W;
     __shared__ tile<T, W> sk, sv, sq, sd, so[2];
-    __shared__ tile<T, CHUNK> sp[2];
+    __shared__ pieces_of<T> sp[2];
     __shared__ powers w;
     const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
     if ((int64_t)blockIdx.x >= all) {
@@ -931,7 +1064,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     struct tiles {
         incoming<T, W, THREADS> k, v, q, d;
     } coming[1];
-    floats O[2][MANY ? 4 : 1];
+    floats O[2][4];
     float seen[2] = {0.0f, 0.0f};
     T *ready[2] = {nullptr, nullptr};
     int ready_rows = 0;
@@ -969,33 +1102,32 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
             const bool enter = !MANY || h == 0, leave = !MANY || h == heads - 1;
             const float keep = MANY && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n);
             const operand<T> d[2] = {sd.across(l.across_c, 0, wave), sd.across(l.across_c, 1, wave)}, c[2] = {sq.across(l.across_c, 0, wave), sq.across(l.across_c, 1, wave)};
-            operand<T> s[W / 32], t[W / 32];
-            int e = 0, f = 0;
             if (enter) {
-                e = as_operands<T>(R, s);
-                f = as_operands<T>(Rt, t);
+                from_memory<AHEAD<T, W, W>>(O[0], sk, R, weight_in, tile_on, l.along_a);
+                from_memory<AHEAD<T, W, W>>(O[1], sv, Rt, weight_in, tile_on, l.along_a);
             }
-            make_pieces<WAVES>(sk, sq, sp[0], w, 0, tile_on, l.along_a, l.spread_b, l, wave);
-            make_pieces<WAVES>(sv, sd, sp[1], w, 1, tile_on, l.along_a, l.spread_b, l, WAVES - 1 - wave);
+            make_pieces<AHEAD<T, W, W>, WAVES>(sk, sq, sp[0], w, 0, tile_on, l.along_a, l.spread_b, wave);
+            make_pieces<AHEAD<T, W, W>, WAVES>(sv, sd, sp[1], w, 1, tile_on, l.along_a, l.spread_b, WAVES - 1 - wave);
             remember(R, sq, d, w, keep, l.across_b);
             remember(Rt, sd, c, w, keep, l.across_b);
             __syncthreads();
-            const auto results = [&](tile<T, W> &a, const operand<T> (&memory)[W / 32], int exponent, const operand<T> (&x)[2], int which) {
-                float weight = NARROW<T> ? ldexpf(weight_in, exponent) : weight_in;
+            const auto results = [&](const operand<T> (&x)[2], int which) {
+                operand<T> P[2][2][PARTS<T>];
+                sp[which].get(P[0], 0);
 #pragma unroll
                 for (int it = 0; it < 4; ++it) {
-                    floats &o = O[which][MANY ? it : 0];
-                    if (enter) o = from_memory(a, memory, it, weight, l.along_a);
-                    weight *= tile_on;
-                    from_rows(o, x, sp[which], w, which, it, l.along_p);
+                    floats &o = O[which][it];
+                    if (it < 3) sp[which].get(P[(it + 1) & 1], it + 1);
+                    reads_before_products<AHEAD<T, W, W>>();
+                    from_rows(o, x, P[it & 1], w, which, it);
                     if constexpr (MANY) settle(o);
                     if (!leave) continue;
                     look_at(seen[which], o);
                     so[which].entries(l.entries_o, it, wave) = rounded<T>(o, 1.0f);
                 }
             };
-            results(sk, s, e, d, 0);
-            results(sv, t, f, c, 1);
+            results(d, 0);
+            results(c, 1);
             ready[0] = leave ? p.out.at(base, state) : nullptr;
             ready[1] = leave ? q.out.at(base, state) : nullptr;
             ready_rows = n;
