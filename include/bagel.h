@@ -559,7 +559,7 @@ typedef struct {
     int64_t workspace_bytes;
 } bagel_attention;
 
-int64_t bagel_linear_attention_workspace(const bagel_attention *args, int32_t grad);    /* sizes alone are looked at; grad: whether for the gradient */
+int64_t bagel_linear_attention_workspace(const bagel_attention *args, int32_t grad);    /* sizes alone are looked at, of rows, heads and sequences: enough for every type; grad: whether for the gradient */
 int bagel_linear_attention(const bagel_attention *args, void *hip_stream);
 int bagel_linear_attention_grad(const bagel_attention *args, void *hip_stream);
 int bagel_linear_attention_step(const bagel_attention *args, void *hip_stream);

@@ -6,6 +6,8 @@
 //   R_t = c q_t do_t^T + l R_{t+1},   dq_t = c S_t do_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dS_0 = l R_1
 // So every gradient is a linear attention of its own: dq that of do, v, k with the memory S^T; dv that of k, q, do and dk that of v, do, q from the
 // last row to the first, with the memories R and R^T.
+#include <algorithm>
+
 #include "linear_attention.h"
 
 namespace {
@@ -377,8 +379,15 @@ const char *check_attention(const bagel_attention *b, bool grad)
 extern "C" int64_t bagel_linear_attention_workspace(const bagel_attention *b, int32_t grad)
 {
     if (check_sizes(b)) return BAGEL_EINVAL;
-    const int64_t with = memories_floats(*b, segments_of(*b, true)), without = memories_floats(*b, segments_of(*b, false));      // (which it is may not be known yet)
-    return (with > without ? with : without) * (grad ? 2 : 1) * (int64_t)sizeof(float);
+    // with offsets or without, in 32 bits or 16: which it is may not be known yet
+    int64_t most = 0;
+    for (int32_t dtype : {BAGEL_FLOAT32, BAGEL_BFLOAT16})
+        for (bool offsets : {false, true}) {
+            bagel_attention a = *b;
+            a.dtype = dtype;
+            most = std::max(most, memories_floats(a, segments_of(a, offsets)));
+        }
+    return most * (grad ? 2 : 1) * (int64_t)sizeof(float);
 }
 
 extern "C" int bagel_linear_attention(const bagel_attention *b, void *hip_stream)
