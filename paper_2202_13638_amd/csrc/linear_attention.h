@@ -2,6 +2,8 @@
 // each type on its own).  Nothing here is part of the public ABI (see include/bagel.h).
 #pragma once
 
+#include <algorithm>
+
 #include "activations.h"
 
 template <typename T> struct bagel_heads_of {
@@ -34,7 +36,20 @@ template <typename T> struct bagel_attention_pass {
     int64_t further;                                 // numbers of segments that are not the first of their sequence
     bool join;                                       // whether a segment joins what those before it have added, which then no launch has done
     float *memories;                                 // [sequences + further][states][..]: behind every segment but the last; null: one segment to a sequence
+    int64_t groups, launched;                        // workgroups of all launches, and of those before this one
 };
+
+// A grid has fewer than 2^32 threads, and a workgroup up to 512: more workgroups than these go by several launches, each `kernel(workgroups, those before)`.
+constexpr int64_t BAGEL_ATTENTION_GROUPS = 1 << 22;
+template <typename F> hipError_t bagel_attention_launches(int64_t groups, F &&kernel)
+{
+    hipError_t e = hipSuccess;
+    for (int64_t from = 0; from < groups && e == hipSuccess; from += BAGEL_ATTENTION_GROUPS) {
+        kernel((unsigned)std::min(groups - from, BAGEL_ATTENTION_GROUPS), from);
+        e = hipGetLastError();
+    }
+    return e;
+}
 
 // The memories behind all segments but the last of their sequences, of one pass or two (with as many sequences, rows, states and segments).
 template <typename T> hipError_t bagel_launch_attention_memories(const bagel_attention_pass<T> *p, int n, hipStream_t stream);

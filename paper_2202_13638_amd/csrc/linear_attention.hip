@@ -6,8 +6,6 @@
 //   R_t = c q_t do_t^T + l R_{t+1},   dq_t = c S_t do_t,   dk_t = R_t v_t,   dv_t = R_t^T k_t,   dS_0 = l R_1
 // So every gradient is a linear attention of its own: dq that of do, v, k with the memory S^T; dv that of k, q, do and dk that of v, do, q from the
 // last row to the first, with the memories R and R^T.
-#include <algorithm>
-
 #include "linear_attention.h"
 
 namespace {
@@ -17,9 +15,9 @@ template <typename T> __global__ __launch_bounds__(256) void rows_kernel(bagel_a
 {
     constexpr int MOST = BAGEL_ATTENTION_MAX_WIDTH;
     __shared__ float sa[MOST], sb[MOST], sc[MOST], part[MOST];
-    const int64_t work = (int64_t)p.sequences * p.states;
-    if ((int64_t)blockIdx.x >= work) return bagel_clear_behind(p, blockIdx.x - work, gridDim.x - work);
-    const int state = blockIdx.x % p.states, sequence = blockIdx.x / p.states, t = threadIdx.x, column = t & 127, half = t >> 7;
+    const int64_t work = (int64_t)p.sequences * p.states, group = p.launched + blockIdx.x;
+    if (group >= work) return bagel_clear_behind(p, group - work, p.groups - work);
+    const int state = (int)(group % p.states), sequence = (int)(group / p.states), t = threadIdx.x, column = t & 127, half = t >> 7;
     int64_t begin = (int64_t)sequence * p.each, end = begin + p.each;
     if (p.offsets) {
         begin = min(max((int64_t)p.offsets[sequence], (int64_t)0), p.rows);
@@ -210,9 +208,12 @@ template <typename T> hipError_t launch_pass(const bagel_attention_pass<T> &p, c
 {
     if (!by_rows<T>(b)) return bagel_launch_attention_pass(p, stream);
     const int64_t work = (int64_t)p.sequences * p.states, clear = p.offsets && p.out.data && p.rows > 0 ? 32 : 0;
-    if (work + clear == 0) return hipSuccess;
-    rows_kernel<T><<<(unsigned)(work + clear), 256, 0, stream>>>(p);
-    return hipGetLastError();
+    bagel_attention_pass<T> a = p;
+    a.groups = work + clear;
+    return bagel_attention_launches(a.groups, [&](unsigned groups, int64_t before) {
+        a.launched = before;
+        rows_kernel<T><<<groups, 256, 0, stream>>>(a);
+    });
 }
 
 // S along the rows, and R from the last row to the first.

@@ -669,7 +669,7 @@ template <typename T, int NB> __device__ __forceinline__ void again(int which)
     uint64_t arguments = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(arguments));
     const bagel_attention_pass<T> p = ((const bagel_attention_pass<T> *)arguments)[which];
-    const int64_t first = (int64_t)p.sequences * p.states, work = by_dies(blockIdx.x, first, first + p.further * p.states), number = work / p.states;
+    const int64_t first = (int64_t)p.sequences * p.states, work = by_dies(p.launched + blockIdx.x, first, first + p.further * p.states), number = work / p.states;
     const int state = (int)(work - number * p.states), column = afresh(threadIdx.x >> 6) * 16 + (threadIdx.x & 15);
     const place at = place_of(p, number);
     const int step = p.back ? -1 : 1, g = (threadIdx.x & 63) >> 4;
@@ -793,7 +793,7 @@ template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch
     __shared__ tile<T, WB> sb;
     __shared__ tile<T, WC> sc;
     __shared__ powers w;
-    const int64_t work = by_dies(blockIdx.x, 0, p.further * p.states), further = work / p.states;
+    const int64_t work = by_dies(p.launched + blockIdx.x, 0, p.further * p.states), further = work / p.states;
     const int state = (int)(work - further * p.states);
     const place behind_it = place_of(p, p.sequences + further);
     if (!behind_it.there) return;
@@ -886,9 +886,9 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
     __shared__ pieces_of<T> sp;
     __shared__ tile<T, THROUGH ? WC : 16> so;
     __shared__ powers w;
-    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
-    if ((int64_t)blockIdx.x >= all) return bagel_clear_behind(p, blockIdx.x - all, gridDim.x - all);
-    const int64_t work = by_dies(blockIdx.x, first, all), number = work / p.states;
+    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states, group = p.launched + blockIdx.x;
+    if (group >= all) return bagel_clear_behind(p, group - all, p.groups - all);
+    const int64_t work = by_dies(group, first, all), number = work / p.states;
     const int state = (int)(work - number * p.states);
     const place at = place_of(p, number);
     if (!at.there) return;
@@ -1036,12 +1036,12 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     __shared__ tile<T, W> sk, sv, sq, sd, so[2];
     __shared__ pieces_of<T> sp[2];
     __shared__ powers w;
-    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states;
-    if ((int64_t)blockIdx.x >= all) {
-        bagel_clear_behind(p, blockIdx.x - all, gridDim.x - all);
-        return bagel_clear_behind(q, blockIdx.x - all, gridDim.x - all);
+    const int64_t first = (int64_t)p.sequences * p.states, all = first + p.further * p.states, group = p.launched + blockIdx.x;
+    if (group >= all) {
+        bagel_clear_behind(p, group - all, p.groups - all);
+        return bagel_clear_behind(q, group - all, p.groups - all);
     }
-    const int64_t work = by_dies(blockIdx.x, first, all), number = work / p.states;
+    const int64_t work = by_dies(group, first, all), number = work / p.states;
     const int state = (int)(work - number * p.states);
     const place at = place_of(p, number);
     if (!at.there) return;
@@ -1153,9 +1153,9 @@ template <typename T, typename F> void by_widths(const bagel_attention_pass<T> &
     else p.wc <= 64 ? filled(wide, narrow) : filled(wide, wide);
 }
 
-template <typename T> unsigned groups_of(const bagel_attention_pass<T> &p)
+template <typename T> int64_t groups_of(const bagel_attention_pass<T> &p)
 {
-    return (unsigned)((p.sequences + p.further) * p.states + (p.offsets && p.out.data && p.rows > 0 ? 32 : 0));
+    return (p.sequences + p.further) * p.states + (p.offsets && p.out.data && p.rows > 0 ? 32 : 0);
 }
 
 }  // namespace
@@ -1166,15 +1166,19 @@ template <typename T> hipError_t bagel_launch_attention_memories(const bagel_att
     both.p[0] = passes[0];
     both.p[1] = passes[n - 1];
     const bagel_attention_pass<T> &p = both.p[0];
-    const unsigned work = (unsigned)(p.further * p.states);
+    const int64_t work = p.further * p.states;
     if (work == 0) return hipSuccess;
+    hipError_t e = hipSuccess;
     const bool many = p.ks > 1 || both.p[1].ks > 1;
     by_widths(p, [&](auto wb, auto wc, auto whole) {
         constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value;
-        if (many) sums_kernel<T, WB, WC, decltype(whole)::value, true><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
-        else sums_kernel<T, WB, WC, decltype(whole)::value, false><<<dim3(work, n), 4 * WC, 0, stream>>>(both);
+        e = bagel_attention_launches(work, [&](unsigned groups, int64_t before) {
+            both.p[0].launched = both.p[1].launched = before;
+            if (many) sums_kernel<T, WB, WC, decltype(whole)::value, true><<<dim3(groups, n), 4 * WC, 0, stream>>>(both);
+            else sums_kernel<T, WB, WC, decltype(whole)::value, false><<<dim3(groups, n), 4 * WC, 0, stream>>>(both);
+        });
     });
-    if (p.join) return hipGetLastError();
+    if (p.join || e != hipSuccess) return e;
     // some workgroups to a memory where there are few of them
     const int64_t all = (int64_t)p.sequences * p.states, most = (p.wb * p.wc + 255) / 256, wanted = 1024 / all;
     const int blocks = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
@@ -1182,34 +1186,42 @@ template <typename T> hipError_t bagel_launch_attention_memories(const bagel_att
     return hipGetLastError();
 }
 
-template <typename T> hipError_t bagel_launch_attention_pass(const bagel_attention_pass<T> &p, hipStream_t stream)
+template <typename T> hipError_t bagel_launch_attention_pass(const bagel_attention_pass<T> &pass, hipStream_t stream)
 {
-    const unsigned groups = groups_of(p);
-    if (groups == 0) return hipSuccess;
+    bagel_attention_pass<T> p = pass;
+    p.groups = groups_of(p);
+    hipError_t e = hipSuccess;
     by_widths(p, [&](auto wb, auto wc, auto whole) {
         constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value, ON_SIMD = sizeof(T) == 4 && WB == 128 && WC == 64 ? 1 : 2;
         constexpr bool WHOLE = decltype(whole)::value;
-        if (p.ks > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_B, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
-        else if (p.qs > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_A, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
-        else chunks_kernel<T, WB, WC, WHOLE, ONE, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+        e = bagel_attention_launches(p.groups, [&](unsigned groups, int64_t before) {
+            p.launched = before;
+            if (p.ks > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_B, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+            else if (p.qs > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_A, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+            else chunks_kernel<T, WB, WC, WHOLE, ONE, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+        });
     });
-    return hipGetLastError();
+    return e;
 }
 
-template <typename T> hipError_t bagel_launch_attention_keys(const bagel_attention_pass<T> &p, const bagel_attention_pass<T> &q, hipStream_t stream)
+template <typename T> hipError_t bagel_launch_attention_keys(const bagel_attention_pass<T> &values, const bagel_attention_pass<T> &keys, hipStream_t stream)
 {
-    const unsigned groups = groups_of(p);
-    if (groups == 0) return hipSuccess;
+    bagel_attention_pass<T> p = values, q = keys;
+    p.groups = q.groups = groups_of(p);
+    hipError_t e = hipSuccess;
     const auto launch = [&](auto w, auto whole) {
         constexpr int W = decltype(w)::value;
         constexpr bool WHOLE = decltype(whole)::value;
-        if constexpr (W == 64)
-            if (p.ks > 1) return keys_kernel<T, W, WHOLE, true><<<groups, 4 * W, 0, stream>>>(p, q);
-        keys_kernel<T, W, WHOLE, false><<<groups, 4 * W, 0, stream>>>(p, q);
+        e = bagel_attention_launches(p.groups, [&](unsigned groups, int64_t before) {
+            p.launched = q.launched = before;
+            if constexpr (W == 64)
+                if (p.ks > 1) return keys_kernel<T, W, WHOLE, true><<<groups, 4 * W, 0, stream>>>(p, q);
+            keys_kernel<T, W, WHOLE, false><<<groups, 4 * W, 0, stream>>>(p, q);
+        });
     };
     const std::integral_constant<int, 64> narrow;
     const std::integral_constant<int, 128> wide;
     if (p.wb <= 64) p.wb == 64 && p.wc == 64 ? launch(narrow, std::true_type()) : launch(narrow, std::false_type());
     else p.wb == 128 && p.wc == 128 ? launch(wide, std::true_type()) : launch(wide, std::false_type());
-    return hipGetLastError();
+    return e;
 }

@@ -28,3 +28,31 @@ def test_work_spaces_are_for_every_type(heads, states):
             lib = binding.load()
             assert (lib.bagel_linear_attention_grad if grad else lib.bagel_linear_attention)(C.byref(a), None) == binding.EINVAL
             assert b"16 bytes" in lib.bagel_last_error(None), (rows, sequences, dtype, offsets, lib.bagel_last_error(None))
+
+
+@gpu
+@pytest.mark.parametrize("dk,dv,heads,states,offsets", [(8, 8, 1, 1, False), (8, 8, 2, 1, True), (8, 72, 1, 1, True), (2, 3, 1, 1, True)])
+def test_more_memories_than_a_grid_has_workgroups_for(dk, dv, heads, states, offsets):
+    """A grid has fewer than 2^32 threads: with workgroups of 256 (512 for values wider than 64), sequences of one row and an empty one at the end."""
+    n, t = (1 << (23 if dv > 64 else 24)) + 5, torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(1)
+
+    def whole(*shape):
+        return torch.randint(-4, 5, shape, generator=g, device="cuda", dtype=torch.int8).to(t)
+
+    q, k, v, d = whole(n, heads, dk), whole(n, states, dk), whole(n, states, dv), whole(n, heads, dv)
+    at = n
+    if offsets:                                      # two rows behind the last sequence, whose results are zero
+        at = torch.arange(n, device="cuda", dtype=torch.int32).clamp(max=n - 2)
+    ld = torch.tensor([-0.5], device="cuda")
+    out, dq, dk_, dv_ = (torch.full_like(x, 7.0) for x in (d, q, k, v))
+    binding.bagel_linear_attention(q, k, v, out, at, ld)
+    binding.bagel_linear_attention_grad(q, k, v, d, dq, dk_, dv_, at, ld)
+    last = n - 2 if offsets else n
+    for a in range(0, n, 1 << 22):                   # whole numbers, which 32 bits hold
+        b = min(a + (1 << 22), n)
+        x, y, z, e = (i[a:b].float() for i in (q, k, v, d))
+        qk, de = (x * y).sum(2, keepdim=True), (e * z).sum(2, keepdim=True)
+        for got, want in ((out, qk * z), (dq, de * y), (dk_, (de * x).sum(1, keepdim=True)), (dv_, (qk * e).sum(1, keepdim=True))):
+            want[max(last - a, 0):] = 0
+            assert torch.equal(got[a:b], want.to(t)), a
