@@ -215,7 +215,14 @@ template <bool WANTED> __device__ __forceinline__ void reads_before_products()
     if constexpr (WANTED) __builtin_amdgcn_sched_barrier(0x216);
 }
 
-// l^e for whole e >= 0; l2 = log2(l), finite
+// log2(l) of a memory, no less than what e times it can be said of; NaN stays NaN.
+template <typename T> __device__ __forceinline__ float log2_decay(const bagel_attention_pass<T> &p, int state)
+{
+    const float d = p.log_decay[state];
+    return (d < -1e30f ? -1e30f : d) * 1.44269504f;
+}
+
+// l^e for whole e >= 0; l2 = log2(l), not infinite
 __device__ __forceinline__ float power(float l2, int e) { return __builtin_amdgcn_exp2f(l2 * (float)e); }
 
 // The largest magnitude in a wave (NaN does not count).
@@ -636,7 +643,7 @@ __device__ __forceinline__ void look_at(float &seen, const floats &o)
 // What a segment's length leaves of the memory before it.
 template <typename T> __device__ __forceinline__ float kept(const bagel_attention_pass<T> &p, int state)
 {
-    return __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f * (float)p.segment);
+    return __builtin_amdgcn_exp2f(log2_decay(p, state) * (float)p.segment);
 }
 
 // The memory that a segment begins with: joined here, of what the segments before it have added, where that has not been done.
@@ -673,7 +680,7 @@ template <typename T, int NB> __device__ __forceinline__ void again(int which)
     const int state = (int)(work - number * p.states), column = afresh(threadIdx.x >> 6) * 16 + (threadIdx.x & 15);
     const place at = place_of(p, number);
     const int step = p.back ? -1 : 1, g = (threadIdx.x & 63) >> 4;
-    const float decay = __builtin_amdgcn_exp2f(fmaxf(p.log_decay[state], -1e30f) * 1.44269504f);
+    const float decay = __builtin_amdgcn_exp2f(log2_decay(p, state));
     const auto entry = [&](const T *row, int bt, int j) {
         const int r = memory_row<NB>(bt, j);
         return r < p.wb ? (float)row[r] : 0.0f;
@@ -802,7 +809,7 @@ template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch
     at.base = behind_it.base + (p.back ? p.segment : -p.segment);
     const bool first = behind_it.before < p.sequences;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = wave * 16 + (threadIdx.x & 15), step = p.back ? -1 : 1;
-    const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f, whole = power(l2, CHUNK);
+    const float l2 = log2_decay(p, state), whole = power(l2, CHUNK);
     floats S[WB / 16];
     const int64_t size = (int64_t)p.wb * p.wc;
     read_memory(S, first && p.first ? p.first + ((int64_t)at.sequence * p.states + state) * size : nullptr, p.step_b, p.step_c, column, p.wb, p.wc);
@@ -893,7 +900,7 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
     const place at = place_of(p, number);
     if (!at.there) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = (threadIdx.x & 63) >> 4, j16 = threadIdx.x & 15, column = wave * 16 + j16;
-    const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
+    const float l2 = log2_decay(p, state);
     const int step = p.back ? -1 : 1, behind = p.back ? 1 : 0;       // of powers of l
     floats S[WB / 16];
     read_before(S, p, at, state, column);
@@ -1046,7 +1053,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
     const place at = place_of(p, number);
     if (!at.there) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), column = wave * 16 + (threadIdx.x & 15);
-    const float l2 = fmaxf(p.log_decay[state], -1e30f) * 1.44269504f;
+    const float l2 = log2_decay(p, state);
     floats R[W / 16], Rt[W / 16];
     read_before(R, p, at, state, column);
     read_before(Rt, q, at, state, column);

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2202_13638_amd import binding
-from test_more_operators import _attention_struct
+from test_more_operators import HALF_ULP, TYPES, _attention_all, _attention_inputs, _attention_struct, _attention_want, _near
 
 gpu = pytest.mark.gpu
 
@@ -56,3 +56,26 @@ def test_more_memories_than_a_grid_has_workgroups_for(dk, dv, heads, states, off
         for got, want in ((out, qk * z), (dq, de * y), (dk_, (de * x).sum(1, keepdim=True)), (dv_, (qk * e).sum(1, keepdim=True))):
             want[max(last - a, 0):] = 0
             assert torch.equal(got[a:b], want.to(t)), a
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths", [[150, 0, 3], [700]], ids=["chunks", "shared out"])
+@pytest.mark.parametrize("heads,states,dk,dv", [(2, 2, 64, 64), (8, 2, 64, 40), (4, 2, 128, 128), (2, 2, 5, 3)])
+def test_a_decay_that_is_nan_is_seen(heads, states, dk, dv, lengths, dtype):
+    """In what it multiplies, and in nothing of the other memory: whole sequences, gradients and steps alike."""
+    t = TYPES[dtype]
+    x, _ = _attention_inputs(lengths, heads, states, dk, dv, t, seed=4)
+    ld = torch.tensor([-0.1, float("nan")])
+    want, _ = _attention_want(x, lengths, ld, 0.2)
+    _, terms = _attention_want(x, lengths, torch.full_like(ld, -0.1), 0.2)
+    got = _attention_all(x, lengths, ld, 0.2)
+    for k, g in got.items():
+        g, w = g.cpu(), want[k]
+        assert torch.equal(g.isnan(), w.isnan()), k
+        _near(torch.where(w.isnan(), torch.zeros_like(g), g), torch.nan_to_num(w), k, terms[k], 0.0 if dtype == "f32" else 2 * HALF_ULP[t])
+    state, out = x["initial"].cuda(), torch.zeros(len(lengths), heads, dv, dtype=t, device="cuda")
+    q, k, v = (x[i][:len(lengths)].cuda() for i in "qkv")
+    if len(q) == len(lengths):
+        binding.bagel_linear_attention_step(q, k, v, state, out, ld.cuda())
+        assert state[:, 1].isnan().all() and out[:, heads // 2:].isnan().all() and state[:, 0].isfinite().all() and out[:, :heads // 2].isfinite().all()
