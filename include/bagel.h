@@ -519,6 +519,7 @@ int bagel_layer_norm_grad(const bagel_norm *args, void *hip_stream);
  *   initial[sequences][states][key_width][value_width]  S before the first row, NULL: zero
  *   final_state of the same shape or NULL: S after the last row; of an empty sequence, its initial state.  Not in the place of `initial`, nor d_initial
  *     in that of d_final (EINVAL)
+ *   Results lie apart from each other and from all that a call reads (not looked at, but for these two): rows may be read again after results are written.
  * Rows behind the last sequence: what they hold is not used, and their results are zero.  Sums, memories and decays are in float32.  Matrix
  * products take operands in the type of the activations: query, key, value and d_out as they are; what is in float32, the memory and the products of rows with each
  * other, as the sum of two such numbers (16 bits in bfloat16, 22 in float16), so that what is seen of it in a result is the one rounding to its type.

@@ -525,6 +525,7 @@ def bagel_layer_norm_grad(x, d_out, d_x=None, *, weight=None, groups=1, eps=1e-5
 
 
 _ONE_ROW_EACH = object()         # in the place of offsets: as many sequences as rows
+_READ = ("query", "key", "value")
 
 
 def _attention(device, query, key, value, out, offsets, log_decay, scale):
@@ -557,6 +558,7 @@ def bagel_linear_attention(query, key, value, out, offsets, log_decay, *, scale=
     lib = _load()
     on, device = _stream(stream)
     rows, heads, states, dk, dv, code, n, head = _attention(device, query, key, value, _needed(out, "out"), offsets, log_decay, scale)
+    _marshal.apart(("out",), (out,), _READ, (query, key, value))
     workspace, space = _workspace(workspace, lib.bagel_linear_attention_workspace(head, 0), device, stream)
     args = head + _marshal.vectors(device, (n, states, dk, dv), ("initial", "final"), (initial, final)) + bytes(8 + 4 * 24 + 16) + space
     _done(lib, lib.bagel_linear_attention(args, on))
@@ -573,6 +575,7 @@ def bagel_linear_attention_grad(query, key, value, d_out, d_query, d_key, d_valu
             _marshal.heads(device, code, rows, ("d_out", "d_query", "d_key", "d_value"), (heads, dv, heads, dk, states, dk, states, dv),
                            (_needed(d_out, "d_out"), d_query, d_key, d_value)) +
             _marshal.vectors(device, (n, states, dk, dv), ("d_final", "d_initial"), (d_final, d_initial)) + space)
+    _marshal.apart(("d_query", "d_key", "d_value"), (d_query, d_key, d_value), _READ + ("d_out",), (query, key, value, d_out))
     _done(lib, lib.bagel_linear_attention_grad(args, on))
 
 
@@ -581,6 +584,7 @@ def bagel_linear_attention_step(query, key, value, state, out, log_decay, *, sca
     lib = _load()
     on, device = _stream(stream)
     rows, heads, states, dk, dv, code, n, head = _attention(device, query, key, value, _needed(out, "out"), _ONE_ROW_EACH, log_decay, scale)
+    _marshal.apart(("out",), (out,), _READ, (query, key, value))
     args = head + bytes(16) + _marshal.vectors(device, (n, states, dk, dv), ("state",), (_needed(state, "state"),)) + _NOTHING
     _done(lib, lib.bagel_linear_attention_step(args, on))
 

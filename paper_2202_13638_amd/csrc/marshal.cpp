@@ -3,6 +3,7 @@
 // Errors are Python's ValueError; nothing here touches the GPU.
 #include <Python.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstring>
 #include <string>
@@ -161,6 +162,50 @@ PyObject *heads(PyObject *, PyObject *const *args, Py_ssize_t n)
             out.insert(out.end(), {(int64_t)(intptr_t)t.data_ptr(), rows > 1 ? t.stride(0) : head * shape[1], head});
         }
         return bytes_of(out);
+    });
+}
+
+// Whether two tensors of heads, of as many rows, have an entry in the same place.  Where their rows or heads are different distances apart it is not found out (false), unless
+// one lies behind the other: parts of one projection have the same.
+bool meet(const at::Tensor &x, const at::Tensor &y)
+{
+    struct place {
+        int64_t rows, heads, width, stride, head;
+        explicit place(const at::Tensor &t) : rows(t.size(0)), heads(t.size(1)), width(t.size(2)), stride(rows > 1 ? t.stride(0) : 0), head(heads > 1 ? t.stride(1) : 0) {}
+        int64_t reach() const { return (rows - 1) * stride + (heads - 1) * head + width; }
+    };
+    if (x.numel() == 0 || y.numel() == 0) return false;
+    const place a(x), b(y);
+    const int64_t bytes = x.element_size(), apart = (int64_t)((intptr_t)y.data_ptr() - (intptr_t)x.data_ptr());
+    if (apart >= a.reach() * bytes || -apart >= b.reach() * bytes) return false;
+    if (a.stride != b.stride || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return false;
+    const int64_t head = a.heads > 1 ? a.head : b.head;
+    for (int64_t h = 1 - b.heads; h < a.heads; ++h) {                 // the difference of their heads, and those of their rows at which such heads are nearest
+        const int64_t off = h * head * bytes - apart, row = a.stride * bytes, nearest = row > 0 ? -off / row : 0;
+        for (int64_t r = std::max(nearest - 1, 1 - a.rows); r <= std::min(nearest + 1, a.rows - 1); ++r) {
+            const int64_t from = r * row + off;                       // from an entry of y to one of x
+            if (from < b.width * bytes && -from < a.width * bytes) return true;
+        }
+    }
+    return false;
+}
+
+// apart(names, results, names, tensors): refuses results in the place of one of the tensors, or of each other; None: left out
+PyObject *apart(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        if (n != 4 || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || !PyTuple_Check(args[2]) || !PyTuple_Check(args[3])) throw refused{"apart(names, results, names, tensors)"};
+        const Py_ssize_t results = PyTuple_GET_SIZE(args[1]), others = PyTuple_GET_SIZE(args[3]);
+        for (Py_ssize_t i = 0; i < results; ++i) {
+            PyObject *const o = PyTuple_GET_ITEM(args[1], i);
+            if (o == Py_None) continue;
+            for (Py_ssize_t j = i + 1; j < results + others; ++j) {
+                PyObject *const other = j < results ? PyTuple_GET_ITEM(args[1], j) : PyTuple_GET_ITEM(args[3], j - results);
+                if (other == Py_None || !meet(THPVariable_Unpack(o), THPVariable_Unpack(other))) continue;
+                throw refused{std::string(name_of(args[0], i)) + " may not be in the place of " + (j < results ? name_of(args[0], j) : name_of(args[2], j - results))};
+            }
+        }
+        Py_RETURN_NONE;
     });
 }
 
@@ -345,6 +390,7 @@ PyMethodDef METHODS[] = {{"first", (PyCFunction)(void *)first, METH_FASTCALL, nu
                          {"vectors", (PyCFunction)(void *)vectors, METH_FASTCALL, nullptr},
                          {"first_heads", (PyCFunction)(void *)first_heads, METH_FASTCALL, nullptr},
                          {"heads", (PyCFunction)(void *)heads, METH_FASTCALL, nullptr},
+                         {"apart", (PyCFunction)(void *)apart, METH_FASTCALL, nullptr},
                          {"clip", (PyCFunction)(void *)clip, METH_FASTCALL, nullptr},
                          {"adamw", (PyCFunction)(void *)adamw, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -1,6 +1,7 @@
 """Calls of linear attention, layer norm and clipping that their documentation allows: sizes, places and values that other tests do not have."""
 import ctypes as C
 import itertools
+import random
 
 import pytest
 import torch
@@ -79,3 +80,68 @@ def test_a_decay_that_is_nan_is_seen(heads, states, dk, dv, lengths, dtype):
     if len(q) == len(lengths):
         binding.bagel_linear_attention_step(q, k, v, state, out, ld.cuda())
         assert state[:, 1].isnan().all() and out[:, heads // 2:].isnan().all() and state[:, 0].isfinite().all() and out[:, :heads // 2].isfinite().all()
+
+
+def test_tensors_of_heads_that_meet():
+    """Against sets of places: refused only where an entry is shared, and always where rows and heads are the same distances apart."""
+    from paper_2202_13638_amd import _marshal
+    g, buffer, hits, misses = random.Random(1), torch.zeros(400), 0, 0
+    place = torch.arange(400.0)
+
+    def refused(x, y):
+        try:
+            _marshal.apart(("x",), (x,), ("y",), (y,))
+        except ValueError as e:
+            assert str(e) == "x may not be in the place of y"
+            return True
+        return False
+
+    for _ in range(20000):
+        rows = g.randint(1, 5)
+        strides = [(g.choice([0, 3, 7, 12, 24, 40]), g.choice([0, 2, 5, 8, 13]))] * 2
+        if g.random() < 0.2:
+            strides[1] = (g.randint(0, 40), g.randint(0, 13))
+        shapes = [(rows, g.randint(1, 4), g.randint(1, 6)) for _ in range(2)]
+        x, y = (torch.as_strided(buffer, s, (*d, 1), g.randint(0, 60)) for s, d in zip(shapes, strides))
+        a, b = (set(torch.as_strided(place, t.shape, t.stride(), t.storage_offset()).flatten().tolist()) for t in (x, y))
+        if a & b:
+            hits += refused(x, y)
+            assert refused(x, y) or strides[0] != strides[1], (x.shape, x.stride(), x.storage_offset(), y.shape, y.stride(), y.storage_offset())
+        else:
+            misses += 1
+            assert not refused(x, y)
+    assert hits > 3000 and misses > 3000
+    # and results with each other
+    x = torch.zeros(6, 2, 8)
+    with pytest.raises(ValueError, match="a may not be in the place of b"):
+        _marshal.apart(("a", "b"), (x, x), (), ())
+    _marshal.apart(("a", "b"), (x, None), ("c",), (None,))
+
+
+@gpu
+def test_results_in_the_place_of_what_is_read_are_refused():
+    """The gradients of keys read the values again where both are not made at once, and rows with what is not finite are gone through once more."""
+    proj = torch.randn(90, 3 * 2 * 16, device="cuda", dtype=torch.bfloat16)
+    q, k, v = (proj[:, 32 * i:32 * i + 32].unflatten(1, (2, 16)) for i in range(3))
+    d, ld, new = torch.randn(90, 2, 16, device="cuda", dtype=torch.bfloat16), torch.tensor([-0.1, -0.2], device="cuda"), torch.empty_like(proj).unflatten(1, (3, 2, 16))
+    for out in (q, k, v, proj[:, 8:40].unflatten(1, (2, 16))):
+        with pytest.raises(ValueError, match="out may not be in the place of"):
+            binding.bagel_linear_attention(q, k, v, out, 1, ld)
+        with pytest.raises(ValueError, match="out may not be in the place of"):
+            binding.bagel_linear_attention_step(q, k, v, torch.zeros(90, 2, 16, 16, device="cuda"), out, ld)
+    for place, bad in itertools.product(range(3), (q, k, v, d)):
+        outs = [new[:, i] for i in range(3)]
+        outs[place] = bad
+        with pytest.raises(ValueError, match=f"d_{('query', 'key', 'value')[place]} may not be in the place of"):
+            binding.bagel_linear_attention_grad(q, k, v, d, *outs, 1, ld)
+    with pytest.raises(ValueError, match="d_query may not be in the place of d_value"):
+        binding.bagel_linear_attention_grad(q, k, v, d, new[:, 0], new[:, 1], new[:, 0], 1, ld)
+    # parts of one projection, and of the gradient of one, lie apart
+    out = torch.empty_like(d)
+    binding.bagel_linear_attention(q, k, v, out, 1, ld)
+    binding.bagel_linear_attention_grad(q, k, v, d, new[:, 0], new[:, 1], new[:, 2], 1, ld)
+    wide = torch.zeros(90, 4 * 2 * 16, device="cuda", dtype=torch.bfloat16)              # and a result beside what is read
+    wide[:, :96] = proj
+    parts = [wide[:, 32 * i:32 * i + 32].unflatten(1, (2, 16)) for i in range(4)]
+    binding.bagel_linear_attention(*parts, 1, ld)
+    assert torch.equal(parts[3], out) and torch.equal(wide[:, :96], proj)
