@@ -569,7 +569,8 @@ int bagel_linear_attention_step(const bagel_attention *args, void *hip_stream);
  * The norm of the gradients of many tensors together, of any of the three types each, and their clipping:
  *   norm[0] = |grad_scale[0]| sqrt(sum of g^2 over all tensors),   factor[0] = grad_scale[0] min(1, max_norm / (norm + eps)),   out = g * factor
  * grad_scale is a device scalar, NULL: one.  factor is what bagel_adamw_step takes as its grad_scale, and no gradient needs to be written then: out may be
- * NULL, for some tensors or all.  out may be the gradient itself, but overlap nothing else that is read for a result or written (EINVAL).  Where the norm is not finite, factor is NaN (bagel_adamw_step then changes nothing) and
+ * NULL, for some tensors or all.  out may be the gradient itself, but overlap no other tensor of the call that is read for a result or written (EINVAL).  norm, factor,
+ * grad_scale and the work space are places of their own (not looked at; factor may be grad_scale).  Where the norm is not finite, factor is NaN (bagel_adamw_step then changes nothing) and
  * out is left as it was.  Squares and sums are in float64: a norm is finite wherever float32 holds it.  The sum has an order that depends on the counts alone.
  * The tensors are an array on the host, read before the call returns; any number, of any count >= 0, at any alignment of their type.
  * Work space: bagel_clip_norm_workspace(n_tensors) bytes.  max_norm >= 0 (infinity: no clipping), eps > 0.  Errors: EINVAL, EHIP.

@@ -606,6 +606,8 @@ def bagel_clip_norm(grads, max_norm, norm, factor, *, grad_scale=None, out=None,
         if not isinstance(t, _torch.Tensor) or t.numel() != 1 or t.dtype != _torch.float32 or t.get_device() != device:
             raise ValueError(f"{name} must hold one float32 value and be on the current GPU")
         places.append(t.data_ptr())
+    if places[1] in (places[0], places[2]):
+        raise ValueError("norm may not be in the place of factor or grad_scale")
     workspace, space = _workspace(workspace, lib.bagel_clip_norm_workspace(n), device, stream)
     try:
         options = _CLIP_OPTIONS.pack(max_norm, eps, *places)

@@ -145,3 +145,17 @@ def test_results_in_the_place_of_what_is_read_are_refused():
     parts = [wide[:, 32 * i:32 * i + 32].unflatten(1, (2, 16)) for i in range(4)]
     binding.bagel_linear_attention(*parts, 1, ld)
     assert torch.equal(parts[3], out) and torch.equal(wide[:, :96], proj)
+
+
+@gpu
+def test_the_norm_has_a_place_of_its_own():
+    """The factor is written behind it; the factor itself may take the place of the scale that it is made of."""
+    g, one, other = [torch.full((5000,), 2.0, device="cuda")], torch.full((1,), 0.5, device="cuda"), torch.zeros(1, device="cuda")
+    with pytest.raises(ValueError, match="norm may not be in the place of"):
+        binding.bagel_clip_norm(g, 1.0, other, other)
+    with pytest.raises(ValueError, match="norm may not be in the place of"):
+        binding.bagel_clip_norm(g, 1.0, one, other, grad_scale=one)
+    norm, factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    binding.bagel_clip_norm(g, 1.0, norm, factor, grad_scale=one)
+    binding.bagel_clip_norm(g, 1.0, other, one, grad_scale=one)
+    assert torch.equal(one, factor) and torch.equal(other, norm) and abs(float(norm) - 5000 ** 0.5) < 1e-4
