@@ -34,8 +34,8 @@ class MemoryPolicy:
     def __init__(self, d_in: int, d_out: int, width: int, blocks: int, dtype=torch.bfloat16, state_bits: int = 32, seed: int = 0, heads: int = 0):
         g = torch.Generator().manual_seed(seed)
         self.width, self.blocks, self.dtype, self.seed, self.updates = width, blocks, dtype, seed, 0
-        if heads and width % heads:
-            raise ValueError("heads must divide the width")
+        if heads < 0 or heads and (width % heads or width // heads > binding.ATTENTION_MAX_WIDTH):
+            raise ValueError(f"heads must divide the width, into parts of {binding.ATTENTION_MAX_WIDTH} at most")
         self.memory = _Heads(width, heads) if heads else _Channels(width)
 
         def matrix(rows, columns):

@@ -159,3 +159,38 @@ def test_the_norm_has_a_place_of_its_own():
     binding.bagel_clip_norm(g, 1.0, norm, factor, grad_scale=one)
     binding.bagel_clip_norm(g, 1.0, other, one, grad_scale=one)
     assert torch.equal(one, factor) and torch.equal(other, norm) and abs(float(norm) - 5000 ** 0.5) < 1e-4
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lengths,heads,states,dk,dv", [([700], 8, 2, 64, 64), ([700], 4, 1, 128, 128), ([40, 2900], 8, 1, 24, 16), ([90, 1500], 2, 2, 64, 64)],
+                         ids=["joined by the parts", "wide", "joined by a launch", "a head to a memory"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_is_not_finite_in_a_sequence_that_is_shared_out(bad, lengths, heads, states, dk, dv, dtype):
+    """Segments before it, and the rows of its own segment before it, have the results that they have without it; those behind it have nothing finite where it is."""
+    t, n = TYPES[dtype], sum(lengths)
+    at, first = n - 333, n - lengths[-1]
+    x, _ = _attention_inputs(lengths, heads, states, dk, dv, t, seed=51)
+    ld = torch.full((states,), -0.004)
+    want, terms = _attention_want(x, lengths, ld, 0.2)
+    clean = _attention_all(x, lengths, ld, 0.2)
+    g = heads // states
+    before, behind = slice(0, at), slice(at + 1, n)
+    for name, places in (("v", {"out": before}), ("k", {"out": before, "d_query": before}), ("q", {"d_key": behind, "d_value": behind}), ("d_out", {"d_key": behind, "d_value": behind})):
+        y = dict(x, **{name: x[name].clone()})
+        y[name][at, 0, 2] = bad
+        got = _attention_all(y, lengths, ld, 0.2)
+        for k, rows in places.items():
+            _near(got[k][rows], want[k][rows], f"{k} for {name}", terms[k][rows], 0.0 if dtype == "f32" else 2 * HALF_ULP[t])
+        for k, v in got.items():                     # the other sequence and the other memory
+            if k in ("final", "d_initial"):
+                assert torch.equal(v[:-1], clean[k][:-1]) and torch.equal(v[:, 1:], clean[k][:, 1:]), (name, k)
+            else:
+                of = g if v.shape[1] == heads else 1
+                assert torch.equal(v[:first], clean[k][:first]) and torch.equal(v[:, of:], clean[k][:, of:]), (name, k)
+        hit = {"v": got["out"][at:, :g, 2], "k": got["out"][at:, :g], "q": got["d_value"][first:at + 1, 0], "d_out": got["d_value"][first:at + 1, 0, 2]}[name]
+        assert not hit.isfinite().any(), name
+        if name in "vk":
+            assert not got["final"][-1, 0].isfinite().all()
+        else:
+            assert not got["d_initial"][-1, 0].isfinite().all()
