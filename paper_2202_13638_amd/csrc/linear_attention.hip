@@ -137,23 +137,22 @@ __global__ __launch_bounds__(256) void step_kernel(int64_t rows, int states, int
     }
 }
 
-// Rows of a segment: as many segments as the card takes at a time, some less, as one more would be a round of its own; but no shorter than is worth a memory that is
+// Rows of a segment: as many segments as the card takes at a time, some less, as one more is a round of its own; but no shorter than is worth a memory that is
 // written and read.  Where there are sequences enough, they are left whole, and only one that is far longer than the others is shared out.
-//   An odd number of chunks: workgroups go through their rows side by side, and with a power of two between them they ask the same channels of the memory
-// (131072 rows, 8 heads of 128 on 2 memories, bf16: 259 us with 16 chunks and 256 workgroups, 162 with 18 chunks and 228).
+//   131072 rows in one sequence, bf16, by chunks to a segment: 8 heads of 128 on 2 memories, 16 chunks (258 workgroups, of which 256 fit) 353 us, 17 to 20 (242 to 206
+// workgroups) 244, 242, 242 and 244, 24 279; 8 heads of 64 on 8 memories, 32 chunks (520 workgroups, of which 512 fit) 227, 33 to 36 202, 204, 199 and 204, 40 208.
 int64_t wanted_groups(const bagel_attention &b) { return b.key_width > 64 || b.value_width > 64 ? 248 : 496; }      // one or two workgroups to a compute unit
 int64_t segment_rows(const bagel_attention &b)
 {
     constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
-    // What a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits, two in 32.  (Of 8 heads of 64 in
-    // bf16 on 8 memories, 20 sequences of up to 4000 rows: 486 us by segments of one chunk, 249 by eight.  10007 rows, 61 sequences, 6 heads of 40 and 77 on 3
-    // memories, float32: between 356 and 375 us with one to four chunks, 563 with seven.)
+    // What a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits, two in 32.  That is for sequences
+    // enough (8 heads of 64 on 8 memories, bf16, 61 sequences of 20000 rows: 46 us with eight chunks, 58 with four, 62 with two; f32, 10007 rows of 6 heads of 40 and 77 on 3,
+    // 91 with two, 87 with one, 105 with three); one short sequence would do with fewer (8000 rows, bf16: 38 with eight, 27 with four).
     const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 4 : 1), least = step < 8 ? 8 / step : 1;
     const int64_t wanted = wanted_groups(b);
     int64_t rows = (b.rows * b.states + wanted - 1) / wanted;
-    if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = rows > 2 * b.rows / b.sequences ? rows : 2 * b.rows / b.sequences;
-    const int64_t chunks = (rows + chunk - 1) / chunk;
-    return chunk * (chunks <= least ? least : chunks == 2 ? 2 : chunks | 1);
+    if (b.sequences > 0 && (int64_t)b.sequences * b.states >= wanted) rows = std::max(rows, 2 * b.rows / b.sequences);
+    return chunk * std::max((rows + chunk - 1) / chunk, least);
 }
 
 // A segment's rows, and how many numbers there are for segments that are not the first of their sequence.

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2202_13638_amd import binding
-from test_more_operators import HALF_ULP, TYPES, _attention_all, _attention_inputs, _attention_struct, _attention_want, _near
+from test_more_operators import (HALF_ULP, TYPES, _attention_all, _attention_check, _attention_inputs, _attention_struct, _attention_want, _near)
 
 gpu = pytest.mark.gpu
 
@@ -194,3 +194,15 @@ def test_what_is_not_finite_in_a_sequence_that_is_shared_out(bad, lengths, heads
             assert not got["final"][-1, 0].isfinite().all()
         else:
             assert not got["d_initial"][-1, 0].isfinite().all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [1600, 1536, 1537])
+def test_segments_of_four_chunks(rows, dtype):
+    """Many memories of one sequence, so that segments are longer than the least: of an even number of chunks."""
+    t = TYPES[dtype]
+    x, ld = _attention_inputs([rows], 256, 64, 8, 12, t, seed=52)
+    ld = torch.linspace(-0.05, -0.001, 64)
+    want, terms = _attention_want(x, [rows], ld, 0.2)
+    _attention_check(_attention_all(x, [rows], ld, 0.2), want, terms, t)
