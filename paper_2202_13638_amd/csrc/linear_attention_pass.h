@@ -563,6 +563,8 @@ template <typename T, int W, int NB> __device__ __forceinline__ void remember(fl
             for (int j = 0; j < 4; ++j) x[j] = fmaf(S[bt][j], keep, x[j] * up);
         }
         S[bt] = x;
+        // Tile after tile: of eight at a time, registers go to memory and back (64000 rows, 8 heads of 128, float16, the gradient 680 us, 532 so).
+        if constexpr (W == 128 && sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (sizeof(T) == 4) settle(S);
 }
@@ -1040,6 +1042,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
 {
     if constexpr (WHOLE) p.wb = p.wc = q.wb = q.wc = W;
     constexpr int WAVES = W / 16, THREADS = 4 * W;
+    constexpr bool EARLY = W == 64;                  // two memories of 128 leave no registers for what is read ahead (8 heads of 100, float16, 712 us with it, 644 without)
     __shared__ tile<T, W> sk, sv, sq, sd, so[2];
     __shared__ pieces_of<T> sp[2];
     __shared__ powers w;
@@ -1110,11 +1113,11 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
             const float keep = MANY && h > 0 ? 1.0f : n == CHUNK ? whole : power(l2, n);
             const operand<T> d[2] = {sd.across(l.across_c, 0, wave), sd.across(l.across_c, 1, wave)}, c[2] = {sq.across(l.across_c, 0, wave), sq.across(l.across_c, 1, wave)};
             if (enter) {
-                from_memory<AHEAD<T, W, W>>(O[0], sk, R, weight_in, tile_on, l.along_a);
-                from_memory<AHEAD<T, W, W>>(O[1], sv, Rt, weight_in, tile_on, l.along_a);
+                from_memory<EARLY>(O[0], sk, R, weight_in, tile_on, l.along_a);
+                from_memory<EARLY>(O[1], sv, Rt, weight_in, tile_on, l.along_a);
             }
-            make_pieces<AHEAD<T, W, W>, WAVES>(sk, sq, sp[0], w, 0, tile_on, l.along_a, l.spread_b, wave);
-            make_pieces<AHEAD<T, W, W>, WAVES>(sv, sd, sp[1], w, 1, tile_on, l.along_a, l.spread_b, WAVES - 1 - wave);
+            make_pieces<EARLY, WAVES>(sk, sq, sp[0], w, 0, tile_on, l.along_a, l.spread_b, wave);
+            make_pieces<EARLY, WAVES>(sv, sd, sp[1], w, 1, tile_on, l.along_a, l.spread_b, WAVES - 1 - wave);
             remember(R, sq, d, w, keep, l.across_b);
             remember(Rt, sd, c, w, keep, l.across_b);
             __syncthreads();
@@ -1125,7 +1128,7 @@ template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__
                 for (int it = 0; it < 4; ++it) {
                     floats &o = O[which][it];
                     if (it < 3) sp[which].get(P[(it + 1) & 1], it + 1);
-                    reads_before_products<AHEAD<T, W, W>>();
+                    reads_before_products<EARLY>();
                     from_rows(o, x, P[it & 1], w, which, it);
                     if constexpr (MANY) settle(o);
                     if (!leave) continue;
