@@ -57,7 +57,8 @@ template <typename T> hipError_t bagel_launch_attention_memories(const bagel_att
 // The gradients of keys and values in one pass: `p` is that of the values (memory R, a = key, b = query, c = gradient of the results), `q` that of the
 // keys (R transposed, a = value, b = gradient of the results, c = query).  Only where bagel_attention_keys_fit.
 template <typename T> hipError_t bagel_launch_attention_keys(const bagel_attention_pass<T> &p, const bagel_attention_pass<T> &q, hipStream_t stream);
-// (Two memories of wide heads and the sums over several heads of queries are more than a lane's registers hold; in 32 bits the tiles leave room for one workgroup only.)
+// (Two memories of wide heads and the sums over several heads of queries are more than a lane's registers hold, and no other place for the sums has been built; in 32 bits the
+// tiles of 64 leave room for one workgroup only, those of 128 for none.)
 template <typename T> inline bool bagel_attention_keys_fit(int key_width, int value_width, int heads_to_a_memory)
 {
     return sizeof(T) == 2 && (key_width <= 64) == (value_width <= 64) && (key_width <= 64 || heads_to_a_memory == 1);

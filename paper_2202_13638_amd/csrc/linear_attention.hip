@@ -146,7 +146,7 @@ int64_t segment_rows(const bagel_attention &b)
 {
     constexpr int64_t chunk = BAGEL_ATTENTION_CHUNK;
     // What a segment's steps take is at least what the launches for the memories take: some eight steps of one head in 16 bits, two in 32.  That is for sequences
-    // enough (8 heads of 64 on 8 memories, bf16, 61 sequences of 20000 rows: 46 us with eight chunks, 58 with four, 62 with two; f32, 10007 rows of 6 heads of 40 and 77 on 3,
+    // enough (8 heads of 64 on 8 memories, bf16, 20000 rows in 61 sequences: 46 us with eight chunks, 58 with four, 62 with two; f32, 10007 rows in 61, 6 heads of 40 and 77 on 3,
     // 91 with two, 87 with one, 105 with three); one short sequence would do with fewer (8000 rows, bf16: 38 with eight, 27 with four).
     const int64_t step = (int64_t)(b.heads / b.states) * (b.dtype == BAGEL_FLOAT32 ? 4 : 1), least = step < 8 ? 8 / step : 1;
     const int64_t wanted = wanted_groups(b);

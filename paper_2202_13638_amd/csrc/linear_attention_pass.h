@@ -845,7 +845,7 @@ template <typename T, int WB, int WC, bool WHOLE, bool MANY> __global__ __launch
 }
 
 // What segments have added to the memory, into the memory behind each: a thread to an entry, along its sequence's segments but the last, 16 of which are asked for at
-// a time (114 segments of 2 memories of 128 x 128: 14 us).
+// a time (121 segments of 2 memories of 128 x 128: 14 us).
 template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two_passes<T> both, int blocks)
 {
     const bagel_attention_pass<T> p = blockIdx.y ? both.p[1] : both.p[0];
@@ -877,11 +877,14 @@ template <typename T> __global__ __launch_bounds__(256) void memories_kernel(two
 // A pass over a segment.  A wave to 16 columns of a memory, of c and of out, in float32 in its registers.  The rows' products with each other, P, are shared out
 // among the waves by pieces (16 rows of it, 32 rows they are multiplied with), and meet in shared memory.
 // WHOLE: a and b are as wide as their tiles, and so are c and out.
-//   In 16 bits the memory's rate bounds it: 64000 rows, 8 heads of 64, bf16, 56 us (262 MB, 4.7 TB/s); 131072 rows, 8 heads of 128 on 2 memories 157 to 180 us (671 MB, 4.3 to 3.7 TB/s).
-// What brought it there: one chunk of the next step on its way 175 -> 129 us (the former case with its other launches), loads without a branch and results in packs -> 79,
-// slots without bank conflicts and two steps on their way -> 62.  A workgroup has two compute units' neighbours at most (its tiles take 57 to 90 KB), so what is on its
-// way, not how many waves there are, keeps the memory busy.  In 32 bits the matrix instructions have a sixteenth of the rate, and padded widths count as whole.
-template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD> __global__ __launch_bounds__(4 * WC, ON_SIMD) void chunks_kernel(bagel_attention_pass<T> p)
+//   In 16 bits the memory's rate bounds it, and beside it what a step takes between its barriers: 64000 rows, 8 heads of 64, bf16, 59 to 65 us (262 MB, 4.4 to 4.0 TB/s); 131072
+// rows, 8 heads of 128 on 2 memories 182 to 202 us (671 MB, 3.7 to 3.3 TB/s).  What brought the former there, in whole calls: one chunk of the next step on its way 175 -> 129 us
+// (with other launches), loads without a branch and results in packs -> 79, slots without bank conflicts and two steps on their way -> 62, few segments' memories
+// joined by themselves -> 57, memories and P in two operands -> 63.
+//   Two waves to a SIMD are all that a lane's 190 to 256 registers leave room for: two workgroups to a compute unit with values of 64, one with 128.  (Their tiles take 50 to 82 KB
+// in 16 bits, 66 to 146 with a memory held for several heads, 69 to 117 in 32.)  So what is on its way, not how many waves there are, keeps the memory busy.  In 32 bits
+// the matrix instructions have a sixteenth of the rate, and padded widths count as whole.
+template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS> __global__ __launch_bounds__(4 * WC, 2) void chunks_kernel(bagel_attention_pass<T> p)
 {
     if constexpr (WHOLE) {
         p.wb = WB;
@@ -1037,7 +1040,7 @@ template <typename T, int WB, int WC, bool WHOLE, heads_kind HEADS, int ON_SIMD>
 }
 
 // The gradients of keys and values: two such passes at once, whose memories are each other's transpose, from the same tiles.  Four tiles are read in the place of six
-// (64000 rows, 8 heads of 64, bf16: 92 us for 393 MB, 4.3 TB/s; two passes one after the other took 130).
+// (64000 rows, 8 heads of 64, bf16: 98 to 108 us for 393 MB, 4.0 to 3.6 TB/s; when it took 92, two passes one after the other took 130).
 template <typename T, int W, bool WHOLE, bool MANY> __global__ __launch_bounds__(4 * W, 2) void keys_kernel(bagel_attention_pass<T> p, bagel_attention_pass<T> q)
 {
     if constexpr (WHOLE) p.wb = p.wc = q.wb = q.wc = W;
@@ -1202,13 +1205,13 @@ template <typename T> hipError_t bagel_launch_attention_pass(const bagel_attenti
     p.groups = groups_of(p);
     hipError_t e = hipSuccess;
     by_widths(p, [&](auto wb, auto wc, auto whole) {
-        constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value, ON_SIMD = sizeof(T) == 4 && WB == 128 && WC == 64 ? 1 : 2;
+        constexpr int WB = decltype(wb)::value, WC = decltype(wc)::value;
         constexpr bool WHOLE = decltype(whole)::value;
         e = bagel_attention_launches(p.groups, [&](unsigned groups, int64_t before) {
             p.launched = before;
-            if (p.ks > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_B, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
-            else if (p.qs > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_A, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
-            else chunks_kernel<T, WB, WC, WHOLE, ONE, ON_SIMD><<<groups, 4 * WC, 0, stream>>>(p);
+            if (p.ks > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_B><<<groups, 4 * WC, 0, stream>>>(p);
+            else if (p.qs > 1) chunks_kernel<T, WB, WC, WHOLE, MANY_A><<<groups, 4 * WC, 0, stream>>>(p);
+            else chunks_kernel<T, WB, WC, WHOLE, ONE><<<groups, 4 * WC, 0, stream>>>(p);
         });
     });
     return e;
