@@ -374,10 +374,10 @@ template <int NB> __device__ __forceinline__ void write_memory(const floats (&S)
 
 // What is in float32 and becomes an operand, the memory before a chunk and P, is a sum of so many of them.  In 16 bits one alone would round it to 8 or 11 bits, which would be
 // seen in the results (64000 rows, 8 heads of 64, bf16: 0.0023 from 64 bits, where the rounding of the results alone makes 0.0017).  Two hold 16 or 22 bits, of whose
-// rounding nothing is left in results of 8 or 11.  They take 5 to 10 % of the time (that case 57 us with one, 63 with two; its gradient 181 and 193).
+// rounding nothing is left in results of 8 or 11.  They take up to 12 % of the time (that case 57 us with one, 63 with two; its gradient 181 and 193).
 template <typename T> constexpr int PARTS = sizeof(T) == 4 ? 1 : 2;
 // All parts but the last are cut off: what is left is exact, as it would be behind a rounding, which the compiler makes once for the operand and once more for what is left
-// (842 instead of 612 vector instructions in two steps, 716 so).
+// (844 instead of 612 vector instructions in two steps; 716 so).
 template <typename T, int N> __device__ __forceinline__ void in_parts(float (&x)[8], operand<T> (&part)[N])
 {
     using words = uint32_t __attribute__((ext_vector_type(4)));
